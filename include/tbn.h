@@ -321,6 +321,57 @@ tbn_status tbn_sgd_step_quantize(float* w, float* v, const float* g, int64_t k, 
                                  float momentum, float weight_decay, uint32_t* codes, float* alpha,
                                  int32_t* counts, hipStream_t stream);
 
+/*
+ * AdamW over many tensors at once (Adam with decoupled weight decay), for what is trained beside the
+ * two-bit filters: normalisation parameters, low-rank adapters, real weights.  In place, for every element,
+ * with t = step counted from 1:
+ *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2;
+ *   w = w - lr weight_decay w - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)     (fp32)
+ *   tensors  `n` of them in host memory (read during the call only): w [count] fp32, g [count] of type
+ *            gt, the weight decay, and the moments:
+ *            TBN_STATE_F32   m, v [count] fp32; m_scale, v_scale unused.
+ *            TBN_STATE_E4M3  m, v [count] E4M3 codes (the format of tbn_quantize_act_fp8) of the first
+ *                            moment and of the root of the second, over a scale for every 256 elements:
+ *                            moment = code * m_scale[i / 256], second moment = (code * v_scale[i / 256])^2,
+ *                            m_scale, v_scale [ceil(count / 256)] fp32.  All zero is the state before the
+ *                            first step.  The moments are updated in fp32, each operation rounded by itself;
+ *                            then scale = (largest finite magnitude of the 256) * (1 / 448), and a code is
+ *                            the value times 448 * (1 / largest), rounded to one of its two neighbours, away
+ *                            from zero with the probability of its distance from the one nearer to zero, so
+ *                            that moments that move by less than a code's step arrive on average.  The random
+ *                            numbers are a function of seed, step, the tensor's place in the list and the element (mod
+ *                            2^32): the same call gives the same bits.  256 values below 2^-100 are stored as
+ *                            zeros, a value that is not finite as NaN.
+ *   hyper    lr, beta1, beta2 in [0, 1), eps >= 0, step, seed.  step_dev / lr_dev (optional) replace step
+ *            and lr by values in device memory, read when the kernel runs (for captured steps, which the
+ *            caller advances between replays); *step_dev >= 1 is the caller's to keep.
+ * w, m, v and the scales need no alignment beyond their elements' (views into flat buffers); 16-byte aligned
+ * ones are faster.  No two of the written arrays may overlap (TBN_ERR_SHAPE): among them is a tensor listed twice.
+ */
+typedef enum tbn_state { TBN_STATE_F32 = 0, TBN_STATE_E4M3 = 1 } tbn_state;
+
+typedef struct tbn_adamw_tensor {
+    float* w;
+    void* m;
+    void* v;
+    const void* g;
+    float* m_scale;
+    float* v_scale;
+    int64_t count;
+    float weight_decay;
+} tbn_adamw_tensor;
+
+typedef struct tbn_adamw_hyper {
+    double lr, beta1, beta2, eps;
+    int32_t step;
+    uint32_t seed;
+    const int32_t* step_dev;
+    const float* lr_dev;
+} tbn_adamw_hyper;
+
+tbn_status tbn_adamw_step(const tbn_adamw_tensor* tensors, int32_t n, tbn_state state, tbn_dtype gt,
+                          const tbn_adamw_hyper* hyper, hipStream_t stream);
+
 /* ------------------------------------------------------------------------------------ */
 /* Layers around the two-bit convolutions in the workloads (Sec. 4 names ResNet-18 with   */
 /* batch normalisation; the smaller workloads add max pooling, ReLU and a softmax         */
@@ -374,6 +425,21 @@ tbn_status tbn_batchnorm_train_bwd(const void* x, const void* y, const void* dy,
                                    int32_t relu, const float* mean, const float* inv_std, const float* gamma,
                                    float* dgamma, float* dbeta, void* dx, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* Layer normalisation of `rows` rows of c values: y = (x - mean) inv_std gamma + beta with the row's mean and
+ * inv_std = 1/sqrt(biased var + eps), all in fp32.  x has dtype xt, y yt; gamma and beta [c] are optional (1 and
+ * 0), and so are the outputs mean and inv_std [rows], which the backward pass takes.  rows * c at most 2^40. */
+tbn_status tbn_layernorm_fwd(const void* x, tbn_dtype xt, int64_t rows, int32_t c, const float* gamma,
+                             const float* beta, float eps, void* y, tbn_dtype yt, float* mean, float* inv_std,
+                             hipStream_t stream);
+
+/* Backward of the above: with xhat = (x - mean) inv_std and h = dy gamma, dx = inv_std (h - mean(h) - xhat
+ * mean(h xhat)) (the means over a row), dgamma = sum over the rows of dy xhat, dbeta = sum of dy [c].  dy has y's dtype
+ * yt, dx x's.  Deterministic: partial sums in ws (tbn_layernorm_workspace_size bytes), added in a fixed order. */
+tbn_status tbn_layernorm_workspace_size(int64_t rows, int32_t c, size_t* bytes);
+tbn_status tbn_layernorm_bwd(const void* x, tbn_dtype xt, const void* dy, tbn_dtype yt, int64_t rows, int32_t c,
+                             const float* mean, const float* inv_std, const float* gamma, void* dx, float* dgamma,
+                             float* dbeta, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* dx = dy where y > 0, else 0 (ReLU'(0) = 0). */
 tbn_status tbn_relu_bwd(const void* y, const void* dy, int64_t count, void* dx, hipStream_t stream);
 
@@ -385,6 +451,40 @@ tbn_status tbn_relu_bwd(const void* y, const void* dy, int64_t count, void* dx, 
  * out of bounds. */
 tbn_status tbn_softmax_xent(const float* logits, const int32_t* labels, int32_t n, int32_t classes, float* loss,
                             float* loss_per_sample, void* dlogits, hipStream_t stream);
+
+/*
+ * Low-rank adapters of many requests beside a shared two-bit projection (a fully-connected layer C -> K whose
+ * codes cannot be moved by small steps): row i of a batch has the adapter index[i] of a bank, or none.
+ *   desc     rows of the batch, C inputs, K outputs, rank R (1 to 128), adapters S in the bank (1 to 65535).
+ *   index    [rows] int32; a value outside [0, S) (such as -1) is no adapter: that row's product is zero.
+ *            Rows may come in any order; those of one adapter side by side run fastest.
+ *   a, b     [S][R][C] and [S][K][R], dtype wt.   scale  [S] fp32, optional (1).
+ *
+ * tbn_adapter_fwd:  t = A x (fp32, optional output [rows][R], for the backward pass),
+ *   y = residual + scale B t.  x [rows][C] dtype xt; residual (optional) and y [rows][K] dtype yt; residual may be y.
+ *   Given to tbn_conv2d_fwd as its epilogue's residual, y adds the adapters to the projection before bias-free
+ *   activation: act(alpha_k (x W~) + bias + y).
+ * tbn_adapter_bwd:  dt = scale B^T dy, dx = residual + A^T dt (residual: the projection's own gradient, optional; it may be
+ *   dx), da = sum over the adapter's rows of dt x, db = scale * sum of dy t, fp32, shaped as a and b and overwritten (zero
+ *   for an adapter without rows).  dy [rows][K] dtype dyt; dx and residual [rows][C] dtype dxt; t from the forward pass.
+ *   dx, da and db are each optional; one has to be given.
+ * Products are exact (of fp32 factors but for 2^-23 of them), sums and t are fp32 in a fixed order.
+ * ws: tbn_adapter_workspace_size bytes for TBN_OP_FWD (forward) or TBN_OP_BWD_DATA (backward).
+ * Limits: rows <= 2^27, C and K <= 2^24, S R C and S R K < 2^31 (TBN_ERR_SHAPE).
+ */
+typedef struct tbn_adapter_desc {
+    int64_t rows;
+    int32_t c, k, rank, adapters;
+} tbn_adapter_desc;
+
+tbn_status tbn_adapter_workspace_size(tbn_op op, const tbn_adapter_desc* desc, size_t* bytes);
+tbn_status tbn_adapter_fwd(const tbn_adapter_desc* desc, const void* x, tbn_dtype xt, const int32_t* index, const void* a,
+                           const void* b, tbn_dtype wt, const float* scale, const void* residual, void* y, tbn_dtype yt,
+                           float* t, void* ws, size_t ws_bytes, hipStream_t stream);
+tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtype xt, const void* dy, tbn_dtype dyt,
+                           const int32_t* index, const void* a, const void* b, tbn_dtype wt, const float* scale,
+                           const float* t, const void* residual, void* dx, tbn_dtype dxt, float* da, float* db, void* ws,
+                           size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

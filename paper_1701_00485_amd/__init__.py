@@ -19,6 +19,8 @@ Calls (same names as the C ABI, without the ``tbn_`` prefix):
   conv2d_bwd_weight(desc, x, dy)    Sec. 3 (straight-through) -> dW
   sgd_step(w, v, g, lr, momentum, weight_decay)  Sec. 4 optimiser
   sgd_step_quantize(w, v, g, lr, ...)  the update fused with the next quantisation
+  layernorm_fwd / layernorm_bwd, adamw_step, adapter_fwd / adapter_bwd: what is trained and served beside
+                                   frozen two-bit filters
 """
 from __future__ import annotations
 
@@ -116,6 +118,14 @@ def load():
                                     i32),
         "tbn_relu_bwd": ([vp, vp, i64, vp, vp], i32),
         "tbn_softmax_xent": ([vp, vp, i32, i32, vp, vp, vp, vp], i32),
+        "tbn_layernorm_fwd": ([vp, i32, i64, i32, vp, vp, f32, vp, i32, vp, vp, vp], i32),
+        "tbn_layernorm_workspace_size": ([i64, i32, vp], i32),
+        "tbn_layernorm_bwd": ([vp, i32, vp, i32, i64, i32, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp], i32),
+        "tbn_adamw_step": ([vp, i32, i32, i32, vp, vp], i32),
+        "tbn_adapter_workspace_size": ([i32, vp, vp], i32),
+        "tbn_adapter_fwd": ([vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, i32, vp, vp, ctypes.c_size_t, vp], i32),
+        "tbn_adapter_bwd": ([vp, vp, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, ctypes.c_size_t, vp],
+                            i32),
         "tbn_conv2d_fwd_noalloc": ([vp, vp, i32, vp, vp, vp, vp, i32, vp], i32),
         "tbn_tuning_set": ([i32, i32], i32),
         "tbn_tuning_get": ([i32], i32),
@@ -167,6 +177,8 @@ def exported_symbols():
                    "tbn_conv2d_bwd_weight", "tbn_sgd_step", "tbn_sgd_step_quantize", "tbn_pool_out_dims", "tbn_maxpool2d_fwd",
                    "tbn_maxpool2d_bwd", "tbn_avgpool_global", "tbn_batchnorm_workspace_size",
                    "tbn_batchnorm_train_fwd", "tbn_batchnorm_train_bwd", "tbn_relu_bwd", "tbn_softmax_xent",
+                   "tbn_layernorm_fwd", "tbn_layernorm_workspace_size", "tbn_layernorm_bwd", "tbn_adamw_step",
+                   "tbn_adapter_workspace_size", "tbn_adapter_fwd", "tbn_adapter_bwd",
                    "tbn_tuning_set", "tbn_tuning_get", "tbn_conv2d_fwd_noalloc"])
 
 
@@ -744,3 +756,264 @@ def softmax_xent(logits, labels):
     _call("tbn_softmax_xent", _dev(logits, "logits", (torch.float32,)), _dev(labels, "labels", (torch.int32,)),
           n, k, _dev(loss, "loss"), _dev(per, "per"), _dev(dz, "dz"), _stream())
     return loss, dz
+
+
+# --------------------------------------------------------------------------------------
+# What is trained and served beside frozen two-bit filters: layer normalisation, AdamW over many
+# tensors, low-rank adapters.  These calls run on the device of their tensors, on its current stream.
+# --------------------------------------------------------------------------------------
+STATE_F32, STATE_E4M3 = 0, 1
+STATE_BLOCK = 256  # elements of an 8-bit state that share a scale
+MAX_RANK = 128
+_F32, _FLOATS = (torch.float32,), (torch.bfloat16, torch.float32)
+
+
+def _beside(t, name, like, dtypes):
+    """The pointer of an operand that has to lie on the device of `like`; None for one that is not given."""
+    if t is None:
+        return None
+    p = _dev(t, name, dtypes)
+    if t.device != like.device:
+        raise ValueError("%s is on %s, expected %s" % (name, t.device, like.device))
+    return p
+
+
+def _call_on(x, name, *args):
+    with torch.cuda.device(x.device):
+        _call(name, *args, _stream())
+
+
+def layernorm_workspace_size(rows: int, c: int) -> int:
+    b = ctypes.c_size_t()
+    _call("tbn_layernorm_workspace_size", int(rows), int(c), ctypes.byref(b))
+    return b.value
+
+
+def _rows_of(x):
+    if x.dim() < 1 or x.numel() < 1:
+        raise ValueError("x has no values")
+    return x.numel() // x.shape[-1], x.shape[-1]
+
+
+def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, out_dtype=None, want_stats=True):
+    """Layer normalisation over the last axis: y = (x - mean) inv_std gamma + beta; x bf16 or fp32, gamma and beta
+    fp32 [C] or None (1 and 0), y of `out_dtype` (default: x's).  Returns (y, mean, inv_std), the statistics fp32 [rows]
+    (None without `want_stats`)."""
+    out = (_native or _load_native()).layernorm_fwd(x, gamma, beta, eps, out_dtype, want_stats)
+    if out is not NotImplemented:
+        return out
+    rows, c = _rows_of(x)
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    _at_least(gamma, c, "gamma")
+    _at_least(beta, c, "beta")
+    xt, yt = _dtype_code(x.dtype), _dtype_code(out_dtype)
+    px, pg, pb = _dev(x, "x"), _beside(gamma, "gamma", x, _F32), _beside(beta, "beta", x, _F32)
+    y = torch.empty(x.shape, dtype=out_dtype, device=x.device)
+    mean, inv_std = (torch.empty(rows, dtype=torch.float32, device=x.device) if want_stats else None for _ in range(2))
+    _call_on(x, "tbn_layernorm_fwd", px, xt, rows, c, pg, pb, float(eps), _dev(y, "y"), yt,
+             _beside(mean, "mean", x, _F32), _beside(inv_std, "inv_std", x, _F32))
+    return y, mean, inv_std
+
+
+def layernorm_bwd(x, dy, mean, inv_std, gamma=None, ws=None, dgamma=None, dbeta=None):
+    """Returns (dx, dgamma, dbeta): dx of x's type and shape, dgamma and dbeta fp32 [C] (caller-provided ones are
+    written: for example views into one flat gradient buffer)."""
+    out = (_native or _load_native()).layernorm_bwd(x, dy, mean, inv_std, gamma, ws, dgamma, dbeta)
+    if out is not NotImplemented:
+        return out
+    rows, c = _rows_of(x)
+    _numel(dy, x.numel(), "dy")
+    _at_least(mean, rows, "mean")
+    _at_least(inv_std, rows, "inv_std")
+    _at_least(gamma, c, "gamma")
+    for t, name in ((dgamma, "dgamma"), (dbeta, "dbeta")):
+        if t is not None:
+            _numel(t, c, name)
+    px, pd = _dev(x, "x", _FLOATS), _beside(dy, "dy", x, _FLOATS)
+    pm, pi, pg = (_beside(t, name, x, _F32) for t, name in ((mean, "mean"), (inv_std, "inv_std"), (gamma, "gamma")))
+    dx = torch.empty_like(x)
+    if dgamma is None:
+        dgamma = torch.empty(c, dtype=torch.float32, device=x.device)
+    if dbeta is None:
+        dbeta = torch.empty(c, dtype=torch.float32, device=x.device)
+    if ws is None:
+        ws = torch.empty(layernorm_workspace_size(rows, c), dtype=torch.uint8, device=x.device)
+    _call_on(x, "tbn_layernorm_bwd", px, _dtype_code(x.dtype), pd, _dtype_code(dy.dtype), rows, c, pm, pi, pg,
+             _dev(dx, "dx"), _beside(dgamma, "dgamma", x, _F32), _beside(dbeta, "dbeta", x, _F32),
+             _beside(ws, "ws", x, None), ws.numel() * ws.element_size())
+    return dx, dgamma, dbeta
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("w", "m", "v", "g", "m_scale", "v_scale")] + [
+        ("count", ctypes.c_int64), ("weight_decay", ctypes.c_float)]
+
+
+class AdamwHyper(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_double) for f in ("lr", "beta1", "beta2", "eps")] + [
+        ("step", ctypes.c_int32), ("seed", ctypes.c_uint32), ("step_dev", ctypes.c_void_p), ("lr_dev", ctypes.c_void_p)]
+
+
+def adamw_state(w, bits=32):
+    """The state of a tensor before its first step: (m, v, m_scale, v_scale).  32 bits: fp32 moments and no scales; 8:
+    float8_e4m3fn codes of the first moment and of the root of the second, over a scale for every STATE_BLOCK elements:
+    moment = code * scale, second moment = (code * scale)^2."""
+    if bits == 32:
+        return torch.zeros_like(w), torch.zeros_like(w), None, None
+    if bits != 8:
+        raise ValueError("states have 32 or 8 bits")
+    n = -(-w.numel() // STATE_BLOCK)
+    # (zeros as bytes: not every fill kernel knows the 8-bit type)
+    m, v = (torch.zeros(w.shape, dtype=torch.uint8, device=w.device).view(torch.float8_e4m3fn) for _ in range(2))
+    return (m, v) + tuple(torch.zeros(n, dtype=torch.float32, device=w.device) for _ in range(2))
+
+
+def adamw_step(w, m, v, g, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, m_scale=None,
+               v_scale=None, seed=0):
+    """One AdamW step (decoupled weight decay) over lists of tensors, in place: w fp32, g all fp32 or all bf16, m and v as
+    adamw_state gives them (with lists of scales: 8-bit states, rounded by chance from `seed`, `step` and the tensor's
+    place in the list).  `step` counts from 1; `step` (int32) and `lr` (fp32) may be one-element GPU tensors, read when the
+    kernel runs, for captured steps.  `weight_decay`: a number or one for each tensor.  Returns (w, m, v)."""
+    out = (_native or _load_native()).adamw_step(w, m, v, g, step, lr, beta1, beta2, eps, weight_decay, m_scale, v_scale,
+                                                 seed)
+    if out is not NotImplemented:
+        return out
+    n = len(w)
+    if n == 0:
+        raise ValueError("w has no tensors")
+    eight = m_scale is not None or v_scale is not None
+    decays = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(d) for d in weight_decay]
+    lists = [("m", m), ("v", v), ("g", g), ("weight_decay", decays)]
+    if eight:
+        if m_scale is None or v_scale is None:
+            raise ValueError("m_scale and v_scale are given together")
+        lists += [("m_scale", m_scale), ("v_scale", v_scale)]
+    for name, l in lists:
+        if len(l) != n:
+            raise ValueError("%s has %d entries, expected %d" % (name, len(l), n))
+    for i in range(n):
+        for name, t in (("m", m[i]), ("v", v[i]), ("g", g[i])):
+            _numel(t, w[i].numel(), "%s[%d]" % (name, i))
+        if eight:
+            for name, t in (("m_scale", m_scale[i]), ("v_scale", v_scale[i])):
+                _numel(t, -(-w[i].numel() // STATE_BLOCK), "%s[%d]" % (name, i))
+    state = (torch.float8_e4m3fn,) if eight else _F32
+    first = w[0]
+    table = (AdamwTensor * n)()
+    for i in range(n):
+        p = [_beside(t, "%s[%d]" % (name, i), first, types) for name, t, types in (
+            ("w", w[i], _F32), ("m", m[i], state), ("v", v[i], state), ("g", g[i], (g[0].dtype,)))]
+        if eight:
+            p += [_beside(t[i], "%s[%d]" % (name, i), first, _F32) for name, t in (("m_scale", m_scale), ("v_scale", v_scale))]
+        else:
+            p += [None, None]
+        table[i] = AdamwTensor(*p, w[i].numel(), decays[i])
+    h = AdamwHyper(0.0, float(beta1), float(beta2), float(eps), 0, int(seed) & 0xFFFFFFFF, None, None)
+    if isinstance(step, torch.Tensor):
+        _numel(step, 1, "step")
+        h.step_dev = _beside(step, "step", first, (torch.int32,))
+    else:
+        h.step = int(step)
+    if isinstance(lr, torch.Tensor):
+        _numel(lr, 1, "lr")
+        h.lr_dev = _beside(lr, "lr", first, _F32)
+    else:
+        h.lr = float(lr)
+    _call_on(first, "tbn_adamw_step", table, n, STATE_E4M3 if eight else STATE_F32, _dtype_code(g[0].dtype),
+             ctypes.byref(h))
+    return w, m, v
+
+
+class AdapterDesc(ctypes.Structure):
+    """A batch of `rows` rows beside a projection of c inputs and k outputs, a bank of `adapters` of this rank."""
+
+    _fields_ = [("rows", ctypes.c_int64)] + [(f, ctypes.c_int32) for f in ("c", "k", "rank", "adapters")]
+
+
+def adapter_workspace_size(op: int, desc: AdapterDesc) -> int:
+    b = ctypes.c_size_t()
+    _call("tbn_adapter_workspace_size", op, ctypes.byref(desc), ctypes.byref(b))
+    return b.value
+
+
+def _adapter_desc(x, index, a, b, scale):
+    if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2]:
+        raise ValueError("a is [adapters][rank][c] and b [adapters][k][rank]: got %s and %s" % (tuple(a.shape),
+                                                                                               tuple(b.shape)))
+    rows, c = _rows_of(x)
+    if c != a.shape[2]:
+        raise ValueError("x has rows of %d values, expected %d" % (c, a.shape[2]))
+    _numel(index, rows, "index")
+    _at_least(scale, a.shape[0], "scale")
+    return AdapterDesc(rows, c, b.shape[1], a.shape[1], a.shape[0])
+
+
+def adapter_fwd(x, index, a, b, scale=None, residual=None, out_dtype=None, y=None, want_t=True, ws=None):
+    """Low-rank adapters of many requests: row i of x [..][C] has the adapter index[i] (int32) of the bank a [S][R][C],
+    b [S][K][R] (both bf16 or both fp32), none where it is outside [0, S):  t = A x, y = residual + scale[index] B t.
+    `scale` fp32 [S]; y [..][K] of `out_dtype` (default: the residual's type, or bf16); `y` may be the residual.  Returns
+    (y, t), t fp32 [rows][R] for adapter_bwd (None without `want_t`).  Passed to conv2d_fwd as `residual`, y adds the
+    adapters to the two-bit projection before its ReLU."""
+    out = (_native or _load_native()).adapter_fwd(x, index, a, b, scale, residual, out_dtype, y, want_t, ws)
+    if out is not NotImplemented:
+        return out
+    d = _adapter_desc(x, index, a, b, scale)
+    if y is not None:
+        _numel(y, d.rows * d.k, "y")
+        out_dtype = y.dtype
+    elif out_dtype is None:
+        out_dtype = torch.bfloat16 if residual is None else residual.dtype
+    if residual is not None:
+        _numel(residual, d.rows * d.k, "residual")
+        if residual.dtype != out_dtype:
+            raise TypeError("residual must have y's dtype")
+    yt = _dtype_code(out_dtype)
+    px, pi = _dev(x, "x", _FLOATS), _beside(index, "index", x, (torch.int32,))
+    pa, pb, ps = _beside(a, "a", x, _FLOATS), _beside(b, "b", x, (a.dtype,)), _beside(scale, "scale", x, _F32)
+    pr = _beside(residual, "residual", x, _FLOATS)
+    if y is None:
+        y = torch.empty(tuple(x.shape[:-1]) + (d.k,), dtype=out_dtype, device=x.device)
+    py = _beside(y, "y", x, _FLOATS)
+    t = torch.empty((d.rows, d.rank), dtype=torch.float32, device=x.device) if want_t else None
+    if ws is None:
+        ws = torch.empty(adapter_workspace_size(OP_FWD, d), dtype=torch.uint8, device=x.device)
+    _call_on(x, "tbn_adapter_fwd", ctypes.byref(d), px, _dtype_code(x.dtype), pi, pa, pb, _dtype_code(a.dtype), ps, pr,
+             py, yt, _beside(t, "t", x, _F32), _beside(ws, "ws", x, None), ws.numel() * ws.element_size())
+    return y, t
+
+
+def adapter_bwd(x, dy, index, a, b, t, scale=None, residual=None, out_dtype=None, need_dx=True, da=None, db=None, ws=None):
+    """Backward of adapter_fwd, for its inputs, its t and the gradient dy [..][K]: returns (dx, da, db) with
+    dx = residual + scale (dy B) A of `out_dtype` (default: the residual's type, or bf16; None without `need_dx`; the
+    residual is the projection's own gradient, as conv2d_bwd_data gives it) and da, db fp32, shaped as a and b
+    (caller-provided ones are overwritten)."""
+    out = (_native or _load_native()).adapter_bwd(x, dy, index, a, b, t, scale, residual, out_dtype, need_dx, da, db, ws)
+    if out is not NotImplemented:
+        return out
+    d = _adapter_desc(x, index, a, b, scale)
+    _numel(dy, d.rows * d.k, "dy")
+    _numel(t, d.rows * d.rank, "t")
+    for g, like, name in ((da, a, "da"), (db, b, "db")):
+        if g is not None:
+            _numel(g, like.numel(), name)
+    if out_dtype is None:
+        out_dtype = torch.bfloat16 if residual is None else residual.dtype
+    if residual is not None:
+        _numel(residual, x.numel(), "residual")
+        if residual.dtype != out_dtype:
+            raise TypeError("residual must have dx's dtype")
+    xt = _dtype_code(out_dtype)
+    px, pd, pi = _dev(x, "x", _FLOATS), _beside(dy, "dy", x, _FLOATS), _beside(index, "index", x, (torch.int32,))
+    pa, pb, ps = _beside(a, "a", x, _FLOATS), _beside(b, "b", x, (a.dtype,)), _beside(scale, "scale", x, _F32)
+    pt, pr = _beside(t, "t", x, _F32), _beside(residual, "residual", x, _FLOATS)
+    dx = torch.empty(x.shape, dtype=out_dtype, device=x.device) if need_dx else None
+    if da is None:
+        da = torch.empty(a.shape, dtype=torch.float32, device=x.device)
+    if db is None:
+        db = torch.empty(b.shape, dtype=torch.float32, device=x.device)
+    if ws is None:
+        ws = torch.empty(adapter_workspace_size(OP_BWD_DATA, d), dtype=torch.uint8, device=x.device)
+    _call_on(x, "tbn_adapter_bwd", ctypes.byref(d), px, _dtype_code(x.dtype), pd, _dtype_code(dy.dtype), pi, pa, pb,
+             _dtype_code(a.dtype), ps, pt, pr, _beside(dx, "dx", x, _FLOATS), xt, _beside(da, "da", x, _F32),
+             _beside(db, "db", x, _F32), _beside(ws, "ws", x, None), ws.numel() * ws.element_size())
+    return dx, da, db

@@ -352,4 +352,77 @@ hipError_t launch_softmax_xent(const float* z, const int32_t* labels, int32_t N,
 hipError_t launch_sgd(float* w, float* v, const float* g, int64_t count, float lr, float mu,
                       float wd, hipStream_t stream);
 
+// AdamW: the tensors of one launch and the step's factors (c1, c2 = 1 - beta^step; unused with step_dev).
+struct AdamwTensor {
+    float* w;
+    void* m;
+    void* v;
+    const void* g;
+    float* m_scale;
+    float* v_scale;
+    int64_t count;
+    float weight_decay;
+    int32_t first_block;
+};
+constexpr int kAdamwTensors = 56;  // 64 bytes each: below the 4 KiB of kernel arguments
+struct AdamwBatch {
+    AdamwTensor t[kAdamwTensors];
+    int32_t n, first;  // tensors, place of the first one in the caller's list
+    uint32_t step, seed;
+    const int32_t* step_dev;
+    const float* lr_dev;
+    double lr, beta1, beta2, eps, c1, c2;
+};
+int64_t adamw_chunk();  // elements a block takes
+hipError_t launch_adamw(const AdamwBatch& b, int64_t blocks, int g_bf16, int eight, hipStream_t stream);
+
+// Layer normalisation; partial: [2][layernorm_bwd_blocks][C] fp32.
+struct LnArgs {
+    const void* x;
+    const void* dy;
+    void* y;
+    void* dx;
+    const float* gamma;
+    const float* beta;
+    float* mean;     // forward: outputs; backward: inputs
+    float* inv_std;
+    float* dgamma;
+    float* dbeta;
+    float* partial;
+    int64_t rows;
+    int32_t C;
+    float eps;
+    int32_t x_f32, y_f32;
+};
+int64_t layernorm_bwd_blocks(int64_t rows, int32_t C);
+hipError_t launch_layernorm_fwd(const LnArgs& a, hipStream_t stream);
+hipError_t launch_layernorm_bwd(const LnArgs& a, hipStream_t stream);
+
+// Low-rank adapters: operands of the three kernels.
+struct AdapterArgs {
+    const void* x;         // shrink: rows of C values; outer: the same
+    const void* w;         // shrink, expand: the adapters
+    const int32_t* index;  // [rows]
+    const float* scale;    // [S] or null
+    const void* residual;  // expand: [rows][C] or null
+    void* y;               // expand: [rows][C]
+    float* t;              // expand: the summed partials are written here, or null
+    float* part;           // shrink: out [splits][rows][R]; expand, outer: in
+    float* out;            // outer
+    int64_t rows, per_split;
+    int32_t C, R, S, splits;
+    int32_t x_f32, w_f32, y_f32;
+};
+constexpr int64_t kAdapterFewRows = 64;  // up to here each row may well have an adapter of its own
+struct AdapterPlan {
+    int32_t row_tiles, slots, splits, per_split;
+};
+AdapterPlan plan_adapter_shrink(int64_t rows, int32_t C, int32_t R, int32_t S);
+int32_t adapter_outer_splits(int64_t rows, int32_t C, int32_t S, int64_t* per_split);
+hipError_t launch_adapter_shrink(const AdapterArgs& a, const AdapterPlan& p, int across, hipStream_t s);
+hipError_t launch_adapter_finish(const float* part, int64_t count, int32_t splits, float* t, hipStream_t s);
+hipError_t launch_adapter_expand(const AdapterArgs& a, int across, hipStream_t s);
+hipError_t launch_adapter_outer(const AdapterArgs& a, int32_t splits, int64_t per_split, int cols, float* partial,
+                                float* out, hipStream_t s);
+
 }  // namespace tbn

@@ -1,0 +1,512 @@
+// tbn_layernorm.hip -- layer normalisation of rows of C features, forward and backward.
+//
+//   forward   mu = mean_c x, s = 1 / sqrt(mean_c (x - mu)^2 + eps), y = (x - mu) s gamma + beta
+//   backward  xh = (x - mu) s, h = dy gamma,  dx = s (h - mean_c h - xh mean_c(h xh)),
+//             dgamma = sum_rows dy xh,  dbeta = sum_rows dy
+//
+// Bound by HBM: each tensor is read or written once.  A team of T threads (8 to 64 lanes of a wave, or a
+// whole block) keeps a row in registers, NV pieces of 8 neighbouring values per thread, so that the centred
+// sum of squares is a second pass over registers.  Teams walk the rows with the stride of the grid and keep
+// what belongs to their columns in registers over all of them: gamma and beta, and in the backward pass the
+// sums of dgamma and dbeta, which are added over the teams of a block and written as one row of partial
+// sums per block; a second kernel adds those in a fixed order (no atomics: the same bits every time).
+// Rows longer than the registers hold are read again from the caches (the *_long kernels).
+//
+// All sums and statistics are fp32; a value is rounded once, where a bf16 output is stored.  Pieces are
+// loaded as 16-byte words at the alignment of an element, so odd C needs no other path than its last piece.
+#include "tbn_device.h"
+#include "tbn_kernels.h"
+
+namespace tbn {
+
+namespace {
+
+struct Piece {
+    float v[8];
+};
+
+typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
+typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
+
+// 8 values from p, or the first `left` of them (the rest 0).
+__device__ __forceinline__ Piece load_piece(const uint16_t* p, int64_t left) {
+    Piece r;
+    if (left >= 8) {
+        const u32x4 w = *reinterpret_cast<const u32x4_a2*>(p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            r.v[2 * j] = __uint_as_float(w[j] << 16);
+            r.v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r.v[j] = j < left ? bf16_bits_to_f32(p[j]) : 0.0f;
+    }
+    return r;
+}
+
+__device__ __forceinline__ Piece load_piece(const float* p, int64_t left) {
+    Piece r;
+    if (left >= 8) {
+        const f32x4 a = *reinterpret_cast<const f32x4_a4*>(p), b = *reinterpret_cast<const f32x4_a4*>(p + 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            r.v[j] = a[j];
+            r.v[4 + j] = b[j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r.v[j] = j < left ? p[j] : 0.0f;
+    }
+    return r;
+}
+
+__device__ __forceinline__ void store_piece(uint16_t* p, const Piece& r, int64_t left) {
+    if (left >= 8) {
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(r.v[2 * j], r.v[2 * j + 1]);
+        *reinterpret_cast<u32x4_a2*>(p) = w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < left) p[j] = (uint16_t)f32_to_bf16_bits(r.v[j]);
+    }
+}
+
+__device__ __forceinline__ void store_piece(float* p, const Piece& r, int64_t left) {
+    if (left >= 8) {
+        *reinterpret_cast<f32x4_a4*>(p) = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
+        *reinterpret_cast<f32x4_a4*>(p + 4) = f32x4{r.v[4], r.v[5], r.v[6], r.v[7]};
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < left) p[j] = r.v[j];
+    }
+}
+
+// The sum of v (and of w) over the T threads of a team, in every one of them.  T > 64: the team is the block,
+// and `sh` holds two buffers of 2 T / 64 floats, used in turn (`turn`), so that one barrier a sum is enough.
+template <int T>
+__device__ __forceinline__ void team_sum2(float& v, float& w, float* sh, int& turn) {
+#pragma unroll
+    for (int off = (T < 64 ? T : 64) / 2; off >= 1; off >>= 1) {
+        v += __shfl_xor(v, off, kWave);
+        w += __shfl_xor(w, off, kWave);
+    }
+    if constexpr (T > 64) {
+        constexpr int W = T / 64;
+        float* b = sh + (turn & 1) * 2 * W;
+        ++turn;
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) {
+            b[wave] = v;
+            b[W + wave] = w;
+        }
+        __syncthreads();
+        v = 0.0f;
+        w = 0.0f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            v += b[i];
+            w += b[W + i];
+        }
+    }
+}
+
+template <int T>
+__device__ __forceinline__ float team_sum(float v, float* sh, int& turn) {
+    if constexpr (T <= 64) {
+#pragma unroll
+        for (int off = T / 2; off >= 1; off >>= 1) v += __shfl_xor(v, off, kWave);
+        return v;
+    } else {
+        float unused = 0.0f;
+        team_sum2<T>(v, unused, sh, turn);
+        return v;
+    }
+}
+
+template <typename XT, typename YT, int T, int NV, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void ln_fwd_kernel(const XT* __restrict__ x, int64_t rows, int32_t C,
+                                                       const float* __restrict__ gamma,
+                                                       const float* __restrict__ beta, float eps,
+                                                       YT* __restrict__ y, float* __restrict__ mean,
+                                                       float* __restrict__ inv_std) {
+    __shared__ float sh[T > 64 ? T / 16 : 1];
+    constexpr int RPB = BLOCK / T;
+    const int t = threadIdx.x % T;
+    int turn = 0;
+    Piece g[NV], b[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int e = (i * T + t) * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            g[i].v[j] = 1.0f;
+            b[i].v[j] = 0.0f;
+        }
+        if (e < C && gamma) g[i] = load_piece(gamma + e, C - e);
+        if (e < C && beta) b[i] = load_piece(beta + e, C - e);
+    }
+    const float inv_c = 1.0f / (float)C;
+    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / T; row < rows; row += (int64_t)gridDim.x * RPB) {
+        const XT* xr = x + row * C;
+        Piece v[NV];
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int e = (i * T + t) * 8;
+            v[i] = e < C ? load_piece(xr + e, C - e) : Piece{};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += v[i].v[j];
+        }
+        const float mu = team_sum<T>(sum, sh, turn) * inv_c;
+        float sq = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int e = (i * T + t) * 8;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[i].v[j] -= mu;
+                if (e + j < C) sq += v[i].v[j] * v[i].v[j];
+            }
+        }
+        const float s = 1.0f / sqrtf(team_sum<T>(sq, sh, turn) * inv_c + eps);
+        YT* yr = y + row * C;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int e = (i * T + t) * 8;
+            if (e >= C) break;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i].v[j] = v[i].v[j] * s * g[i].v[j] + b[i].v[j];
+            store_piece(yr + e, v[i], C - e);
+        }
+        if (t == 0) {
+            if (mean) mean[row] = mu;
+            if (inv_std) inv_std[row] = s;
+        }
+    }
+}
+
+// Rows that no team holds in registers: a block per row, three passes over it.
+template <typename XT, typename YT>
+__global__ __launch_bounds__(1024) void ln_fwd_long_kernel(const XT* __restrict__ x, int64_t rows, int32_t C,
+                                                           const float* __restrict__ gamma,
+                                                           const float* __restrict__ beta, float eps,
+                                                           YT* __restrict__ y, float* __restrict__ mean,
+                                                           float* __restrict__ inv_std) {
+    __shared__ float sh[64];
+    int turn = 0;
+    const float inv_c = 1.0f / (float)C;
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const XT* xr = x + row * C;
+        float sum = 0.0f;
+        for (int e = threadIdx.x * 8; e < C; e += 8192) {
+            const Piece v = load_piece(xr + e, C - e);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum += v.v[j];
+        }
+        const float mu = team_sum<1024>(sum, sh, turn) * inv_c;
+        float sq = 0.0f;
+        for (int e = threadIdx.x * 8; e < C; e += 8192) {
+            const Piece v = load_piece(xr + e, C - e);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (e + j < C) sq += (v.v[j] - mu) * (v.v[j] - mu);
+        }
+        const float s = 1.0f / sqrtf(team_sum<1024>(sq, sh, turn) * inv_c + eps);
+        YT* yr = y + row * C;
+        for (int e = threadIdx.x * 8; e < C; e += 8192) {
+            Piece v = load_piece(xr + e, C - e), g, b;
+            if (gamma) g = load_piece(gamma + e, C - e);
+            if (beta) b = load_piece(beta + e, C - e);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v.v[j] = (v.v[j] - mu) * s * (gamma ? g.v[j] : 1.0f) + (beta ? b.v[j] : 0.0f);
+            store_piece(yr + e, v, C - e);
+        }
+        if (threadIdx.x == 0) {
+            if (mean) mean[row] = mu;
+            if (inv_std) inv_std[row] = s;
+        }
+    }
+}
+
+// partial: [2][gridDim.x][C] (dgamma, then dbeta).
+template <typename XT, typename YT, int T, int NV, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void ln_bwd_kernel(const XT* __restrict__ x, const YT* __restrict__ dy,
+                                                       int64_t rows, int32_t C, const float* __restrict__ mean,
+                                                       const float* __restrict__ inv_std,
+                                                       const float* __restrict__ gamma, XT* __restrict__ dx,
+                                                       float* __restrict__ partial) {
+    constexpr int RPB = BLOCK / T;
+    __shared__ float sh[T > 64 ? T / 16 : 1];
+    __shared__ float acc[RPB > 1 ? RPB * T * 8 : 1];
+    const int t = threadIdx.x % T, team = threadIdx.x / T;
+    int turn = 0;
+    Piece g[NV], dg[NV], db[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int e = (i * T + t) * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            g[i].v[j] = 1.0f;
+            dg[i].v[j] = 0.0f;
+            db[i].v[j] = 0.0f;
+        }
+        if (e < C && gamma) g[i] = load_piece(gamma + e, C - e);
+    }
+    const float inv_c = 1.0f / (float)C;
+    for (int64_t row = (int64_t)blockIdx.x * RPB + team; row < rows; row += (int64_t)gridDim.x * RPB) {
+        const XT* xr = x + row * C;
+        const YT* dr = dy + row * C;
+        const float mu = mean[row], s = inv_std[row];
+        Piece xv[NV], dv[NV];
+        float sh1 = 0.0f, sh2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int e = (i * T + t) * 8;
+            xv[i] = e < C ? load_piece(xr + e, C - e) : Piece{};
+            dv[i] = e < C ? load_piece(dr + e, C - e) : Piece{};
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int e = (i * T + t) * 8;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (e + j < C) {  // beyond C nothing is added, whatever mu and s are
+                    const float xh = (xv[i].v[j] - mu) * s, d = dv[i].v[j], h = d * g[i].v[j];
+                    dg[i].v[j] += d * xh;
+                    db[i].v[j] += d;
+                    sh1 += h;
+                    sh2 += h * xh;
+                    xv[i].v[j] = xh;
+                    dv[i].v[j] = h;
+                }
+            }
+        }
+        team_sum2<T>(sh1, sh2, sh, turn);
+        sh1 *= inv_c;
+        sh2 *= inv_c;
+        XT* dxr = dx + row * C;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int e = (i * T + t) * 8;
+            if (e >= C) break;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) dv[i].v[j] = s * (dv[i].v[j] - sh1 - xv[i].v[j] * sh2);
+            store_piece(dxr + e, dv[i], C - e);
+        }
+    }
+    float* pg = partial + (int64_t)blockIdx.x * C;
+    float* pb = partial + (int64_t)(gridDim.x + blockIdx.x) * C;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int e = (i * T + t) * 8;
+        if constexpr (RPB == 1) {
+            if (e < C) {
+                store_piece(pg + e, dg[i], C - e);
+                store_piece(pb + e, db[i], C - e);
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {  // teams added in order
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[(team * 8 + j) * T + t] = q ? db[i].v[j] : dg[i].v[j];
+                __syncthreads();
+                for (int o = threadIdx.x; o < 8 * T; o += BLOCK) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int m = 0; m < RPB; ++m) sum += acc[m * 8 * T + o];
+                    const int c = (i * T + o % T) * 8 + o / T;
+                    if (c < C) (q ? pb : pg)[c] = sum;
+                }
+            }
+        }
+    }
+}
+
+// Rows that no team holds in registers: a block per row, two passes over it; the sums of dgamma and dbeta live
+// in the block's own row of `partial` (read and written by the thread that owns the columns).
+template <typename XT, typename YT>
+__global__ __launch_bounds__(1024) void ln_bwd_long_kernel(const XT* __restrict__ x, const YT* __restrict__ dy,
+                                                           int64_t rows, int32_t C, const float* __restrict__ mean,
+                                                           const float* __restrict__ inv_std,
+                                                           const float* __restrict__ gamma, XT* __restrict__ dx,
+                                                           float* __restrict__ partial) {
+    __shared__ float sh[64];
+    int turn = 0;
+    const float inv_c = 1.0f / (float)C;
+    float* pg = partial + (int64_t)blockIdx.x * C;
+    float* pb = partial + (int64_t)(gridDim.x + blockIdx.x) * C;
+    bool first = true;
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const XT* xr = x + row * C;
+        const YT* dr = dy + row * C;
+        const float mu = mean[row], s = inv_std[row];
+        float sh1 = 0.0f, sh2 = 0.0f;
+        for (int e = threadIdx.x * 8; e < C; e += 8192) {
+            const Piece xv = load_piece(xr + e, C - e), dv = load_piece(dr + e, C - e);
+            Piece g, dg = Piece{}, db = Piece{};
+            if (gamma) g = load_piece(gamma + e, C - e);
+            if (!first) {
+                dg = load_piece(pg + e, C - e);
+                db = load_piece(pb + e, C - e);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (e + j < C) {
+                    const float xh = (xv.v[j] - mu) * s, d = dv.v[j], h = gamma ? d * g.v[j] : d;
+                    dg.v[j] += d * xh;
+                    db.v[j] += d;
+                    sh1 += h;
+                    sh2 += h * xh;
+                }
+            }
+            store_piece(pg + e, dg, C - e);
+            store_piece(pb + e, db, C - e);
+        }
+        first = false;
+        team_sum2<1024>(sh1, sh2, sh, turn);
+        sh1 *= inv_c;
+        sh2 *= inv_c;
+        XT* dxr = dx + row * C;
+        for (int e = threadIdx.x * 8; e < C; e += 8192) {
+            Piece xv = load_piece(xr + e, C - e), dv = load_piece(dr + e, C - e), g;
+            if (gamma) g = load_piece(gamma + e, C - e);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                xv.v[j] = s * ((gamma ? dv.v[j] * g.v[j] : dv.v[j]) - sh1 - (xv.v[j] - mu) * s * sh2);
+            store_piece(dxr + e, xv, C - e);
+        }
+    }
+}
+
+// dgamma, dbeta = the sums of the blocks' partial rows: 32 columns a block, whose 32 groups of threads take every
+// 32nd row and are added in order.
+__global__ __launch_bounds__(1024) void ln_reduce_kernel(const float* __restrict__ partial, int32_t blocks, int32_t C,
+                                                         float* __restrict__ dgamma, float* __restrict__ dbeta) {
+    __shared__ float sh[32][33];
+    const int col = threadIdx.x & 31, grp = threadIdx.x >> 5;
+    const int c = blockIdx.x * 32 + col;
+    const float* p = partial + (int64_t)blockIdx.y * blocks * C;
+    float s = 0.0f;
+    if (c < C)
+        for (int b = grp; b < blocks; b += 32) s += p[(int64_t)b * C + c];
+    sh[grp][col] = s;
+    __syncthreads();
+    if (grp == 0 && c < C) {
+        float t = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) t += sh[i][col];
+        (blockIdx.y ? dbeta : dgamma)[c] = t;
+    }
+}
+
+// The team that holds rows of C values: the smallest of these whose 8 T NV values suffice (an index of the
+// switches below; -1: the long kernels).
+constexpr int kTeams[][3] = {{8, 1, 256},  {16, 1, 256}, {32, 1, 256}, {64, 1, 256},  {64, 2, 256},
+                             {64, 4, 256}, {256, 2, 256}, {256, 4, 256}, {512, 4, 512}, {1024, 4, 1024}};
+constexpr int kNumTeams = sizeof(kTeams) / sizeof(kTeams[0]);
+
+int team_of(int32_t C, int most) {
+    for (int i = 0; i < most; ++i)
+        if (C <= 8 * kTeams[i][0] * kTeams[i][1]) return i;
+    return -1;
+}
+
+constexpr int kBwdTeams = kNumTeams - 1;  // the backward pass holds twice as much per column
+
+template <typename XT, typename YT>
+void fwd(const LnArgs& a, hipStream_t stream) {
+    const int team = team_of(a.C, kNumTeams);
+    const XT* x = reinterpret_cast<const XT*>(a.x);
+    YT* y = reinterpret_cast<YT*>(a.y);
+    const int rpb = team < 0 ? 1 : kTeams[team][2] / kTeams[team][0];
+    int64_t blocks = (a.rows + rpb - 1) / rpb;
+    const int64_t most = team < 0 ? 512 : 256 * 2048 / kTeams[team][2];
+    if (blocks > most) blocks = most;
+#define TBN_LN(i, T, NV, B)                                                                                            \
+    case i:                                                                                                            \
+        hipLaunchKernelGGL((ln_fwd_kernel<XT, YT, T, NV, B>), dim3((unsigned)blocks), dim3(B), 0, stream, x, a.rows, a.C, \
+                           a.gamma, a.beta, a.eps, y, a.mean, a.inv_std);                                              \
+        break
+    switch (team) {
+        TBN_LN(0, 8, 1, 256);
+        TBN_LN(1, 16, 1, 256);
+        TBN_LN(2, 32, 1, 256);
+        TBN_LN(3, 64, 1, 256);
+        TBN_LN(4, 64, 2, 256);
+        TBN_LN(5, 64, 4, 256);
+        TBN_LN(6, 256, 2, 256);
+        TBN_LN(7, 256, 4, 256);
+        TBN_LN(8, 512, 4, 512);
+        TBN_LN(9, 1024, 4, 1024);
+        default:
+            hipLaunchKernelGGL((ln_fwd_long_kernel<XT, YT>), dim3((unsigned)blocks), dim3(1024), 0, stream, x, a.rows, a.C,
+                               a.gamma, a.beta, a.eps, y, a.mean, a.inv_std);
+    }
+#undef TBN_LN
+}
+
+template <typename XT, typename YT>
+void bwd(const LnArgs& a, int64_t blocks, hipStream_t stream) {
+    const XT* x = reinterpret_cast<const XT*>(a.x);
+    const YT* dy = reinterpret_cast<const YT*>(a.dy);
+    XT* dx = reinterpret_cast<XT*>(a.dx);
+#define TBN_LN(i, T, NV, B)                                                                                            \
+    case i:                                                                                                            \
+        hipLaunchKernelGGL((ln_bwd_kernel<XT, YT, T, NV, B>), dim3((unsigned)blocks), dim3(B), 0, stream, x, dy, a.rows, \
+                           a.C, a.mean, a.inv_std, a.gamma, dx, a.partial);                                            \
+        break
+    switch (team_of(a.C, kBwdTeams)) {
+        TBN_LN(0, 8, 1, 256);
+        TBN_LN(1, 16, 1, 256);
+        TBN_LN(2, 32, 1, 256);
+        TBN_LN(3, 64, 1, 256);
+        TBN_LN(4, 64, 2, 256);
+        TBN_LN(5, 64, 4, 256);
+        TBN_LN(6, 256, 2, 256);
+        TBN_LN(7, 256, 4, 256);
+        TBN_LN(8, 512, 4, 512);
+        default:
+            hipLaunchKernelGGL((ln_bwd_long_kernel<XT, YT>), dim3((unsigned)blocks), dim3(1024), 0, stream, x, dy, a.rows,
+                               a.C, a.mean, a.inv_std, a.gamma, dx, a.partial);
+    }
+#undef TBN_LN
+}
+
+}  // namespace
+
+int64_t layernorm_bwd_blocks(int64_t rows, int32_t C) {
+    const int team = team_of(C, kBwdTeams);
+    const int rpb = team < 0 ? 1 : kTeams[team][2] / kTeams[team][0];
+    const int64_t blocks = (rows + rpb - 1) / rpb;
+    return blocks < 512 ? blocks : 512;
+}
+
+hipError_t launch_layernorm_fwd(const LnArgs& a, hipStream_t stream) {
+    if (a.x_f32)
+        a.y_f32 ? fwd<float, float>(a, stream) : fwd<float, uint16_t>(a, stream);
+    else
+        a.y_f32 ? fwd<uint16_t, float>(a, stream) : fwd<uint16_t, uint16_t>(a, stream);
+    return hipGetLastError();
+}
+
+hipError_t launch_layernorm_bwd(const LnArgs& a, hipStream_t stream) {
+    const int64_t blocks = layernorm_bwd_blocks(a.rows, a.C);
+    if (a.x_f32)
+        a.y_f32 ? bwd<float, float>(a, blocks, stream) : bwd<float, uint16_t>(a, blocks, stream);
+    else
+        a.y_f32 ? bwd<uint16_t, float>(a, blocks, stream) : bwd<uint16_t, uint16_t>(a, blocks, stream);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(ln_reduce_kernel, dim3((unsigned)((a.C + 31) / 32), 2), dim3(1024), 0, stream, a.partial,
+                       (int32_t)blocks, a.C, a.dgamma, a.dbeta);
+    return hipGetLastError();
+}
+
+}  // namespace tbn

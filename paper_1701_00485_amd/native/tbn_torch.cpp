@@ -18,7 +18,10 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
+
+#include <vector>
 
 #include "tbn.h"
 
@@ -667,6 +670,309 @@ PyObject* maxpool2d_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- beside frozen two-bit filters -------------------------------------------------------
+// These calls run on the device of their first tensor, on its current stream; the others lie there too.
+struct OnDevice {
+    c10::DeviceGuard guard;
+    hipStream_t stream;
+    explicit OnDevice(const at::Tensor& x)
+        : guard(x.device()), stream(c10::hip::getCurrentHIPStream(x.device().index()).stream()) {}
+};
+
+// An optional operand: null pointer where it is None; false where it is no ordinary one.
+struct Opt {
+    const at::Tensor* t = nullptr;
+    bool take(PyObject* o, const at::Tensor& like, at::ScalarType type, int64_t need) {
+        if (o == Py_None) return true;
+        t = dense(o, type, need);
+        return t && t->device() == like.device();
+    }
+    template <typename T = void>
+    T* ptr() const {
+        return t ? reinterpret_cast<T*>(t->data_ptr()) : nullptr;
+    }
+};
+
+const at::Tensor* beside(PyObject* o, const at::Tensor& like) {
+    const at::Tensor* t = dense(o);
+    return t && t->device() == like.device() ? t : nullptr;
+}
+const at::Tensor* beside(PyObject* o, const at::Tensor& like, at::ScalarType type) {
+    const at::Tensor* t = beside(o, like);
+    return t && t->scalar_type() == type ? t : nullptr;
+}
+bool near(const Out& o, const at::Tensor& like) { return !o.given || o.t.device() == like.device(); }
+bool near(const Ws& w, const at::Tensor& like) { return !w.given || w.t.device() == like.device(); }
+
+// (x, gamma, beta, eps, out_dtype, want_stats)
+PyObject* layernorm_fwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    TBN_ARGS(6);
+    const at::Tensor* x = dense(v[0]);
+    tbn_dtype xt;
+    int64_t rows;
+    int32_t c;
+    float eps;
+    bool want;
+    Opt gamma, beta;
+    if (!x || !float_type(*x, &xt) || !rows_of(*x, &rows, &c)) return declined();
+    at::ScalarType yt = x->scalar_type();
+    if (!gamma.take(v[1], *x, at::kFloat, c) || !beta.take(v[2], *x, at::kFloat, c) || !number(v[3], &eps) ||
+        (v[4] != Py_None && !float_type(v[4], &yt)) || !truth(v[5], &want))
+        return declined();
+    OnDevice on(*x);
+    Out y, mean, inv;
+    y.make(x->sizes(), yt, *x);
+    if (want) {
+        mean.make({rows}, at::kFloat, *x);
+        inv.make({rows}, at::kFloat, *x);
+    }
+    void *xp = x->data_ptr(), *yp = y.t.data_ptr();
+    if (!call("tbn_layernorm_fwd", [&] {
+            return tbn_layernorm_fwd(xp, xt, rows, c, gamma.ptr<float>(), beta.ptr<float>(), eps, yp, code(yt),
+                                     want ? f32(mean.t) : nullptr, want ? f32(inv.t) : nullptr, on.stream);
+        }))
+        return nullptr;
+    return pack({y.object(), want ? mean.object() : none(), want ? inv.object() : none()});
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, dy, mean, inv_std, gamma, ws, dgamma, dbeta)
+PyObject* layernorm_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    TBN_ARGS(8);
+    const at::Tensor* x = dense(v[0]);
+    tbn_dtype xt, yt;
+    int64_t rows;
+    int32_t c;
+    if (!x || !float_type(*x, &xt) || !rows_of(*x, &rows, &c)) return declined();
+    const at::Tensor *dy = beside(v[1], *x), *mean = beside(v[2], *x, at::kFloat), *inv = beside(v[3], *x, at::kFloat);
+    Opt gamma;
+    Out dx, dgamma, dbeta;
+    Ws ws;
+    size_t need = 0;
+    if (!dy || !mean || !inv || !float_type(*dy, &yt) || dy->numel() != x->numel() || mean->numel() < rows ||
+        inv->numel() < rows || !gamma.take(v[4], *x, at::kFloat, c) || !ws.take(v[5]) || !near(ws, *x) ||
+        !dgamma.take(v[6], at::kFloat, c) || !dbeta.take(v[7], at::kFloat, c) || !near(dgamma, *x) || !near(dbeta, *x) ||
+        tbn_layernorm_workspace_size(rows, c, &need) != TBN_OK)
+        return declined();
+    OnDevice on(*x);
+    dx.make(x->sizes(), x->scalar_type(), *x);
+    dgamma.make({c}, at::kFloat, *x);
+    dbeta.make({c}, at::kFloat, *x);
+    ws.make(need, *x);
+    void *xp = x->data_ptr(), *dyp = dy->data_ptr(), *dxp = dx.t.data_ptr();
+    if (!call("tbn_layernorm_bwd", [&] {
+            return tbn_layernorm_bwd(xp, xt, dyp, yt, rows, c, f32(*mean), f32(*inv), gamma.ptr<float>(), dxp,
+                                     f32(dgamma.t), f32(dbeta.t), ws.ptr(), ws.bytes(), on.stream);
+        }))
+        return nullptr;
+    return pack({dx.object(), dgamma.object(), dbeta.object()});
+    END_HANDLE_TH_ERRORS
+}
+
+bool real(PyObject* o, double* out) {
+    if (!PyFloat_Check(o) && !PyLong_CheckExact(o)) return false;
+    *out = PyFloat_AsDouble(o);
+    if (*out == -1.0 && PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    return true;
+}
+
+// A number, or one of this type in device memory.
+template <typename T>
+bool number_or_device(PyObject* o, const at::Tensor& like, at::ScalarType type, const T** dev, bool* is_number) {
+    *is_number = !THPVariable_Check(o);
+    if (*is_number) return true;
+    const at::Tensor* t = beside(o, like, type);
+    if (!t || t->numel() != 1) return false;
+    *dev = reinterpret_cast<const T*>(t->data_ptr());
+    return true;
+}
+
+// A list's items, borrowed.
+bool list_of(PyObject* o, Py_ssize_t n, PyObject*** items) {
+    if (!PyList_CheckExact(o) || PyList_GET_SIZE(o) != n) return false;
+    *items = reinterpret_cast<PyListObject*>(o)->ob_item;
+    return true;
+}
+
+// (w, m, v, g, step, lr, beta1, beta2, eps, weight_decay, m_scale, v_scale, seed)
+PyObject* adamw_step(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    TBN_ARGS(13);
+    if (!PyList_CheckExact(v[0]) || PyList_GET_SIZE(v[0]) < 1 || PyList_GET_SIZE(v[0]) > (1 << 20)) return declined();
+    const Py_ssize_t count = PyList_GET_SIZE(v[0]);
+    PyObject **w, **m, **s, **g, **decay = nullptr, **ms = nullptr, **vs = nullptr;
+    double wd = 0.0;
+    tbn_adamw_hyper h = {};
+    int32_t seed;
+    if (!list_of(v[0], count, &w) || !list_of(v[1], count, &m) || !list_of(v[2], count, &s) || !list_of(v[3], count, &g) ||
+        !real(v[6], &h.beta1) || !real(v[7], &h.beta2) || !real(v[8], &h.eps) ||
+        (!real(v[9], &wd) && !list_of(v[9], count, &decay)) || !integer(v[12], &seed))
+        return declined();
+    h.seed = (uint32_t)seed;
+    const bool eight = v[10] != Py_None;
+    if (eight != (v[11] != Py_None) || (eight && (!list_of(v[10], count, &ms) || !list_of(v[11], count, &vs))))
+        return declined();
+    const at::Tensor *first = dense(w[0]), *g0 = dense(g[0]);
+    tbn_dtype gt;
+    bool plain;
+    if (!first || !g0 || !float_type(*g0, &gt)) return declined();
+    if (!number_or_device(v[4], *first, at::kInt, &h.step_dev, &plain) || (plain && !integer(v[4], &h.step)) ||
+        !number_or_device(v[5], *first, at::kFloat, &h.lr_dev, &plain) || (plain && !real(v[5], &h.lr)))
+        return declined();
+    const at::ScalarType state = eight ? at::kFloat8_e4m3fn : at::kFloat;
+    std::vector<tbn_adamw_tensor> table((size_t)count);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        const at::Tensor *wt = beside(w[i], *first, at::kFloat), *mt = beside(m[i], *first, state);
+        const at::Tensor *vt = beside(s[i], *first, state), *gg = beside(g[i], *first, g0->scalar_type());
+        if (!wt || !mt || !vt || !gg) return declined();
+        const int64_t e = wt->numel();
+        if (mt->numel() != e || vt->numel() != e || gg->numel() != e) return declined();
+        tbn_adamw_tensor& t = table[(size_t)i];
+        t.w = f32(*wt);
+        t.m = mt->data_ptr();
+        t.v = vt->data_ptr();
+        t.g = gg->data_ptr();
+        t.count = e;
+        if (eight) {
+            const at::Tensor *a = beside(ms[i], *first, at::kFloat), *b = beside(vs[i], *first, at::kFloat);
+            if (!a || !b || a->numel() != (e + 255) / 256 || b->numel() != (e + 255) / 256) return declined();
+            t.m_scale = f32(*a);
+            t.v_scale = f32(*b);
+        }
+        double d = wd;
+        if (decay && !real(decay[i], &d)) return declined();
+        t.weight_decay = (float)d;
+    }
+    OnDevice on(*first);
+    if (!call("tbn_adamw_step", [&] {
+            return tbn_adamw_step(table.data(), (int32_t)count, eight ? TBN_STATE_E4M3 : TBN_STATE_F32, gt, &h, on.stream);
+        }))
+        return nullptr;
+    for (int i = 0; i < 3; ++i) Py_INCREF(v[i]);
+    return pack({v[0], v[1], v[2]});
+    END_HANDLE_TH_ERRORS
+}
+
+// The operands that both directions have.
+struct Adapters {
+    tbn_adapter_desc d = {};
+    const at::Tensor *x = nullptr, *index = nullptr, *a = nullptr, *b = nullptr;
+    tbn_dtype xt, wt;
+    Opt scale;
+    bool get(PyObject* px, PyObject* pi, PyObject* pa, PyObject* pb, PyObject* ps) {
+        x = dense(px);
+        if (!x || !float_type(*x, &xt) || x->dim() < 1 || x->numel() < 1) return false;
+        index = beside(pi, *x, at::kInt);
+        a = beside(pa, *x);
+        if (!index || !a || !float_type(*a, &wt)) return false;
+        b = beside(pb, *x, a->scalar_type());
+        if (!b || a->dim() != 3 || b->dim() != 3 || a->size(0) != b->size(0) || a->size(1) != b->size(2)) return false;
+        if (x->size(-1) != a->size(2) || a->numel() < 1 || b->numel() < 1) return false;
+        if (a->size(0) > INT32_MAX || a->size(1) > INT32_MAX || a->size(2) > INT32_MAX || b->size(1) > INT32_MAX) return false;
+        d.rows = x->numel() / x->size(-1);
+        d.c = (int32_t)a->size(2);
+        d.k = (int32_t)b->size(1);
+        d.rank = (int32_t)a->size(1);
+        d.adapters = (int32_t)a->size(0);
+        return index->numel() == d.rows && scale.take(ps, *x, at::kFloat, a->size(0));
+    }
+    std::vector<int64_t> y_sizes() const {
+        std::vector<int64_t> s(x->sizes().begin(), x->sizes().end());
+        s.back() = d.k;
+        return s;
+    }
+};
+
+// The type of y (of dx): the given one's, the requested one, the residual's or bf16.
+bool adapter_type(PyObject* requested, const Out* given, const Opt& residual, at::ScalarType* out) {
+    *out = residual.t ? residual.t->scalar_type() : at::kBFloat16;
+    if (given && given->given) *out = given->t.scalar_type();
+    else if (requested != Py_None && !float_type(requested, out)) return false;
+    return (*out == at::kFloat || *out == at::kBFloat16) && (!residual.t || residual.t->scalar_type() == *out);
+}
+
+// A residual of this many values, any type yet.
+bool take_residual(PyObject* o, const at::Tensor& like, int64_t numel, Opt* r) {
+    if (o == Py_None) return true;
+    r->t = beside(o, like);
+    return r->t && r->t->numel() == numel;
+}
+
+// (x, index, a, b, scale, residual, out_dtype, y, want_t, ws)
+PyObject* adapter_fwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    TBN_ARGS(10);
+    Adapters o;
+    Opt residual;
+    Out y, t;
+    Ws ws;
+    at::ScalarType yt;
+    bool want;
+    size_t need = 0;
+    if (!o.get(v[0], v[1], v[2], v[3], v[4]) || !take_residual(v[5], *o.x, o.d.rows * o.d.k, &residual) ||
+        !truth(v[8], &want) || !ws.take(v[9]) || !near(ws, *o.x))
+        return declined();
+    if (v[7] != Py_None) {
+        const at::Tensor* g = beside(v[7], *o.x);
+        if (!g || !y.take(v[7], g->scalar_type(), o.d.rows * o.d.k)) return declined();
+    }
+    if (!adapter_type(v[6], &y, residual, &yt) || tbn_adapter_workspace_size(TBN_OP_FWD, &o.d, &need) != TBN_OK)
+        return declined();
+    OnDevice on(*o.x);
+    y.make(o.y_sizes(), yt, *o.x);
+    if (want) t.make({o.d.rows, o.d.rank}, at::kFloat, *o.x);
+    ws.make(need, *o.x);
+    void *xp = o.x->data_ptr(), *ap = o.a->data_ptr(), *bp = o.b->data_ptr(), *yp = y.t.data_ptr();
+    if (!call("tbn_adapter_fwd", [&] {
+            return tbn_adapter_fwd(&o.d, xp, o.xt, i32(*o.index), ap, bp, o.wt, o.scale.ptr<float>(), residual.ptr(), yp,
+                                   code(yt), want ? f32(t.t) : nullptr, ws.ptr(), ws.bytes(), on.stream);
+        }))
+        return nullptr;
+    return pack({y.object(), want ? t.object() : none()});
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, dy, index, a, b, t, scale, residual, out_dtype, need_dx, da, db, ws)
+PyObject* adapter_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    TBN_ARGS(13);
+    Adapters o;
+    Opt residual;
+    Out dx, da, db;
+    Ws ws;
+    at::ScalarType xt;
+    tbn_dtype dyt;
+    bool need_dx;
+    size_t need = 0;
+    if (!o.get(v[0], v[2], v[3], v[4], v[6])) return declined();
+    const at::Tensor *dy = beside(v[1], *o.x), *t = beside(v[5], *o.x, at::kFloat);
+    if (!dy || !t || !float_type(*dy, &dyt) || dy->numel() != o.d.rows * o.d.k || t->numel() != o.d.rows * o.d.rank ||
+        !take_residual(v[7], *o.x, o.x->numel(), &residual) || !adapter_type(v[8], nullptr, residual, &xt) ||
+        !truth(v[9], &need_dx) || !da.take(v[10], at::kFloat, o.a->numel()) || !db.take(v[11], at::kFloat, o.b->numel()) ||
+        !near(da, *o.x) || !near(db, *o.x) || !ws.take(v[12]) || !near(ws, *o.x) ||
+        tbn_adapter_workspace_size(TBN_OP_BWD_DATA, &o.d, &need) != TBN_OK)
+        return declined();
+    OnDevice on(*o.x);
+    if (need_dx) dx.make(o.x->sizes(), xt, *o.x);
+    da.make(o.a->sizes(), at::kFloat, *o.x);
+    db.make(o.b->sizes(), at::kFloat, *o.x);
+    ws.make(need, *o.x);
+    void *xp = o.x->data_ptr(), *dyp = dy->data_ptr(), *ap = o.a->data_ptr(), *bp = o.b->data_ptr();
+    void* dxp = need_dx ? dx.t.data_ptr() : nullptr;
+    if (!call("tbn_adapter_bwd", [&] {
+            return tbn_adapter_bwd(&o.d, xp, o.xt, dyp, dyt, i32(*o.index), ap, bp, o.wt, o.scale.ptr<float>(), f32(*t),
+                                   residual.ptr(), dxp, code(xt), f32(da.t), f32(db.t), ws.ptr(), ws.bytes(), on.stream);
+        }))
+        return nullptr;
+    return pack({need_dx ? dx.object() : none(), da.object(), db.object()});
+    END_HANDLE_TH_ERRORS
+}
+
 // (ConvDesc, TbnError): the Python types that the calls above know
 PyObject* bind_types(PyObject*, PyObject* const* v, Py_ssize_t n) {
     TBN_ARGS(2);
@@ -683,7 +989,9 @@ PyMethodDef methods[] = {
     TBN_FN(conv2d_bwd_data),  TBN_FN(conv2d_bwd_weight),   TBN_FN(quantize),            TBN_FN(sgd_step),
     TBN_FN(sgd_step_quantize), TBN_FN(quantize_act_i8),    TBN_FN(quantize_act_fp8),    TBN_FN(maxpool2d_fwd),
     TBN_FN(maxpool2d_bwd),    TBN_FN(avgpool_global),      TBN_FN(batchnorm_train_fwd), TBN_FN(batchnorm_train_bwd),
-    TBN_FN(relu_bwd),         TBN_FN(softmax_xent),        TBN_FN(bind_types),          {nullptr, nullptr, 0, nullptr}};
+    TBN_FN(relu_bwd),         TBN_FN(softmax_xent),        TBN_FN(layernorm_fwd),       TBN_FN(layernorm_bwd),
+    TBN_FN(adamw_step),       TBN_FN(adapter_fwd),         TBN_FN(adapter_bwd),         TBN_FN(bind_types),
+    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tbn_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,193 @@
+"""What layer normalisation, AdamW and the adapters refuse, on the CPU: every call here fails its checks before
+anything is launched (through the C ABI on addresses that are never followed, through Python on host tensors)."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_1701_00485_amd as tbn
+
+GOOD, BAD = ctypes.c_void_p(0x100000), ctypes.c_void_p(0x100002)
+NULL, SHAPE, UNSUPPORTED, ALIGN, WORKSPACE = 1, 2, 3, 4, 5
+
+
+def test_layernorm():
+    lib = tbn.load()
+    f = ctypes.c_float(1e-5)
+
+    def fwd(x=GOOD, xt=0, rows=4, c=8, gamma=GOOD, y=GOOD, yt=0, mean=None):
+        return lib.tbn_layernorm_fwd(x, xt, rows, c, gamma, None, f, y, yt, mean, None, None)
+
+    assert fwd(x=None) == NULL and fwd(y=None) == NULL
+    assert fwd(rows=0) == SHAPE and fwd(c=0) == SHAPE and fwd(rows=-1) == SHAPE
+    assert fwd(rows=1 << 40, c=2) == SHAPE
+    assert fwd(xt=2) == UNSUPPORTED and fwd(yt=7) == UNSUPPORTED
+    assert fwd(x=BAD) == ALIGN and fwd(y=BAD) == ALIGN and fwd(gamma=BAD) == ALIGN and fwd(mean=BAD) == ALIGN
+
+    need = tbn.layernorm_workspace_size(1000, 72)
+    assert need > 0 and need % (72 * 8) == 0
+
+    def bwd(x=GOOD, xt=0, dy=GOOD, mean=GOOD, dx=GOOD, dgamma=GOOD, ws=GOOD, bytes=need, rows=1000):
+        return lib.tbn_layernorm_bwd(x, xt, dy, 0, rows, 72, mean, GOOD, None, dx, dgamma, GOOD, ws, bytes, None)
+
+    assert bwd(x=None) == bwd(dy=None) == bwd(mean=None) == bwd(dx=None) == bwd(dgamma=None) == NULL
+    assert bwd(rows=0) == SHAPE and bwd(xt=3) == UNSUPPORTED and bwd(dx=BAD) == ALIGN
+    assert bwd(ws=None) == WORKSPACE and bwd(bytes=need - 1) == WORKSPACE and bwd(ws=ctypes.c_void_p(0x100004)) == ALIGN
+
+
+def _adamw(count=8, n=1, state=0, gt=0, w=0x100000, m=0x200000, v=0x300000, g=0x400000, ms=None, vs=None, decay=0.0, same=False, **h):
+    hyper = tbn.AdamwHyper(1e-3, 0.9, 0.999, 1e-8, 1, 0, None, None)
+    for k, x in h.items():
+        setattr(hyper, k, x)
+    table = (tbn.AdamwTensor * max(n, 1))()
+    for i in range(n):
+        off = 0 if same else i * 0x1000
+        table[i] = tbn.AdamwTensor(w and w + off, m and m + off, v and v + off, g, ms, vs, count, decay)
+    return tbn.load().tbn_adamw_step(table, n, state, gt, ctypes.byref(hyper), None)
+
+
+def test_adamw():
+    assert tbn.load().tbn_adamw_step(None, 1, 0, 0, None, None) == NULL
+    assert _adamw(n=0) == SHAPE and _adamw(count=0) == SHAPE and _adamw(count=1 << 41) == SHAPE
+    assert _adamw(w=None) == _adamw(m=None) == _adamw(v=None) == _adamw(g=None) == NULL
+    assert _adamw(state=1) == NULL and _adamw(state=1, ms=0x500000) == NULL  # no scales
+    assert _adamw(state=2) == UNSUPPORTED and _adamw(gt=2) == UNSUPPORTED
+    assert _adamw(w=0x100002) == ALIGN and _adamw(m=0x200001) == ALIGN and _adamw(g=0x400001) == ALIGN
+    assert _adamw(gt=1, g=0x400002) == ALIGN and _adamw(step_dev=0x600002) == ALIGN
+    for k, bad in (("step", (0, -1)), ("beta1", (1.0, -0.1, float("nan"))), ("beta2", (1.0, 2.0)), ("eps", (-1.0, float("inf"))),
+                   ("lr", (float("nan"), float("inf")))):
+        assert all(_adamw(**{k: b}) == SHAPE for b in bad), k
+    assert _adamw(decay=float("nan")) == SHAPE
+    # a tensor twice, and arrays that reach into each other
+    assert _adamw(n=2, same=True) == SHAPE
+    assert _adamw(n=2, count=0x401) == SHAPE
+    assert _adamw(m=0x100010) == SHAPE
+    assert _adamw(state=1, ms=0x500000, vs=0x500000) == SHAPE
+
+
+def _desc(rows=4, c=8, k=8, rank=2, adapters=3):
+    return tbn.AdapterDesc(rows, c, k, rank, adapters)
+
+
+def test_adapters():
+    lib = tbn.load()
+    b = ctypes.c_size_t()
+    for d in (_desc(rows=0), _desc(c=0), _desc(k=-1), _desc(rank=0), _desc(adapters=0), _desc(rows=(1 << 27) + 1),
+              _desc(c=(1 << 24) + 1), _desc(c=1 << 20, rank=128, adapters=100)):
+        assert lib.tbn_adapter_workspace_size(0, ctypes.byref(d), ctypes.byref(b)) == SHAPE
+    for d in (_desc(rank=129), _desc(adapters=65536)):
+        assert lib.tbn_adapter_workspace_size(0, ctypes.byref(d), ctypes.byref(b)) == UNSUPPORTED
+    d = _desc(rows=1000, c=4096, k=512)
+    assert lib.tbn_adapter_workspace_size(2, ctypes.byref(d), ctypes.byref(b)) == UNSUPPORTED
+    assert lib.tbn_adapter_workspace_size(0, ctypes.byref(d), None) == NULL
+    sizes = [tbn.adapter_workspace_size(op, d) for op in (tbn.OP_FWD, tbn.OP_BWD_DATA)]
+
+    def fwd(desc=d, x=GOOD, xt=0, index=GOOD, a=GOOD, wt=0, res=None, y=GOOD, yt=0, t=None, ws=GOOD, bytes=sizes[0]):
+        return lib.tbn_adapter_fwd(desc and ctypes.byref(desc), x, xt, index, a, GOOD, wt, None, res, y, yt, t, ws, bytes, None)
+
+    assert fwd(desc=None) == fwd(x=None) == fwd(index=None) == fwd(a=None) == fwd(y=None) == NULL
+    assert fwd(desc=_desc(rank=0)) == SHAPE
+    assert fwd(xt=2) == fwd(wt=2) == fwd(yt=2) == UNSUPPORTED
+    assert fwd(x=BAD) == fwd(a=BAD) == fwd(y=BAD) == fwd(res=BAD) == fwd(t=BAD) == fwd(index=BAD) == ALIGN
+    assert fwd(ws=None) == WORKSPACE and fwd(bytes=sizes[0] - 1) == WORKSPACE
+
+    def bwd(x=GOOD, dy=GOOD, t=GOOD, dx=GOOD, dxt=0, da=GOOD, db=GOOD, ws=GOOD, bytes=sizes[1], dyt=0):
+        return lib.tbn_adapter_bwd(ctypes.byref(d), x, 0, dy, dyt, GOOD, GOOD, GOOD, 0, None, t, None, dx, dxt, da, db, ws, bytes, None)
+
+    assert bwd(x=None) == bwd(dy=None) == bwd(t=None) == bwd(dx=None, da=None, db=None) == NULL
+    assert bwd(dxt=2) == bwd(dyt=2) == UNSUPPORTED and bwd(da=BAD) == bwd(dx=BAD) == bwd(t=BAD) == ALIGN
+    assert bwd(ws=None) == WORKSPACE and bwd(bytes=sizes[1] - 1) == WORKSPACE
+
+
+# ---- the Python calls, on host tensors (whose device is refused last) and on the GPU's (the native code declines) ----
+def _calls(dev):
+    bf = torch.bfloat16
+
+    def z(*shape, dtype=torch.float32):
+        return torch.zeros(shape, dtype=dtype, device=dev)
+
+    x, s = z(4, 16, dtype=bf), z(4)
+    i = torch.zeros(4, dtype=torch.int32, device=dev)
+    a, b, t = z(3, 2, 16), z(3, 24, 2), z(4, 2)
+    f8 = z(300, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    w = [z(300)]
+    eight = dict(m=[f8], v=[f8.clone()], m_scale=[z(2)], v_scale=[z(2)])
+
+    def adamw(w=w, m=None, v=None, g=None, step=1, **kw):
+        return lambda: tbn.adamw_step(w, m or [z(300)], v or [z(300)], g or [z(300)], step, **kw)
+
+    return {
+        "gamma has": lambda: tbn.layernorm_fwd(x, z(15)),
+        "beta has": lambda: tbn.layernorm_fwd(x, z(16), z(15)),
+        "x has no values": lambda: tbn.layernorm_fwd(x[:0]),
+        "dy has": lambda: tbn.layernorm_bwd(x, x[:3], s, s),
+        "mean has": lambda: tbn.layernorm_bwd(x, x, s[:3], s),
+        "inv_std has": lambda: tbn.layernorm_bwd(x, x, s, s[:3]),
+        "gamma  has": lambda: tbn.layernorm_bwd(x, x, s, s, z(15)),
+        "dgamma has": lambda: tbn.layernorm_bwd(x, x, s, s, dgamma=z(17)),
+        "dbeta has": lambda: tbn.layernorm_bwd(x, x, s, s, dbeta=z(15)),
+        "w has no tensors": lambda: tbn.adamw_step([], [], [], [], 1),
+        "m has": adamw(m=[z(300)] * 2),
+        r"g\[0\] has": adamw(g=[z(299)]),
+        r"v\[0\] has": adamw(v=[z(301)]),
+        "weight_decay has": adamw(weight_decay=[0.1, 0.2]),
+        "given together": adamw(m=eight["m"], v=eight["v"], m_scale=eight["m_scale"]),
+        r"v_scale\[0\] has": adamw(**dict(eight, v_scale=[z(1)])),
+        "32 or 8 bits": lambda: tbn.adamw_state(w[0], bits=16),
+        "step has": adamw(step=torch.ones(2, dtype=torch.int32, device=dev)) if dev == "cuda" else adamw(g=[z(1)]),
+        "index has": lambda: tbn.adapter_fwd(x, i[:3], a, b),
+        "scale has": lambda: tbn.adapter_fwd(x, i, a, b, scale=z(2)),
+        "residual has": lambda: tbn.adapter_fwd(x, i, a, b, residual=z(4, 23)),
+        "y has": lambda: tbn.adapter_fwd(x, i, a, b, y=z(4, 23)),
+        "x has rows": lambda: tbn.adapter_fwd(x[:, :15], i, a, b),
+        "a is .adapters": lambda: tbn.adapter_fwd(x, i, a, z(3, 24, 3)),
+        "dy  has": lambda: tbn.adapter_bwd(x, z(4, 23, dtype=bf), i, a, b, t),
+        "t has": lambda: tbn.adapter_bwd(x, z(4, 24, dtype=bf), i, a, b, t[:3]),
+        "da has": lambda: tbn.adapter_bwd(x, z(4, 24, dtype=bf), i, a, b, t, da=z(3, 2, 15)),
+        "db has": lambda: tbn.adapter_bwd(x, z(4, 24, dtype=bf), i, a, b, t, db=z(3, 24, 1)),
+    }, {
+        "residual must have": lambda: tbn.adapter_fwd(x, i, a, b, residual=z(4, 24), out_dtype=bf),
+        "residual must  have": lambda: tbn.adapter_bwd(x, z(4, 24, dtype=bf), i, a, b, t, residual=z(4, 16), out_dtype=bf),
+    }
+
+
+def _check(dev):
+    values, types = _calls(dev)
+    for calls, error in ((values, ValueError), (types, TypeError)):
+        for name, f in calls.items():
+            print(name, flush=True)
+            match = " ".join(name.split())
+            with pytest.raises(error, match=match if not (name == "step has" and dev == "cpu") else r"g\[0\] has"):
+                f()
+
+
+def test_python_refusals_of_host_tensors():
+    _check("cpu")
+    for f in (lambda t: tbn.layernorm_fwd(t), lambda t: tbn.adamw_step([t.float()], [t.float()], [t.float()], [t.float()], 1),
+              lambda t: tbn.adapter_fwd(t, torch.zeros(4, dtype=torch.int32), torch.zeros(1, 2, 8), torch.zeros(1, 3, 2))):
+        with pytest.raises(TypeError, match="must be a CUDA"):
+            f(torch.zeros(4, 8, dtype=torch.bfloat16))
+
+
+@pytest.mark.gpu
+def test_python_refusals_of_gpu_tensors():
+    _check("cuda")
+    x = torch.zeros(4, 8, device="cuda")
+    i = torch.zeros(4, dtype=torch.int32, device="cuda")
+    a, b = torch.zeros(2, 2, 8, device="cuda"), torch.zeros(2, 4, 2, device="cuda")
+    for f in (lambda: tbn.layernorm_fwd(x.half()), lambda: tbn.layernorm_fwd(x, torch.ones(8, device="cuda").bfloat16()),
+              lambda: tbn.layernorm_fwd(x, torch.ones(8)), lambda: tbn.adapter_fwd(x, i.long(), a, b),
+              lambda: tbn.adapter_fwd(x, i, a, b.bfloat16()), lambda: tbn.adapter_fwd(x, i, a.half(), b.half()),
+              lambda: tbn.adamw_step([x], [x.clone()], [x.clone()], [x.half()], 1),
+              lambda: tbn.adamw_step([x.bfloat16()], [x.clone()], [x.clone()], [x], 1)):
+        with pytest.raises(TypeError):
+            f()
+    for f in (lambda: tbn.layernorm_fwd(x.t()), lambda: tbn.adapter_fwd(x.t().contiguous().t(), i, a, b)):
+        with pytest.raises(ValueError, match="contiguous"):
+            f()
+    with pytest.raises(tbn.TbnError, match="overlap"):
+        tbn.adamw_step([x, x], [x.clone(), x.clone()], [x.clone(), x.clone()], [x, x], 1)
+    with pytest.raises(tbn.TbnError):
+        tbn.adamw_step([x], [x.clone()], [x.clone()], [x], 0)
+    with pytest.raises(tbn.TbnError, match="workspace too small"):
+        tbn.layernorm_bwd(x, x, i.float(), i.float(), ws=torch.empty(8, device="cuda"))
