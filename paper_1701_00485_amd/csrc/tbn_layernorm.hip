@@ -29,40 +29,85 @@ typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
 typedef u32x4 u32x4_a4 __attribute__((aligned(4)));
 typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
 
-// 8 values from p, or the first `left` of them (the rest 0).
-__device__ __forceinline__ Piece load_piece(const uint16_t* p, int64_t left) {
-    Piece r;
-    if (left >= 8) {
-        const u32x4 w = *reinterpret_cast<const u32x4_a2*>(p);
+// 8 values as they lie in memory: what is in flight.
+template <typename T>
+struct Raw;
+template <>
+struct Raw<uint16_t> {
+    u32x4 w = {0u, 0u, 0u, 0u};
+    // from here on the compiler does not know what was formed from it before
+    __device__ __forceinline__ void forget() { asm volatile("" : "+v"(w)); }
+    __device__ __forceinline__ void load(const uint16_t* p) { w = *reinterpret_cast<const u32x4_a2*>(p); }
+    // the first `left` (1 to 7); the last one again where there are no more, so that the loads go out together
+    __device__ __forceinline__ void load_some(const uint16_t* p, int left) {
+        uint32_t h[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[j] = p[j < left ? j : left - 1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = (2 * j < left ? h[2 * j] : 0u) | (2 * j + 1 < left ? h[2 * j + 1] << 16 : 0u);
+    }
+    __device__ __forceinline__ Piece piece() const {
+        Piece r;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             r.v[2 * j] = __uint_as_float(w[j] << 16);
             r.v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) r.v[j] = j < left ? bf16_bits_to_f32(p[j]) : 0.0f;
+        return r;
     }
-    return r;
-}
-
-__device__ __forceinline__ Piece load_piece(const float* p, int64_t left) {
-    Piece r;
-    if (left >= 8) {
-        const f32x4 a = *reinterpret_cast<const f32x4_a4*>(p), b = *reinterpret_cast<const f32x4_a4*>(p + 4);
+};
+template <>
+struct Raw<float> {
+    f32x4 w[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+    __device__ __forceinline__ void forget() { asm volatile("" : "+v"(w[0]), "+v"(w[1])); }
+    __device__ __forceinline__ void load(const float* p) {
+        w[0] = *reinterpret_cast<const f32x4_a4*>(p);
+        w[1] = *reinterpret_cast<const f32x4_a4*>(p + 4);
+    }
+    __device__ __forceinline__ void load_some(const float* p, int left) {
+        float h[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            r.v[j] = a[j];
-            r.v[4 + j] = b[j];
+        for (int j = 0; j < 8; ++j) h[j] = p[j < left ? j : left - 1];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j >> 2][j & 3] = j < left ? h[j] : 0.0f;
+    }
+    __device__ __forceinline__ Piece piece() const {
+        Piece r;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r.v[j] = w[j >> 2][j & 3];
+        return r;
+    }
+};
+
+// A thread's NV pieces of a row of C values (WHOLE: a multiple of 8), thread t of T; zeros beyond C.  The whole pieces first, without a branch that
+// writes (it would wait for the loads of the others), then the last, shorter one.
+template <bool WHOLE, int T, int NV, typename E>
+__device__ __forceinline__ void load_row(Raw<E> (&r)[NV], const E* row, int t, int C) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int e = (i * T + t) * 8;
+        r[i] = Raw<E>();
+        if (e + 8 <= C) r[i].load(row + e);
+    }
+    if constexpr (!WHOLE) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int e = (i * T + t) * 8;
+            if (e < C && e + 8 > C) r[i].load_some(row + e, C - e);
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) r.v[j] = j < left ? p[j] : 0.0f;
     }
-    return r;
 }
 
-__device__ __forceinline__ void store_piece(uint16_t* p, const Piece& r, int64_t left) {
+// 8 values from p, or the first `left` (>= 1) of them, the rest 0.
+template <typename E>
+__device__ __forceinline__ Piece load_piece(const E* p, int left) {
+    Raw<E> r;
+    if (left >= 8) r.load(p);
+    else r.load_some(p, left);
+    return r.piece();
+}
+
+__device__ __forceinline__ void store_piece(uint16_t* p, const Piece& r, int left) {
     if (left >= 8) {
         u32x4 w;
 #pragma unroll
@@ -75,7 +120,7 @@ __device__ __forceinline__ void store_piece(uint16_t* p, const Piece& r, int64_t
     }
 }
 
-__device__ __forceinline__ void store_piece(float* p, const Piece& r, int64_t left) {
+__device__ __forceinline__ void store_piece(float* p, const Piece& r, int left) {
     if (left >= 8) {
         *reinterpret_cast<f32x4_a4*>(p) = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
         *reinterpret_cast<f32x4_a4*>(p + 4) = f32x4{r.v[4], r.v[5], r.v[6], r.v[7]};
@@ -128,7 +173,7 @@ __device__ __forceinline__ float team_sum(float v, float* sh, int& turn) {
     }
 }
 
-template <typename XT, typename YT, int T, int NV, int BLOCK>
+template <typename XT, typename YT, int T, int NV, int BLOCK, bool WHOLE>
 __global__ __launch_bounds__(BLOCK) void ln_fwd_kernel(const XT* __restrict__ x, int64_t rows, int32_t C,
                                                        const float* __restrict__ gamma,
                                                        const float* __restrict__ beta, float eps,
@@ -138,30 +183,37 @@ __global__ __launch_bounds__(BLOCK) void ln_fwd_kernel(const XT* __restrict__ x,
     constexpr int RPB = BLOCK / T;
     const int t = threadIdx.x % T;
     int turn = 0;
-    Piece g[NV], b[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int e = (i * T + t) * 8;
+    constexpr bool HOLD = NV <= 4;  // gamma and beta in registers; otherwise from the L2 for every row
+    Piece g[HOLD ? NV : 1], b[HOLD ? NV : 1];
+    auto parameters = [&](int e, Piece& gp, Piece& bp) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            g[i].v[j] = 1.0f;
-            b[i].v[j] = 0.0f;
+            gp.v[j] = 1.0f;
+            bp.v[j] = 0.0f;
         }
-        if (e < C && gamma) g[i] = load_piece(gamma + e, C - e);
-        if (e < C && beta) b[i] = load_piece(beta + e, C - e);
+        if (e < C && gamma) gp = load_piece(gamma + e, WHOLE ? 8 : C - e);
+        if (e < C && beta) bp = load_piece(beta + e, WHOLE ? 8 : C - e);
+    };
+    if constexpr (HOLD) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) parameters((i * T + t) * 8, g[i], b[i]);
     }
     const float inv_c = 1.0f / (float)C;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / T; row < rows; row += (int64_t)gridDim.x * RPB) {
-        const XT* xr = x + row * C;
+    const int64_t stride = (int64_t)gridDim.x * RPB;
+    int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / T;
+    Raw<XT> raw[NV];
+    if (row < rows) load_row<WHOLE, T, NV>(raw, x + row * C, t, C);
+    for (; row < rows; row += stride) {
         Piece v[NV];
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int e = (i * T + t) * 8;
-            v[i] = e < C ? load_piece(xr + e, C - e) : Piece{};
+            v[i] = raw[i].piece();
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum += v[i].v[j];
         }
+        if (row + stride < rows) load_row<WHOLE, T, NV>(raw, x + (row + stride) * C, t, C);  // the next row, in flight
+        __builtin_amdgcn_sched_barrier(0);
         const float mu = team_sum<T>(sum, sh, turn) * inv_c;
         float sq = 0.0f;
 #pragma unroll
@@ -169,8 +221,9 @@ __global__ __launch_bounds__(BLOCK) void ln_fwd_kernel(const XT* __restrict__ x,
             const int e = (i * T + t) * 8;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                v[i].v[j] -= mu;
-                if (e + j < C) sq += v[i].v[j] * v[i].v[j];
+                const float d = v[i].v[j] - mu;
+                v[i].v[j] = e + (WHOLE ? 0 : j) < C ? d : 0.0f;
+                sq += v[i].v[j] * v[i].v[j];
             }
         }
         const float s = 1.0f / sqrtf(team_sum<T>(sq, sh, turn) * inv_c + eps);
@@ -179,9 +232,11 @@ __global__ __launch_bounds__(BLOCK) void ln_fwd_kernel(const XT* __restrict__ x,
         for (int i = 0; i < NV; ++i) {
             const int e = (i * T + t) * 8;
             if (e >= C) break;
+            constexpr int kHeld = HOLD ? 1 : 0;
+            if constexpr (!HOLD) parameters(e, g[0], b[0]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i].v[j] = v[i].v[j] * s * g[i].v[j] + b[i].v[j];
-            store_piece(yr + e, v[i], C - e);
+            for (int j = 0; j < 8; ++j) v[i].v[j] = v[i].v[j] * s * g[kHeld * i].v[j] + b[kHeld * i].v[j];
+            store_piece(yr + e, v[i], WHOLE ? 8 : C - e);
         }
         if (t == 0) {
             if (mean) mean[row] = mu;
@@ -235,7 +290,7 @@ __global__ __launch_bounds__(1024) void ln_fwd_long_kernel(const XT* __restrict_
 }
 
 // partial: [2][gridDim.x][C] (dgamma, then dbeta).
-template <typename XT, typename YT, int T, int NV, int BLOCK>
+template <typename XT, typename YT, int T, int NV, int BLOCK, bool WHOLE>
 __global__ __launch_bounds__(BLOCK) void ln_bwd_kernel(const XT* __restrict__ x, const YT* __restrict__ dy,
                                                        int64_t rows, int32_t C, const float* __restrict__ mean,
                                                        const float* __restrict__ inv_std,
@@ -256,48 +311,79 @@ __global__ __launch_bounds__(BLOCK) void ln_bwd_kernel(const XT* __restrict__ x,
             dg[i].v[j] = 0.0f;
             db[i].v[j] = 0.0f;
         }
-        if (e < C && gamma) g[i] = load_piece(gamma + e, C - e);
+        if (e < C && gamma) g[i] = load_piece(gamma + e, WHOLE ? 8 : C - e);
     }
     const float inv_c = 1.0f / (float)C;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + team; row < rows; row += (int64_t)gridDim.x * RPB) {
-        const XT* xr = x + row * C;
-        const YT* dr = dy + row * C;
-        const float mu = mean[row], s = inv_std[row];
-        Piece xv[NV], dv[NV];
+    const int64_t stride = (int64_t)gridDim.x * RPB;
+    int64_t row = (int64_t)blockIdx.x * RPB + team;
+    Raw<XT> xnext[NV];
+    Raw<YT> dnext[NV];
+    float mu_next = 0.0f, s_next = 0.0f;
+    auto load = [&](int64_t r) {
+        load_row<WHOLE, T, NV>(xnext, x + r * C, t, C);
+        load_row<WHOLE, T, NV>(dnext, dy + r * C, t, C);
+        mu_next = mean[r];
+        s_next = inv_std[r];
+    };
+    constexpr bool AHEAD = T < 512;  // the widest team has no registers for the next row
+    if (AHEAD && row < rows) load(row);
+    for (; row < rows; row += stride) {
+        if constexpr (!AHEAD) load(row);
+        const float mu = mu_next, s = s_next;
+        Raw<XT> xr[NV];  // a row stays as it lies in memory; the second pass over it forms xh and h again
+        Raw<YT> dr[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            xr[i] = xnext[i];
+            dr[i] = dnext[i];
+        }
+        if (AHEAD && row + stride < rows) load(row + stride);  // the next row, in flight
+        __builtin_amdgcn_sched_barrier(0);
+        // xh and h of a piece; beyond C the gradient is 0 and xh is made so, whatever mu and s are
+        auto form = [&](int i, Piece& xh, Piece& d, Piece& h) {
+            const int e = (i * T + t) * 8;
+            xh = xr[i].piece();
+            d = dr[i].piece();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float x0 = (xh.v[j] - mu) * s;
+                xh.v[j] = e + (WHOLE ? 0 : j) < C ? x0 : 0.0f;
+                h.v[j] = d.v[j] * g[i].v[j];
+            }
+        };
         float sh1 = 0.0f, sh2 = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int e = (i * T + t) * 8;
-            xv[i] = e < C ? load_piece(xr + e, C - e) : Piece{};
-            dv[i] = e < C ? load_piece(dr + e, C - e) : Piece{};
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int e = (i * T + t) * 8;
+            Piece xh, d, h;
+            form(i, xh, d, h);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                if (e + j < C) {  // beyond C nothing is added, whatever mu and s are
-                    const float xh = (xv[i].v[j] - mu) * s, d = dv[i].v[j], h = d * g[i].v[j];
-                    dg[i].v[j] += d * xh;
-                    db[i].v[j] += d;
-                    sh1 += h;
-                    sh2 += h * xh;
-                    xv[i].v[j] = xh;
-                    dv[i].v[j] = h;
-                }
+                dg[i].v[j] += d.v[j] * xh.v[j];
+                db[i].v[j] += d.v[j];
+                sh1 += h.v[j];
+                sh2 += h.v[j] * xh.v[j];
             }
         }
         team_sum2<T>(sh1, sh2, sh, turn);
         sh1 *= inv_c;
         sh2 *= inv_c;
+        if constexpr (NV >= 4) {  // where registers are short
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                xr[i].forget();
+                dr[i].forget();
+            }
+        }
         XT* dxr = dx + row * C;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int e = (i * T + t) * 8;
             if (e >= C) break;
+            Piece xh, d, h;
+            form(i, xh, d, h);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) dv[i].v[j] = s * (dv[i].v[j] - sh1 - xv[i].v[j] * sh2);
-            store_piece(dxr + e, dv[i], C - e);
+            for (int j = 0; j < 8; ++j) d.v[j] = s * (h.v[j] - sh1 - xh.v[j] * sh2);
+            store_piece(dxr + e, d, WHOLE ? 8 : C - e);
         }
     }
     float* pg = partial + (int64_t)blockIdx.x * C;
@@ -307,8 +393,8 @@ __global__ __launch_bounds__(BLOCK) void ln_bwd_kernel(const XT* __restrict__ x,
         const int e = (i * T + t) * 8;
         if constexpr (RPB == 1) {
             if (e < C) {
-                store_piece(pg + e, dg[i], C - e);
-                store_piece(pb + e, db[i], C - e);
+                store_piece(pg + e, dg[i], WHOLE ? 8 : C - e);
+                store_piece(pb + e, db[i], WHOLE ? 8 : C - e);
             }
         } else {
 #pragma unroll
@@ -409,30 +495,45 @@ __global__ __launch_bounds__(1024) void ln_reduce_kernel(const float* __restrict
 // The team that holds rows of C values: the smallest of these whose 8 T NV values suffice (an index of the
 // switches below; -1: the long kernels).
 constexpr int kTeams[][3] = {{8, 1, 256},  {16, 1, 256}, {32, 1, 256}, {64, 1, 256},  {64, 2, 256},
-                             {64, 4, 256}, {256, 2, 256}, {256, 4, 256}, {512, 4, 512}, {1024, 4, 1024}};
+                             {64, 4, 256}, {256, 2, 256}, {256, 4, 256}, {512, 4, 512}, {512, 8, 512}};
 constexpr int kNumTeams = sizeof(kTeams) / sizeof(kTeams[0]);
 
-int team_of(int32_t C, int most) {
-    for (int i = 0; i < most; ++i)
+int team_of(int32_t C) {
+    for (int i = 0; i < kNumTeams; ++i)
         if (C <= 8 * kTeams[i][0] * kTeams[i][1]) return i;
     return -1;
 }
 
-constexpr int kBwdTeams = kNumTeams - 1;  // the backward pass holds twice as much per column
+// The widest team only where its registers suffice: forward, rows of whole pieces.
+int fwd_team(int32_t C) {
+    const int team = team_of(C);
+    return team == kNumTeams - 1 && C % 8 ? -1 : team;
+}
+int bwd_team(int32_t C) {
+    const int team = team_of(C);
+    return team == kNumTeams - 1 ? -1 : team;
+}
 
 template <typename XT, typename YT>
 void fwd(const LnArgs& a, hipStream_t stream) {
-    const int team = team_of(a.C, kNumTeams);
+    const int team = fwd_team(a.C);
     const XT* x = reinterpret_cast<const XT*>(a.x);
     YT* y = reinterpret_cast<YT*>(a.y);
     const int rpb = team < 0 ? 1 : kTeams[team][2] / kTeams[team][0];
     int64_t blocks = (a.rows + rpb - 1) / rpb;
     const int64_t most = team < 0 ? 512 : 256 * 2048 / kTeams[team][2];
     if (blocks > most) blocks = most;
-#define TBN_LN(i, T, NV, B)                                                                                            \
-    case i:                                                                                                            \
-        hipLaunchKernelGGL((ln_fwd_kernel<XT, YT, T, NV, B>), dim3((unsigned)blocks), dim3(B), 0, stream, x, a.rows, a.C, \
-                           a.gamma, a.beta, a.eps, y, a.mean, a.inv_std);                                              \
+#define TBN_LN_CALL(T, NV, B, WHOLE)                                                                                   \
+    hipLaunchKernelGGL((ln_fwd_kernel<XT, YT, T, NV, B, WHOLE>), dim3((unsigned)blocks), dim3(B), 0, stream, x, a.rows, \
+                       a.C, a.gamma, a.beta, a.eps, y, a.mean, a.inv_std)
+#define TBN_LN_WHOLE(i, T, NV, B)       \
+    case i:                             \
+        TBN_LN_CALL(T, NV, B, true);    \
+        break
+#define TBN_LN(i, T, NV, B)                              \
+    case i:                                              \
+        if (a.C % 8 == 0) TBN_LN_CALL(T, NV, B, true);   \
+        else TBN_LN_CALL(T, NV, B, false);               \
         break
     switch (team) {
         TBN_LN(0, 8, 1, 256);
@@ -444,12 +545,14 @@ void fwd(const LnArgs& a, hipStream_t stream) {
         TBN_LN(6, 256, 2, 256);
         TBN_LN(7, 256, 4, 256);
         TBN_LN(8, 512, 4, 512);
-        TBN_LN(9, 1024, 4, 1024);
+        TBN_LN_WHOLE(9, 512, 8, 512);
         default:
             hipLaunchKernelGGL((ln_fwd_long_kernel<XT, YT>), dim3((unsigned)blocks), dim3(1024), 0, stream, x, a.rows, a.C,
                                a.gamma, a.beta, a.eps, y, a.mean, a.inv_std);
     }
 #undef TBN_LN
+#undef TBN_LN_WHOLE
+#undef TBN_LN_CALL
 }
 
 template <typename XT, typename YT>
@@ -457,12 +560,15 @@ void bwd(const LnArgs& a, int64_t blocks, hipStream_t stream) {
     const XT* x = reinterpret_cast<const XT*>(a.x);
     const YT* dy = reinterpret_cast<const YT*>(a.dy);
     XT* dx = reinterpret_cast<XT*>(a.dx);
-#define TBN_LN(i, T, NV, B)                                                                                            \
-    case i:                                                                                                            \
-        hipLaunchKernelGGL((ln_bwd_kernel<XT, YT, T, NV, B>), dim3((unsigned)blocks), dim3(B), 0, stream, x, dy, a.rows, \
-                           a.C, a.mean, a.inv_std, a.gamma, dx, a.partial);                                            \
+#define TBN_LN_CALL(T, NV, B, WHOLE)                                                                                   \
+    hipLaunchKernelGGL((ln_bwd_kernel<XT, YT, T, NV, B, WHOLE>), dim3((unsigned)blocks), dim3(B), 0, stream, x, dy, a.rows, \
+                       a.C, a.mean, a.inv_std, a.gamma, dx, a.partial)
+#define TBN_LN(i, T, NV, B)                              \
+    case i:                                              \
+        if (a.C % 8 == 0) TBN_LN_CALL(T, NV, B, true);   \
+        else TBN_LN_CALL(T, NV, B, false);               \
         break
-    switch (team_of(a.C, kBwdTeams)) {
+    switch (bwd_team(a.C)) {
         TBN_LN(0, 8, 1, 256);
         TBN_LN(1, 16, 1, 256);
         TBN_LN(2, 32, 1, 256);
@@ -477,12 +583,13 @@ void bwd(const LnArgs& a, int64_t blocks, hipStream_t stream) {
                                a.C, a.mean, a.inv_std, a.gamma, dx, a.partial);
     }
 #undef TBN_LN
+#undef TBN_LN_CALL
 }
 
 }  // namespace
 
 int64_t layernorm_bwd_blocks(int64_t rows, int32_t C) {
-    const int team = team_of(C, kBwdTeams);
+    const int team = bwd_team(C);
     const int rpb = team < 0 ? 1 : kTeams[team][2] / kTeams[team][0];
     const int64_t blocks = (rows + rpb - 1) / rpb;
     return blocks < 512 ? blocks : 512;
