@@ -15,14 +15,14 @@
 // states are rounded, and by chance, up with the probability of the distance: rounded to nearest, a moment that
 // moves by 0.1% a step never leaves its code (the steps of a code are 6 to 12%).  The random bits are a hash of
 // seed, step, tensor and element, the same on every run.  A wave holds the 256 elements of a scale, 4 a lane.
+#include <type_traits>
+
 #include "tbn_device.h"
 #include "tbn_kernels.h"
 
 namespace tbn {
 
 namespace {
-
-constexpr int kChunk = 4096;  // elements a block takes: 4 rounds of 256 threads x 4
 
 typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
 typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
@@ -101,7 +101,13 @@ __device__ __forceinline__ uint32_t encode4(const float (&x)[4], float inv, cons
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], c, true);
 }
 
-// The largest finite magnitude over the wave's 256 values.
+// The largest finite magnitude over the wave's 256 values, by lane permutations within the vector unit: pairs, quads,
+// eights and sixteens by mirrors, then rows of 16 into the next ones; lane 63 has seen all.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float max_with(float t) {
+    const int other = __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, t), __builtin_bit_cast(int, t), CTRL, ROWS, 0xF, false);
+    return fmaxf(t, __builtin_bit_cast(float, other));
+}
 __device__ __forceinline__ float wave_top(const float (&x)[4]) {
     float t = 0.0f;
 #pragma unroll
@@ -109,9 +115,13 @@ __device__ __forceinline__ float wave_top(const float (&x)[4]) {
         const float a = __builtin_fabsf(x[j]);
         t = a < __builtin_inff() ? fmaxf(t, a) : t;
     }
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) t = fmaxf(t, __shfl_xor(t, off, kWave));
-    return t;
+    t = max_with<0xB1, 0xF>(t);   // quad_perm [1, 0, 3, 2]
+    t = max_with<0x4E, 0xF>(t);   // quad_perm [2, 3, 0, 1]
+    t = max_with<0x141, 0xF>(t);  // row_half_mirror
+    t = max_with<0x140, 0xF>(t);  // row_mirror
+    t = max_with<0x142, 0xA>(t);  // row_bcast:15 into rows 1 and 3
+    t = max_with<0x143, 0xC>(t);  // row_bcast:31 into rows 2 and 3
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, t), 63));
 }
 
 template <typename GT, bool EIGHT>
@@ -125,7 +135,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwBatch b) {
     }
     const AdamwTensor& t = b.t[lo];
     const int64_t count = t.count;
-    const int64_t base = (int64_t)((int32_t)blockIdx.x - t.first_block) * kChunk;
+    const int64_t base = (int64_t)((int32_t)blockIdx.x - t.first_block) * ((int64_t)b.rounds * kAdamwRound);
 
     const uint32_t step = b.step_dev ? (uint32_t)*b.step_dev : b.step;
     const double lr = b.lr_dev ? (double)*b.lr_dev : b.lr;
@@ -156,8 +166,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwBatch b) {
         float* const pm = reinterpret_cast<float*>(t.m);
         float* const pv = reinterpret_cast<float*>(t.v);
 #pragma unroll 2
-        for (int k = 0; k < kChunk; k += 1024) {
-            const int64_t i = base + k + threadIdx.x * 4;
+        for (int k = 0; k < b.rounds; ++k) {
+            const int64_t i = base + k * kAdamwRound + threadIdx.x * 4;
             if (i + 4 <= count) {
                 float4 w = load4(pw + i), m = load4(pm + i), v = load4(pv + i);
                 const float4 g = load4(pg + i);
@@ -183,71 +193,109 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwBatch b) {
         uint8_t* const pm = reinterpret_cast<uint8_t*>(t.m);
         uint8_t* const pv = reinterpret_cast<uint8_t*>(t.v);
         const uint32_t key = mix(mix(mix(b.seed) ^ step) ^ (uint32_t)(b.first + lo));
-        for (int k = 0; k < kChunk; k += 1024) {
-            const int64_t i = base + k + threadIdx.x * 4;
-            const int64_t blk = (base + k) / 256 + (threadIdx.x >> 6);  // the scale's index: uniform in the wave
-            if (blk * 256 >= count) break;
-            const float ms = t.m_scale[blk], vs = t.v_scale[blk];
-            const int left = i + 4 <= count ? 4 : (i < count ? (int)(count - i) : 0);
-            float w[4] = {}, g[4] = {}, m[4], v[4], r[4];
-            uint32_t cm = 0, cv = 0;
-            if (left == 4) {
-                const float4 w4 = load4(pw + i), g4 = load4(pg + i);
-                w[0] = w4.x; w[1] = w4.y; w[2] = w4.z; w[3] = w4.w;
-                g[0] = g4.x; g[1] = g4.y; g[2] = g4.z; g[3] = g4.w;
-                cm = *reinterpret_cast<const u32_a1*>(pm + i);
-                cv = *reinterpret_cast<const u32_a1*>(pv + i);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 3; ++j) {
-                    if (j >= left) break;
-                    w[j] = pw[i + j];
-                    g[j] = load1(pg + i + j);
-                    cm |= (uint32_t)pm[i + j] << (8 * j);
-                    cv |= (uint32_t)pv[i + j] << (8 * j);
-                }
-            }
-            const float4 m4 = decode4(cm, ms), r4 = decode4(cv, vs);
+        // a round: the wave's 256 elements of one scale
+        struct Round {
+            float4 w, g;
+            uint32_t m, v;
+            float ms, vs;
+        };
+        const int64_t blk0 = base / 256 + (threadIdx.x >> 6);
+        auto load = [&](int k) {
+            Round r;
+            const int64_t i = base + k * kAdamwRound + threadIdx.x * 4;
+            r.ms = t.m_scale[blk0 + 4 * k];
+            r.vs = t.v_scale[blk0 + 4 * k];
+            r.w = load4(pw + i);
+            r.g = load4(pg + i);
+            r.m = *reinterpret_cast<const u32_a1*>(pm + i);
+            r.v = *reinterpret_cast<const u32_a1*>(pv + i);
+            return r;
+        };
+        // ... with the first `left` of the lane's 4 elements inside the tensor
+        auto step_round = [&](int k, Round& r, int left) {
+            const int64_t i = base + k * kAdamwRound + threadIdx.x * 4;
+            float w[4] = {r.w.x, r.w.y, r.w.z, r.w.w}, g[4] = {r.g.x, r.g.y, r.g.z, r.g.w}, m[4], v[4], root[4];
+            const float4 m4 = decode4(r.m, r.ms), r4 = decode4(r.v, r.vs);
             m[0] = m4.x; m[1] = m4.y; m[2] = m4.z; m[3] = m4.w;
             v[0] = r4.x * r4.x; v[1] = r4.y * r4.y; v[2] = r4.z * r4.z; v[3] = r4.w * r4.w;
             uint32_t rm[4], rv[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                update(w[j], m[j], v[j], r[j], g[j], f);
-                if (j >= left) m[j] = r[j] = 0.0f;
+                update(w[j], m[j], v[j], root[j], g[j], f);
+                if (j >= left) m[j] = root[j] = 0.0f;
                 const uint32_t h = mix((uint32_t)(i + j) ^ key);
                 rm[j] = h & 0xFFFFFu;
                 rv[j] = h >> 12;
             }
-            const float tm = wave_top(m), tv = wave_top(r);
+            const float tm = wave_top(m), tv = wave_top(root);
             // a block below 2^-100 is kept as zeros (1 / top has to be finite)
             const bool zm = tm < 0x1p-100f, zv = tv < 0x1p-100f;
-            cm = encode4(m, zm ? 0.0f : 448.0f * (1.0f / tm), rm);
-            cv = encode4(r, zv ? 0.0f : 448.0f * (1.0f / tv), rv);
+            r.m = encode4(m, zm ? 0.0f : 448.0f * (1.0f / tm), rm);
+            r.v = encode4(root, zv ? 0.0f : 448.0f * (1.0f / tv), rv);
+            r.ms = zm ? 0.0f : tm * (1.0f / 448.0f);
+            r.vs = zv ? 0.0f : tv * (1.0f / 448.0f);
+            r.w = float4{w[0], w[1], w[2], w[3]};
+            if ((threadIdx.x & 63) == 0) {
+                t.m_scale[blk0 + 4 * k] = r.ms;
+                t.v_scale[blk0 + 4 * k] = r.vs;
+            }
+        };
+        auto whole = [&](auto rounds) {
+            constexpr int N = decltype(rounds)::value;
+            Round r[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) r[k] = load(k);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                step_round(k, r[k], 4);
+                const int64_t i = base + k * kAdamwRound + threadIdx.x * 4;
+                *reinterpret_cast<f32x4_a4*>(pw + i) = f32x4{r[k].w.x, r[k].w.y, r[k].w.z, r[k].w.w};
+                *reinterpret_cast<u32_a1*>(pm + i) = r[k].m;
+                *reinterpret_cast<u32_a1*>(pv + i) = r[k].v;
+            }
+        };
+        if (base + (int64_t)b.rounds * kAdamwRound <= count) {
+            if (b.rounds == 4) whole(std::integral_constant<int, 4>());
+            else if (b.rounds == 2) whole(std::integral_constant<int, 2>());
+            else whole(std::integral_constant<int, 1>());
+            return;
+        }
+        for (int k = 0; k < b.rounds; ++k) {  // the tensor's end
+            const int64_t i = base + k * kAdamwRound + threadIdx.x * 4;
+            if ((blk0 + 4 * k) * 256 >= count) break;  // uniform in the wave
+            const int left = i + 4 <= count ? 4 : (i < count ? (int)(count - i) : 0);
+            Round r = {};
             if (left == 4) {
-                *reinterpret_cast<f32x4_a4*>(pw + i) = f32x4{w[0], w[1], w[2], w[3]};
-                *reinterpret_cast<u32_a1*>(pm + i) = cm;
-                *reinterpret_cast<u32_a1*>(pv + i) = cv;
+                r = load(k);
             } else {
+                r.ms = t.m_scale[blk0 + 4 * k];
+                r.vs = t.v_scale[blk0 + 4 * k];
+                float w[3] = {}, g[3] = {};
 #pragma unroll
                 for (int j = 0; j < 3; ++j) {
                     if (j >= left) break;
-                    pw[i + j] = w[j];
-                    pm[i + j] = (uint8_t)(cm >> (8 * j));
-                    pv[i + j] = (uint8_t)(cv >> (8 * j));
+                    w[j] = pw[i + j];
+                    g[j] = load1(pg + i + j);
+                    r.m |= (uint32_t)pm[i + j] << (8 * j);
+                    r.v |= (uint32_t)pv[i + j] << (8 * j);
                 }
+                r.w = float4{w[0], w[1], w[2], 0.0f};
+                r.g = float4{g[0], g[1], g[2], 0.0f};
             }
-            if ((threadIdx.x & 63) == 0) {
-                t.m_scale[blk] = zm ? 0.0f : tm * (1.0f / 448.0f);
-                t.v_scale[blk] = zv ? 0.0f : tv * (1.0f / 448.0f);
+            step_round(k, r, left);
+            const float w[4] = {r.w.x, r.w.y, r.w.z, r.w.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j >= left) break;
+                pw[i + j] = w[j];
+                pm[i + j] = (uint8_t)(r.m >> (8 * j));
+                pv[i + j] = (uint8_t)(r.v >> (8 * j));
             }
         }
     }
 }
 
 }  // namespace
-
-int64_t adamw_chunk() { return kChunk; }
 
 hipError_t launch_adamw(const AdamwBatch& b, int64_t blocks, int g_bf16, int eight, hipStream_t stream) {
     const dim3 grid((unsigned)blocks);

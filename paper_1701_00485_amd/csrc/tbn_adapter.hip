@@ -17,6 +17,8 @@
 // result of its own (nothing of another row or adapter enters it, NaN included); tiles of one request's rows run once.
 // The gradients gather the rows of their adapter into a list first.  An index outside [0, S) is no adapter.
 // Every sum is in a fixed order.
+#include <type_traits>
+
 #include "tbn_device.h"
 #include "tbn_kernels.h"
 
@@ -53,49 +55,73 @@ __device__ __forceinline__ Frag<float> split8(const float (&v)[8]) {
     return f;
 }
 
-// 8 neighbouring values, or the first `left` of them and zeros.
-__device__ __forceinline__ Frag<uint16_t> load_frag(const uint16_t* p, int64_t left) {
-    u32x4 w = {0u, 0u, 0u, 0u};
+// 8 values as they lie in memory: what is in flight while the ones before are multiplied.
+template <typename T>
+struct Raw {
+    u32x4 v;
+};
+template <>
+struct Raw<float> {
+    float v[8];
+};
+__device__ __forceinline__ Frag<uint16_t> frag(const Raw<uint16_t>& r) { return Frag<uint16_t>{as_bf16x8(r.v)}; }
+__device__ __forceinline__ Frag<float> frag(const Raw<float>& r) { return split8(r.v); }
+
+// 8 neighbouring values of a row that has `left` more from p on (or none: left <= 0), zeros behind its end; there the
+// row's last value is read instead, so that all loads are issued at once.
+__device__ __forceinline__ Raw<uint16_t> load_raw(const uint16_t* p, int64_t left) {
+    Raw<uint16_t> r;
     if (left >= 8) {
-        w = *reinterpret_cast<const u32x4_a2*>(p);
+        r.v = *reinterpret_cast<const u32x4_a2*>(p);
     } else {
+        uint32_t h[8] = {};
 #pragma unroll
-        for (int j = 0; j < 7; ++j)
-            if (j < left) w[j / 2] |= (uint32_t)p[j] << (16 * (j & 1));
+        for (int j = 0; j < 8; ++j)
+            if (left > 0) h[j] = p[j < left ? j : left - 1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            r.v[j] = (2 * j < left ? h[2 * j] : 0u) | (2 * j + 1 < left ? h[2 * j + 1] << 16 : 0u);
     }
-    return Frag<uint16_t>{as_bf16x8(w)};
+    return r;
 }
-__device__ __forceinline__ void load_f32(const float* p, int64_t left, float (&v)[8]) {
+__device__ __forceinline__ Raw<float> load_raw(const float* p, int64_t left) {
+    Raw<float> r;
     if (left >= 8) {
         const f32x4 a = *reinterpret_cast<const f32x4_a4*>(p), b = *reinterpret_cast<const f32x4_a4*>(p + 4);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            v[j] = a[j];
-            v[4 + j] = b[j];
+            r.v[j] = a[j];
+            r.v[4 + j] = b[j];
         }
     } else {
+        float h[8] = {};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < left ? p[j] : 0.0f;
+        for (int j = 0; j < 8; ++j)
+            if (left > 0) h[j] = p[j < left ? j : left - 1];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r.v[j] = j < left ? h[j] : 0.0f;
     }
+    return r;
 }
-__device__ __forceinline__ Frag<float> load_frag(const float* p, int64_t left) {
-    float v[8];
-    load_f32(p, left, v);
-    return split8(v);
-}
-// 8 values `stride` apart.
-__device__ __forceinline__ Frag<uint16_t> gather_frag(const uint16_t* p, int64_t stride, int64_t left) {
-    u32x4 w = {0u, 0u, 0u, 0u};
+// 8 values `stride` apart, of `left` >= 1 more, zeros behind them (and all of them zeros without `any`, loaded all the same).
+__device__ __forceinline__ Raw<uint16_t> gather_raw(const uint16_t* p, int64_t stride, int64_t left, bool any = true) {
+    Raw<uint16_t> r;
+    uint32_t h[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j < left) w[j / 2] |= (uint32_t)p[j * stride] << (16 * (j & 1));
-    return Frag<uint16_t>{as_bf16x8(w)};
-}
-__device__ __forceinline__ Frag<float> gather_frag(const float* p, int64_t stride, int64_t left) {
-    float v[8];
+    for (int j = 0; j < 8; ++j) h[j] = p[(j < left ? j : left - 1) * stride];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < left ? p[j * stride] : 0.0f;
-    return split8(v);
+    for (int j = 0; j < 4; ++j)
+        r.v[j] = (any && 2 * j < left ? h[2 * j] : 0u) | (any && 2 * j + 1 < left ? h[2 * j + 1] << 16 : 0u);
+    return r;
+}
+__device__ __forceinline__ Raw<float> gather_raw(const float* p, int64_t stride, int64_t left, bool any = true) {
+    Raw<float> r;
+    float h[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[j] = p[(j < left ? j : left - 1) * stride];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.v[j] = any && j < left ? h[j] : 0.0f;
+    return r;
 }
 
 __device__ __forceinline__ f32x4 product(const Frag<uint16_t>& a, const Frag<uint16_t>& b, f32x4 c) {
@@ -112,28 +138,105 @@ __device__ __forceinline__ f32x4 product(const Frag<float>& a, const Frag<float>
     return mfma16(a.hi, b.hi, mfma16(a.mid, b.hi, mfma16(a.hi, b.mid, c)));
 }
 
+// Nothing moves across: left alone, the compiler turns a loop that multiplies what the round before has loaded back
+// into one that loads and waits.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
 // The adapter of a row, -1 for none.
 __device__ __forceinline__ int adapter_of(const int32_t* index, int64_t row, int32_t S) {
     const int32_t a = index[row];
     return (uint32_t)a < (uint32_t)S ? a : -1;
 }
 
+// ---- the rows of each adapter ------------------------------------------------------------
+// order[]: the rows that have an adapter, by adapter and ascending; span[s] = where adapter s begins and how many rows
+// it has.  One block an adapter: the rows of lower adapters counted, its own listed behind them, 16 rows a thread
+// at a time, each wave behind the rows of the waves before it.
+template <int WV>
+__device__ void order_rows(const int32_t* __restrict__ index, int64_t rows, int32_t S, int32_t aid,
+                           int32_t* __restrict__ order, int2* __restrict__ span, int* sh) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int lower = 0;
+#pragma unroll 8
+    for (int64_t r = threadIdx.x; r < rows; r += 64 * WV) lower += (uint32_t)index[r] < (uint32_t)aid;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) lower += __shfl_xor(lower, off, kWave);
+    if (lane == 0) sh[wave] = lower;
+    __syncthreads();
+    int begin = 0, total = 0;
+#pragma unroll
+    for (int k = 0; k < WV; ++k) begin += sh[k];
+    for (int64_t base = 0; base < rows; base += 1024 * WV) {
+        const int64_t first = base + wave * 1024 + lane;
+        uint32_t found = 0;
+        int count = 0;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int64_t row = first + 64 * k;
+            const bool is = row < rows && index[row < rows ? row : 0] == aid;
+            found |= (uint32_t)is << k;
+            count += __popcll(__ballot(is));
+        }
+        __syncthreads();  // the counts of the round before have been read
+        if (lane == 0) sh[wave] = count;
+        __syncthreads();
+        int at = begin + total;
+#pragma unroll
+        for (int k = 0; k < WV; ++k) {
+            at += k < wave ? sh[k] : 0;
+            total += sh[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const bool is = found >> k & 1;
+            const uint64_t m = __ballot(is);
+            if (is) order[at + __popcll(m & ((1ull << lane) - 1))] = (int32_t)(first + 64 * k);
+            at += __popcll(m);
+        }
+    }
+    if (threadIdx.x == 0) span[aid] = int2{begin, total};
+}
+
+__global__ __launch_bounds__(256) void order_kernel(const AdapterArgs a) {
+    __shared__ int sh[4];
+    order_rows<4>(a.index, a.rows, a.S, (int32_t)blockIdx.x, a.order, a.span, sh);
+}
+
 // ---- shrink ------------------------------------------------------------------------------
 // out[split][row][r] = scale sum over the split's c of x[row][c] W[r][c], W = the row's adapter: [R][C], or with ACROSS
-// [C][R].  A block has a tile of 16 RT rows and one split; its four waves take every fourth 32 values of c and
-// add through LDS.  With gridDim.z > 1 (few rows, each with its own adapter) the tile's adapters are dealt over z.
-template <typename XT, typename WT, bool ACROSS, int RN, int RT>
-__global__ __launch_bounds__(256) void shrink_kernel(const AdapterArgs a) {
-    __shared__ f32x4 red[4][RN * RT * 64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// [C][R].  A block has a tile of 16 RT rows and one split; its WV waves take the 64 values of c (whole 128-byte lines of
+// bf16 rows) in turn, the next ones in flight, and add through LDS.  With gridDim.z > 1 (few rows, each with its own
+// adapter) the tile's adapters are dealt over z.  In the backward pass S more blocks order the rows for the gradients
+// beside it.
+template <bool ACROSS, typename WT>
+__device__ __forceinline__ Raw<WT> across_or_along(const WT* w, int c, int R, int left) {
+    if constexpr (ACROSS) {
+        const int back = left > 0 ? 0 : 1 - left;  // beyond the end: from the last value on
+        return gather_raw(w + (int64_t)(c - back) * R, R, left + back, left > 0);
+    } else {
+        return load_raw(w + c, left);
+    }
+}
+
+template <typename XT, typename WT, bool ACROSS, int RN, int RT, int WV>
+__global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
+    constexpr int STEP = 64 * WV;
+    __shared__ f32x4 red[WV][RN * RT * 64];
+    if (blockIdx.x >= a.row_blocks) {
+        if (blockIdx.y == 0 && blockIdx.z == 0)
+            order_rows<WV>(a.index, a.rows, a.S, (int32_t)(blockIdx.x - a.row_blocks), a.order, a.span,
+                       reinterpret_cast<int*>(red));
+        return;
+    }
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4;
     const XT* x = reinterpret_cast<const XT*>(a.x);
     const WT* w = reinterpret_cast<const WT*>(a.w);
     const int64_t row0 = (int64_t)blockIdx.x * (16 * RT);
     const int rows = a.rows - row0 < 16 * RT ? (int)(a.rows - row0) : 16 * RT;
     const int32_t C = a.C, R = a.R;
-    const int c_lo = blockIdx.y * a.per_split;
-    const int c_hi = C - c_lo < a.per_split ? C : c_lo + a.per_split;
+    const int c_lo = blockIdx.y * (int)a.per_split;
+    const int c_hi = C - c_lo < a.per_split ? C : c_lo + (int)a.per_split;
     float* out = a.part + ((int64_t)blockIdx.y * a.rows + row0) * R;
 
     const int mine = lane < rows ? adapter_of(a.index, row0 + lane, a.S) : -1;
@@ -160,30 +263,57 @@ __global__ __launch_bounds__(256) void shrink_kernel(const AdapterArgs a) {
         for (int n = 0; n < RN; ++n)
 #pragma unroll
             for (int t = 0; t < RT; ++t) acc[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        auto step = [&](int c, int left) {
-            Frag<WT> wf[RN];
-            Frag<XT> xf[RT];
+        Raw<WT> wv[2][RN];
+        Raw<XT> xv[2][RT];
+        auto load = [&](int h, int c, int left) {
 #pragma unroll
-            for (int n = 0; n < RN; ++n)
-                wf[n] = ACROSS ? gather_frag(wr[n] + (int64_t)c * R, R, left) : load_frag(wr[n] + c, left);
+            for (int n = 0; n < RN; ++n) wv[h][n] = across_or_along<ACROSS>(wr[n], c, R, left);
 #pragma unroll
-            for (int t = 0; t < RT; ++t) xf[t] = load_frag(xr[t] + c, left);
-#pragma unroll
-            for (int n = 0; n < RN; ++n)
-#pragma unroll
-                for (int t = 0; t < RT; ++t) acc[n][t] = product(wf[n], xf[t], acc[n][t]);
+            for (int t = 0; t < RT; ++t) xv[h][t] = load_raw(xr[t] + c, left);
         };
-        int c = c_lo + 32 * wave;
-        for (; c + 32 <= c_hi; c += 128) step(c, 8);
-        if (c < c_hi) step(c, C - c - 8 * g);  // the last, shorter 32 values
+        auto multiply = [&](int h) {
+            Frag<WT> wf[RN];
+#pragma unroll
+            for (int n = 0; n < RN; ++n) wf[n] = frag(wv[h][n]);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                const Frag<XT> xf = frag(xv[h][t]);
+#pragma unroll
+                for (int n = 0; n < RN; ++n) acc[n][t] = product(wf[n], xf, acc[n][t]);
+            }
+        };
+        int c = c_lo + 64 * wave;
+        if (c + 64 <= c_hi) {
+            load(0, c, 8);
+            load(1, c + 32, 8);
+            for (; c + STEP + 64 <= c_hi; c += STEP) {
+                multiply(0);
+                load(0, c + STEP, 8);
+                in_order();
+                multiply(1);
+                load(1, c + STEP + 32, 8);
+                in_order();
+            }
+            multiply(0);
+            multiply(1);
+            c += STEP;
+        }
+        if (c < c_hi) {  // the last, shorter 64 values
+            load(0, c, C - c - 8 * g);
+            load(1, c + 32, C - c - 32 - 8 * g);
+            multiply(0);
+            multiply(1);
+        }
 #pragma unroll
         for (int n = 0; n < RN; ++n)
 #pragma unroll
             for (int t = 0; t < RT; ++t) red[wave][(n * RT + t) * 64 + lane] = acc[n][t];
         __syncthreads();
         const float sc = a.scale ? a.scale[aid] : 1.0f;
-        for (int o = threadIdx.x; o < RN * RT * 64; o += 256) {
-            const f32x4 s = (red[0][o] + red[1][o]) + (red[2][o] + red[3][o]);
+        for (int o = threadIdx.x; o < RN * RT * 64; o += 64 * WV) {
+            f32x4 s = red[0][o];
+#pragma unroll
+            for (int k = 1; k < WV; ++k) s += red[k][o];
             const int l = o & 63, n = (o >> 6) / RT, row = 16 * ((o >> 6) % RT) + (l & 15);
             if (!(same >> row & 1)) continue;
 #pragma unroll
@@ -217,273 +347,469 @@ __global__ __launch_bounds__(256) void finish_kernel(const float* __restrict__ p
 // ---- expand ------------------------------------------------------------------------------
 // y[row][k] = residual[row][k] + scale sum_r t[row][r] W[k][r], W = the row's adapter: [K][R], or with ACROSS [R][K];
 // t = the sum of `splits` partial ones.  A wave has 64 columns, whose factors stay in registers from one tile of 16
-// rows to the next while the adapter does.  Rows of the MFMA's result are dealt to columns so that a lane holds 16
-// neighbouring ones of one row: 16-byte residual reads and stores.
+// rows to the next while the adapter does; the next tile's rows are in flight meanwhile.  Rows of the MFMA's result are
+// dealt to columns so that the four lanes of a row read and store 64 neighbouring bytes at a time.
+//
+// The 16 outputs of lane group g: for bf16 columns 32 p + 8 g + 0..7 (p = 0, 1), for fp32 16 q + 4 g + 0..3 (q = 0..3);
+// result q of the MFMAs, row 4 g + j, is the lane's output 4 q + j.
 template <typename T>
-__device__ __forceinline__ void load_out(const T* p, int left, float (&y)[16]);
+struct Outputs;
 template <>
-__device__ __forceinline__ void load_out(const float* p, int left, float (&y)[16]) {
-    if (left >= 16) {
+struct Outputs<uint16_t> {
+    u32x4 v[2];
+    static __device__ __forceinline__ int column(int q, int m) { return 32 * (q >> 1) + 8 * (m >> 2) + 4 * (q & 1) + (m & 3); }
+    // p: the row's column col0 + 8 g, of which `left` = K - col0 - 8 g are inside the row; full: all 64 columns are
+    __device__ __forceinline__ void load(const uint16_t* p, bool full, int left) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const f32x4 v = reinterpret_cast<const f32x4_a4*>(p)[q];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) y[4 * q + j] = v[j];
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) y[j] = j < left ? p[j] : 0.0f;
+        for (int h = 0; h < 2; ++h) v[h] = full ? *reinterpret_cast<const u32x4_a2*>(p + 32 * h) : load_raw(p + 32 * h, left - 32 * h).v;
     }
-}
-template <>
-__device__ __forceinline__ void load_out(const uint16_t* p, int left, float (&y)[16]) {
-    if (left >= 16) {
+    __device__ __forceinline__ float get(int o) const {
+        const uint32_t w = v[o >> 3][(o & 7) >> 1];
+        return __uint_as_float(o & 1 ? w & 0xFFFF0000u : w << 16);
+    }
+    static __device__ __forceinline__ void store(uint16_t* p, bool full, int left, const f32x4 (&y)[4]) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const u32x4 v = reinterpret_cast<const u32x4_a2*>(p)[q];
+        for (int h = 0; h < 2; ++h) {
+            u32x4 w;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                y[8 * q + 2 * j] = __uint_as_float(v[j] << 16);
-                y[8 * q + 2 * j + 1] = __uint_as_float(v[j] & 0xFFFF0000u);
+            for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(y[2 * h + (j >> 1)][2 * (j & 1)], y[2 * h + (j >> 1)][2 * (j & 1) + 1]);
+            if (full) {
+                *reinterpret_cast<u32x4_a2*>(p + 32 * h) = w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (32 * h + j < left) p[32 * h + j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
             }
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) y[j] = j < left ? bf16_bits_to_f32(p[j]) : 0.0f;
     }
-}
-__device__ __forceinline__ void store_out(float* p, int left, const float (&y)[16]) {
-    if (left >= 16) {
+    static constexpr int kLane = 8;  // a lane group's first column is kLane g
+};
+template <>
+struct Outputs<float> {
+    f32x4 v[4];
+    static __device__ __forceinline__ int column(int q, int m) { return 16 * q + m; }
+    __device__ __forceinline__ void load(const float* p, bool full, int left) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            reinterpret_cast<f32x4_a4*>(p)[q] = f32x4{y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]};
-    } else {
+        for (int q = 0; q < 4; ++q) {
+            if (full) {
+                v[q] = *reinterpret_cast<const f32x4_a4*>(p + 16 * q);
+            } else {
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (j < left) p[j] = y[j];
-    }
-}
-__device__ __forceinline__ void store_out(uint16_t* p, int left, const float (&y)[16]) {
-    if (left >= 16) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            u32x4 v;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = pack_bf16x2(y[8 * q + 2 * j], y[8 * q + 2 * j + 1]);
-            reinterpret_cast<u32x4_a2*>(p)[q] = v;
+                for (int j = 0; j < 4; ++j) v[q][j] = p[16 * q + j < left ? 16 * q + j : left - 1];
+            }
         }
-    } else {
+    }
+    __device__ __forceinline__ float get(int o) const { return v[o >> 2][o & 3]; }
+    static __device__ __forceinline__ void store(float* p, bool full, int left, const f32x4 (&y)[4]) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (j < left) p[j] = (uint16_t)f32_to_bf16_bits(y[j]);
+        for (int q = 0; q < 4; ++q) {
+            if (full) {
+                *reinterpret_cast<f32x4_a4*>(p + 16 * q) = y[q];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (16 * q + j < left) p[16 * q + j] = y[q][j];
+            }
+        }
+    }
+    static constexpr int kLane = 4;
+};
+
+// Values r..r + 7 of a row of R, zeros behind its end.  Every lane loads (from the row's end where it has nothing to): a
+// branch that writes the zeros would wait for the loads of the others.  WHOLE: R is a multiple of 8.
+template <bool WHOLE, typename T>
+__device__ __forceinline__ Raw<T> rank_raw(const T* row, int r, int R) {
+    if constexpr (WHOLE) {
+        Raw<T> v = load_raw(row + (r < R ? r : R - 8), 8);
+        const uint32_t keep = r < R ? 0xFFFFFFFFu : 0u;
+        u32x4* w = reinterpret_cast<u32x4*>(&v);
+#pragma unroll
+        for (int j = 0; j < (int)sizeof v / 16; ++j) w[j] &= keep;
+        return v;
+    } else {
+        return gather_raw(row + (r < R ? r : R - 1), 1, r < R ? R - r : 1, r < R);
+    }
+}
+// Factors r..r + 7 of a column (of the last one beyond K: not stored).
+template <bool ACROSS, bool WHOLE, typename WT>
+__device__ __forceinline__ Raw<WT> factors(const WT* w, int aid, int col, int r, int K, int R) {
+    col = col < K ? col : K - 1;
+    if constexpr (ACROSS)
+        return gather_raw(w + ((int64_t)aid * R + (r < R ? r : R - 1)) * K + col, K, r < R ? R - r : 1, r < R);
+    else return rank_raw<WHOLE>(w + ((int64_t)aid * K + col) * R, r, R);
+}
+// Values r..r + 7 of a row's t: the partial sums in order, four loads in flight.
+template <bool WHOLE>
+__device__ __forceinline__ Raw<float> sum_t(const float* row, int64_t stride, int splits, int r, int R) {
+    Raw<float> t = rank_raw<WHOLE>(row, r, R);
+    int s = 1;
+    for (; s + 4 <= splits; s += 4) {
+        Raw<float> u[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) u[k] = rank_raw<WHOLE>(row + (s + k) * stride, r, R);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t.v[j] += u[k].v[j];
+    }
+    for (; s < splits; ++s) {
+        const Raw<float> u = rank_raw<WHOLE>(row + s * stride, r, R);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t.v[j] += u.v[j];
+    }
+    return t;
+}
+__device__ __forceinline__ void store_t(float* row, const Raw<float>& t, int r, int R) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (r + j < R) row[r + j] = t.v[j];
+}
+__device__ __forceinline__ Frag<float> scaled(const Raw<float>& t, float scale) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = t.v[j] * scale;
+    return split8(v);
+}
+
+// WHOLE: every wave's columns are inside and R is a multiple of 8, so that no load has a branch (whose other side would wait
+// for the loads of this one).
+
+// A wave has NC groups of 64 columns, whose factors stay in registers from one tile of 16 rows to the next while the
+// adapter does; the next tile's rows are in flight meanwhile.
+template <typename WT, typename OT, bool ACROSS, bool WHOLE, int RK, int NC>
+__global__ __launch_bounds__(256) void expand_kernel(const AdapterArgs a) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i = lane & 15, g = lane >> 4;
+    const int32_t K = a.C, R = a.R;
+    const int col0 = (blockIdx.x * 4 + wave) * (64 * NC);
+    if (col0 >= K) return;
+    const int lc = Outputs<OT>::kLane * g;  // the lane group's first column
+    const WT* w = reinterpret_cast<const WT*>(a.w);
+    const int64_t tiles = (a.rows + 15) / 16, rank_stride = a.rows * R;
+    const int64_t t_lo = (int64_t)blockIdx.y * a.per_split;  // tiles of this block
+    const int64_t t_hi = t_lo + a.per_split < tiles ? t_lo + a.per_split : tiles;
+    const bool writes_t = a.t && col0 == 0;
+    const OT* res = a.residual ? reinterpret_cast<const OT*>(a.residual) + col0 + lc : nullptr;
+    OT* y = reinterpret_cast<OT*>(a.y) + col0 + lc;
+
+    {
+        struct Tile {
+            int mine;  // the row's adapter, -1: none
+            Outputs<OT> out[NC];
+            Raw<float> t[RK];
+        };
+        auto load = [&](Tile& n, int64_t tile) {
+            int64_t row = tile * 16 + i;
+            const bool in = row < a.rows;
+            row = in ? row : a.rows - 1;  // loaded for nothing, not stored
+            n.mine = in ? adapter_of(a.index, row, a.S) : -1;
+            if (res) {
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+                    if (WHOLE || col0 + 64 * c + lc < K)
+                        n.out[c].load(res + row * K + 64 * c, WHOLE, K - col0 - 64 * c - lc);
+            }
+#pragma unroll
+            for (int k = 0; k < RK; ++k) n.t[k] = sum_t<WHOLE>(a.part + row * R, rank_stride, a.splits, 32 * k + 8 * g, R);
+        };
+        Frag<WT> wf[NC][4][RK];
+        int held = -1;
+        Tile cur, next = {};
+        load(next, t_lo);
+        for (int64_t tile = t_lo; tile < t_hi; ++tile) {
+            cur = next;
+            if (tile + 1 < t_hi) load(next, tile + 1);
+            in_order();
+            const int64_t row = tile * 16 + i;
+            const bool in = row < a.rows;
+            if (writes_t && in) {
+#pragma unroll
+                for (int k = 0; k < RK; ++k) store_t(a.t + row * R, cur.t[k], 32 * k + 8 * g, R);
+            }
+            f32x4 out[NC][4];
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) out[c][j >> 2][j & 3] = cur.out[c].get(j);
+            const uint32_t rows = (uint32_t)__ballot(in) & 0xFFFFu;
+            uint32_t todo = (uint32_t)__ballot(cur.mine >= 0) & 0xFFFFu;
+            while (todo) {
+                const int aid = __builtin_amdgcn_readfirstlane(__shfl(cur.mine, __ffs(todo) - 1, kWave));
+                const uint32_t same = (uint32_t)__ballot(cur.mine == aid) & 0xFFFFu;
+                todo &= ~same;
+                if (aid != held) {
+                    held = aid;
+#pragma unroll
+                    for (int c = 0; c < NC; ++c)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int k = 0; k < RK; ++k)
+                                wf[c][q][k] = frag(factors<ACROSS, WHOLE>(w, aid, col0 + 64 * c + Outputs<OT>::column(q, i),
+                                                                          32 * k + 8 * g, K, R));
+                }
+                // (the adapter's scale by a scalar load: a vector load's wait would be one for the next tile as well)
+                const float scale = a.scale ? a.scale[aid] : 1.0f;
+                Frag<float> tf[RK];
+#pragma unroll
+                for (int k = 0; k < RK; ++k) tf[k] = scaled(cur.t[k], scale);
+                const bool all = same == rows;  // of the tile's rows: the products on top of the residual
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        f32x4 acc = out[c][q];
+#pragma unroll
+                        for (int k = 0; k < RK; ++k) acc = product(wf[c][q][k], tf[k], acc);
+                        if (all) {
+                            out[c][q] = acc;
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) out[c][q][j] = cur.mine == aid ? acc[j] : out[c][q][j];
+                        }
+                    }
+            }
+            if (in) {
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+                    Outputs<OT>::store(y + row * K + 64 * c, WHOLE, K - col0 - 64 * c - lc, out[c]);
+            }
+        }
     }
 }
 
-template <typename WT, typename OT, bool ACROSS, int RK>
-__global__ __launch_bounds__(256) void expand_kernel(const AdapterArgs a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Few rows, each likely with an adapter of its own: the adapters of a tile of 16 rows are dealt over z (never more of
+// them than gridDim.z), so that a block streams the factors of one adapter, kGroups groups of 64 columns a wave, the
+// next group in flight, and touches that adapter's rows alone (z = 0 also those without one).
+constexpr int kGroups = 4;
+
+template <typename WT, typename OT, bool ACROSS, bool WHOLE, int RK>
+__global__ __launch_bounds__(256) void expand_few_kernel(const AdapterArgs a) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4;
     const int32_t K = a.C, R = a.R;
-    const int col0 = (blockIdx.x * 4 + wave) * 64;
-    if (col0 >= K) return;
+    const int col_lo = (blockIdx.x * 4 + wave) * (64 * kGroups);
+    if (col_lo >= K) return;
+    const int lc = Outputs<OT>::kLane * g;
     const WT* w = reinterpret_cast<const WT*>(a.w);
-    const OT* res = reinterpret_cast<const OT*>(a.residual);
-    OT* y = reinterpret_cast<OT*>(a.y);
-    const int64_t tiles = (a.rows + 15) / 16;
-    const bool writes_t = a.t && col0 == 0;
-    const int out_col = col0 + 16 * g, out_left = K - out_col;
-    Frag<WT> wf[4][RK];
-    int held = -1;
-    for (int64_t tile = blockIdx.y; tile < tiles; tile += gridDim.y) {
-        const int64_t row = tile * 16 + i;
-        const bool in = row < a.rows;
-        const int mine = in ? adapter_of(a.index, row, a.S) : -1;
-        float out[16];
+    const int64_t row = (int64_t)blockIdx.y * 16 + i;
+    const bool in = row < a.rows;
+    const int mine = in ? adapter_of(a.index, row, a.S) : -1;
+    uint32_t todo = (uint32_t)__ballot(mine >= 0) & 0xFFFFu;
+    int aid = -1;
+    for (uint32_t slot = 0; todo; ++slot) {
+        aid = __builtin_amdgcn_readfirstlane(__shfl(mine, __ffs(todo) - 1, kWave));
+        if (slot == blockIdx.z) break;
+        todo &= ~(uint32_t)__ballot(mine == aid);
+        aid = -1;
+    }
+    const bool touch = in && ((aid >= 0 && mine == aid) || (mine < 0 && blockIdx.z == 0));
+    if (!__ballot(touch)) return;
+    if (aid < 0) aid = 0;  // only rows without an adapter: they take no product
+    const OT* res = a.residual && touch ? reinterpret_cast<const OT*>(a.residual) + row * K + lc : nullptr;
+    OT* y = reinterpret_cast<OT*>(a.y) + row * K + lc;
+
+    {
+        struct Group {
+            Raw<WT> w[4][RK];
+            Outputs<OT> out;
+        };
+        auto load = [&](Group& n, int col0) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) out[j] = 0.0f;
-        if (in && res && out_left > 0) load_out(res + row * K + out_col, out_left, out);
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int k = 0; k < RK; ++k)
+                    n.w[q][k] = factors<ACROSS, WHOLE>(w, aid, col0 + Outputs<OT>::column(q, i), 32 * k + 8 * g, K, R);
+            if (res && (WHOLE || col0 + lc < K)) n.out.load(res + col0, WHOLE, K - col0 - lc);
+        };
+        Group cur, next = {};
+        load(next, col_lo);
         Frag<float> tf[RK];
-        const float sc = mine >= 0 && a.scale ? a.scale[mine] : 1.0f;
+        const float scale = a.scale ? a.scale[aid] : 1.0f;
+        const float* part = a.part + (in ? row : a.rows - 1) * R;
 #pragma unroll
         for (int k = 0; k < RK; ++k) {
-            const int r = 32 * k + 8 * g, left = in ? R - r : 0;
-            float v[8];
-            load_f32(a.part + row * R + r, left, v);
-            for (int s = 1; s < a.splits; ++s) {
-                float u[8];
-                load_f32(a.part + ((int64_t)s * a.rows + row) * R + r, left, u);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += u[j];
+            Raw<float> t = {};
+            if (touch) {
+                t = sum_t<WHOLE>(part, a.rows * R, a.splits, 32 * k + 8 * g, R);
+                if (a.t && col_lo == 0) store_t(a.t + row * R, t, 32 * k + 8 * g, R);
             }
-            if (writes_t) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < left) a.t[row * R + r + j] = v[j];
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= sc;
-            tf[k] = split8(v);
+            tf[k] = scaled(t, scale);
         }
-        uint32_t todo = (uint32_t)__ballot(mine >= 0) & 0xFFFFu;
-        while (todo) {
-            const int aid = __builtin_amdgcn_readfirstlane(__shfl(mine, __ffs(todo) - 1, kWave));
-            todo &= ~(uint32_t)__ballot(mine == aid);
-            if (aid != held) {
-                held = aid;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    int col = col0 + 16 * (i >> 2) + 4 * q + (i & 3);
-                    col = col < K ? col : K - 1;
-#pragma unroll
-                    for (int k = 0; k < RK; ++k) {
-                        const int r = 32 * k + 8 * g;
-                        wf[q][k] = ACROSS ? gather_frag(w + ((int64_t)aid * R + r) * K + col, K, R - r)
-                                          : load_frag(w + ((int64_t)aid * K + col) * R + r, R - r);
-                    }
-                }
-            }
+        for (int n = 0; n < kGroups; ++n) {
+            const int col0 = col_lo + 64 * n;
+            if (!WHOLE && col0 >= K) break;
+            cur = next;
+            if (n + 1 < kGroups && (WHOLE || col0 + 64 < K)) load(next, col0 + 64);
+            in_order();
+            f32x4 out[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int k = 0; k < RK; ++k) acc = product(wf[q][k], tf[k], acc);
-                if (mine == aid) {
+                for (int j = 0; j < 4; ++j) out[q][j] = cur.out.get(4 * q + j);
+                f32x4 acc = out[q];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) out[4 * q + j] += acc[j];
-                }
+                for (int k = 0; k < RK; ++k) acc = product(frag(cur.w[q][k]), tf[k], acc);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) out[q][j] = mine >= 0 ? acc[j] : out[q][j];
             }
+            if (touch) Outputs<OT>::store(y + col0, WHOLE, K - col0 - lc, out);
         }
-        if (in && out_left > 0) store_out(y + row * K + out_col, out_left, out);
     }
 }
 
 // ---- outer -------------------------------------------------------------------------------
-// out[adapter] = sum over its rows of u[row][r] v[row][c], as [R][C], or with COLS [C][R]; u times the adapter's scale.
-// A block has 64 columns of one adapter and a range of the rows; it gathers the adapter's rows, kList rows of the
-// batch at a time, into a list, whose tiles of 32 its four waves take in turn: v through the wave's own LDS tile
-// (16-byte copies in, the MFMA's 8 rows of a column out).  The waves add through LDS at the end.
-constexpr int kList = 4096;
+// The gradients: out[adapter] = sum over its rows of u[row][r] v[row][c], as [R][C] (da), or with COLS [C][R] (db), u times
+// the adapter's scale.  A block has 64 columns of one adapter and a share of its rows (in the order of order[]), which
+// its eight waves take in tiles of 32.  A wave copies a tile's rows (whole 128-byte pieces of bf16 ones) into LDS and
+// reads the MFMA's operand, 8 rows of a column, by the transposing LDS read, the next tile's rows in flight and the rows of the
+// one after that known.  The waves add through LDS at the end.  Both gradients are one launch.
 constexpr int kPitch = 72;  // elements of a tile's row in LDS: 64 and a shift of the banks
+constexpr int kOuterWaves = 8;
 
-__device__ __forceinline__ void put_tile(uint16_t* to, const uint16_t* p, int left) {
-    *reinterpret_cast<bf16x8*>(to) = load_frag(p, left).hi;
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+
+__device__ __forceinline__ void put_tile(uint16_t* to, const Raw<uint16_t>& r) { *reinterpret_cast<u32x4*>(to) = r.v; }
+__device__ __forceinline__ void put_tile(float* to, const Raw<float>& r) {
+    reinterpret_cast<f32x4*>(to)[0] = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
+    reinterpret_cast<f32x4*>(to)[1] = f32x4{r.v[4], r.v[5], r.v[6], r.v[7]};
 }
-__device__ __forceinline__ void put_tile(float* to, const float* p, int left) {
-    float v[8];
-    load_f32(p, left, v);
-    reinterpret_cast<f32x4*>(to)[0] = f32x4{v[0], v[1], v[2], v[3]};
-    reinterpret_cast<f32x4*>(to)[1] = f32x4{v[4], v[5], v[6], v[7]};
+// Rows 8 g .. 8 g + 7 of column col0 + i.  16 lanes read 4 rows of 16 columns, lane i the 8 bytes of columns 4 (i % 4) .. + 3
+// of row i / 4, and get the 4 rows of column i each.
+__device__ __forceinline__ Frag<uint16_t> get_tile(const uint16_t* tile, int g, int i, int col0) {
+    const uint16_t* p = tile + (8 * g + (i >> 2)) * kPitch + col0 + 4 * (i & 3);
+    const v4i16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)p);
+    const v4i16 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(p + 4 * kPitch));
+    typedef short v8i16 __attribute__((ext_vector_type(8)));
+    const v8i16 v = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    return Frag<uint16_t>{__builtin_bit_cast(bf16x8, v)};
 }
-__device__ __forceinline__ Frag<uint16_t> column(const uint16_t* tile, int g, int col) {
-    return gather_frag(tile + 8 * g * kPitch + col, kPitch, 8);
-}
-__device__ __forceinline__ Frag<float> column(const float* tile, int g, int col) {
-    return gather_frag(tile + 8 * g * kPitch + col, kPitch, 8);
+__device__ __forceinline__ Frag<float> get_tile(const float* tile, int g, int i, int col0) {
+    return frag(gather_raw(tile + 8 * g * kPitch + col0 + i, kPitch, 8));
 }
 
-template <typename VT, bool COLS, int RN>
-__global__ __launch_bounds__(256) void outer_kernel(const AdapterArgs a) {
-    __shared__ uint16_t list[kList];
-    __shared__ int counts[4];
-    __shared__ __attribute__((aligned(16))) VT tiles[4][32 * kPitch];
-    __shared__ f32x4 red[4][4 * 64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+template <typename VT, int RN>
+__global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOuter o) {
+    constexpr int WV = sizeof(VT) == 4 ? 6 : kOuterWaves;  // with a tile: what 64 KB of LDS hold
+    constexpr int kTile = 32 * kPitch * (int)sizeof(VT), kRed = 4 * 64 * 16;
+    __shared__ __attribute__((aligned(16))) char lds[WV * kTile > kOuterWaves * kRed ? WV * kTile : kOuterWaves * kRed];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4;
-    const VT* v = reinterpret_cast<const VT*>(a.x);
-    const int32_t C = a.C, R = a.R;
-    const int col0 = blockIdx.x * 64;
+    const bool second = blockIdx.x >= o.blocks0;
+    const AdapterOuterJob& job = o.job[second ? 1 : 0];
+    const VT* v = reinterpret_cast<const VT*>(job.v);
+    const float* u = job.u;
+    const int32_t C = job.C, R = o.R;
+    const int col0 = (int)(blockIdx.x - (second ? o.blocks0 : 0)) * 64;
     const int aid = blockIdx.z;
-    const float sc = a.scale ? a.scale[aid] : 1.0f;
-    const int64_t r_lo = (int64_t)blockIdx.y * a.per_split;
-    const int64_t r_hi = a.rows - r_lo < a.per_split ? a.rows : r_lo + a.per_split;
-    VT* tile = tiles[wave];
+    const float sc = job.scale ? job.scale[aid] : 1.0f;
+    const int2 span = o.span[aid];
+    const int share = ((span.y + (int)gridDim.y - 1) / (int)gridDim.y + 31) / 32 * 32;
+    const int lo = share * (int)blockIdx.y < span.y ? share * (int)blockIdx.y : span.y;
+    const int n = span.y - lo < share ? span.y - lo : share;  // rows of this block
+    const int32_t* list = o.order + span.x + lo;
 
     f32x4 acc[RN][4];
 #pragma unroll
-    for (int n = 0; n < RN; ++n)
+    for (int m = 0; m < RN; ++m)
 #pragma unroll
-        for (int f = 0; f < 4; ++f) acc[n][f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int f = 0; f < 4; ++f) acc[m][f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    for (int64_t base = r_lo; base < r_hi; base += kList) {
-        // the adapter's rows among these kList: each wave lists a quarter, behind those of the waves before it
-        constexpr int kMine = kList / 4 / 64;
-        const int64_t first = base + wave * (kList / 4);
-        uint32_t found = 0;
-        int count = 0;
-#pragma unroll
-        for (int k = 0; k < kMine; ++k) {
-            const int64_t row = first + 64 * k + lane;
-            const bool is = row < r_hi && a.index[row < r_hi ? row : r_lo] == aid;
-            found |= (uint32_t)is << k;
-            count += __popcll(__ballot(is));
-        }
-        __syncthreads();  // the list's readers of the round before are done
-        if (lane == 0) counts[wave] = count;
-        __syncthreads();
-        int at = 0, n = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            at += k < wave ? counts[k] : 0;
-            n += counts[k];
-        }
-#pragma unroll
-        for (int k = 0; k < kMine; ++k) {
-            const bool is = found >> k & 1;
-            const uint64_t m = __ballot(is);
-            if (is) list[at + __popcll(m & ((1ull << lane) - 1))] = (uint16_t)(wave * (kList / 4) + 64 * k + lane);
-            at += __popcll(m);
-        }
-        __syncthreads();
-        for (int t = wave * 32; t < n; t += 128) {
+    auto body = [&](auto inside) {
+        constexpr bool WHOLE = decltype(inside)::value;  // all 64 columns: no load has a branch
+        VT* tile = reinterpret_cast<VT*>(lds + wave * kTile);
+        const int e = 8 * (lane & 7);  // a row's 64 columns: 8 lanes
+        Raw<VT> raw[4];
+        Raw<float> ur[RN];
+        // lane l: the batch's row of row l % 32 of a tile (of its last one behind the end: that one's values again, times 0)
+        auto rows_of = [&](int t) { return list[t + (lane & 31) < n ? t + (lane & 31) : n - 1]; };
+        auto load = [&](int t, int rows) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int lr = 8 * k + (lane >> 3), e = 8 * (lane & 7);
-                const bool in = t + lr < n;
-                const int64_t row = base + (in ? list[t + lr] : 0);
-                const int left = in ? C - col0 - e : 0;
-                put_tile(tile + lr * kPitch + e, v + row * C + col0 + e, left);
+                const int lr = 8 * k + (lane >> 3);
+                const int64_t row = __shfl(rows, lr, kWave);
+                raw[k] = load_raw(v + row * C + col0 + e, WHOLE ? 8 : C - col0 - e);
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float* ux = u + (int64_t)__shfl(rows, 8 * g + j, kWave) * R;
+#pragma unroll
+                for (int m = 0; m < RN; ++m) ur[m].v[j] = ux[16 * m + i < R ? 16 * m + i : R - 1];
+            }
+        };
+        constexpr int STEP = 32 * WV;
+        int t = wave * 32, rows = 0;
+        if (t < n) {
+            rows = rows_of(t);
+            load(t, rows);
+            if (t + STEP < n) rows = rows_of(t + STEP);
+        }
+        for (; t < n; t += STEP) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) put_tile(tile + (8 * k + (lane >> 3)) * kPitch + e, raw[k]);
             Frag<float> uf[RN];
 #pragma unroll
-            for (int n2 = 0; n2 < RN; ++n2) {
-                float u[8];
-                const int r = 16 * n2 + i;
+            for (int m = 0; m < RN; ++m) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int lr = t + 8 * g + j;
-                    u[j] = lr < n && r < R ? sc * a.part[(base + list[lr]) * R + r] : 0.0f;
-                }
-                uf[n2] = split8(u);
+                for (int j = 0; j < 8; ++j)
+                    ur[m].v[j] = t + 8 * g + j < n && 16 * m + i < R ? ur[m].v[j] * sc : 0.0f;
+                uf[m] = frag(ur[m]);
             }
+            if (t + STEP < n) {
+                load(t + STEP, rows);
+                if (t + 2 * STEP < n) rows = rows_of(t + 2 * STEP);
+            }
+            in_order();
             // the tile is the wave's own: its stores before these reads, in program order
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int f = 0; f < 4; ++f) {
-                const Frag<VT> vf = column(tile, g, 16 * f + i);
+                const Frag<VT> vf = get_tile(tile, g, i, 16 * f);
 #pragma unroll
-                for (int n2 = 0; n2 < RN; ++n2) acc[n2][f] = product(uf[n2], vf, acc[n2][f]);
+                for (int m = 0; m < RN; ++m) acc[m][f] = product(uf[m], vf, acc[m][f]);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
+    };
+    if (wave < WV) {
+        if (col0 + 64 <= C) body(std::true_type());
+        else body(std::false_type());
     }
-    float* out = a.out + ((int64_t)blockIdx.y * a.S + aid) * R * C;
+    float* out = job.out + ((int64_t)blockIdx.y * o.split_stride + (int64_t)aid * R * C);
+    f32x4* red = reinterpret_cast<f32x4*>(lds);  // [waves][4 * 64]
 #pragma unroll
-    for (int n = 0; n < RN; ++n) {
+    for (int m = 0; m < RN; ++m) {
         __syncthreads();
 #pragma unroll
-        for (int f = 0; f < 4; ++f) red[wave][f * 64 + lane] = acc[n][f];
+        for (int f = 0; f < 4; ++f) red[wave * 256 + f * 64 + lane] = acc[m][f];
         __syncthreads();
-        const f32x4 s = (red[0][threadIdx.x] + red[1][threadIdx.x]) + (red[2][threadIdx.x] + red[3][threadIdx.x]);
+        if (threadIdx.x >= 256) continue;
+        f32x4 s = red[threadIdx.x];
+#pragma unroll
+        for (int k = 1; k < kOuterWaves; ++k) s += red[k * 256 + threadIdx.x];
         const int c = col0 + 16 * wave + i;  // thread = (column tile wave, lane)
         if (c < C) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int r = 16 * n + 4 * g + j;
-                if (r < R) out[COLS ? (int64_t)c * R + r : (int64_t)r * C + c] = s[j];
+                const int r = 16 * m + 4 * g + j;
+                if (r < R) out[job.cols ? (int64_t)c * R + r : (int64_t)r * C + c] = s[j];
             }
         }
+    }
+}
+
+// da[i], db[i] = the sum over the splits, in order; part: [splits][na + nb].
+__global__ __launch_bounds__(256) void outer_sum_kernel(const float* __restrict__ part, int32_t splits, int64_t na,
+                                                        int64_t nb, float* __restrict__ da, float* __restrict__ db) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < na + nb; i += (int64_t)gridDim.x * 256) {
+        float s = part[i];
+        for (int k = 1; k < splits; ++k) s += part[k * (na + nb) + i];
+        if (i < na) da[i] = s;
+        else db[i - na] = s;
     }
 }
 
@@ -491,40 +817,76 @@ __global__ __launch_bounds__(256) void outer_kernel(const AdapterArgs a) {
 int tiles16(int32_t R) { return R <= 16 ? 1 : R <= 32 ? 2 : R <= 64 ? 4 : 8; }
 
 template <typename XT, typename WT, bool ACROSS>
-void shrink(const AdapterArgs& a, const AdapterPlan& p, hipStream_t s) {
-    const dim3 grid((unsigned)((a.rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles)), (unsigned)p.splits, (unsigned)p.slots);
-#define TBN_SHRINK(rn, rt) hipLaunchKernelGGL((shrink_kernel<XT, WT, ACROSS, rn, rt>), grid, dim3(256), 0, s, a)
+void shrink(const AdapterArgs& args, const AdapterPlan& p, hipStream_t s) {
+    AdapterArgs a = args;
+    a.per_split = p.per_split;
+    a.row_blocks = (uint32_t)((a.rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
+    const dim3 grid(a.row_blocks + (a.order ? (uint32_t)a.S : 0u), (unsigned)p.splits, (unsigned)p.slots);
+#define TBN_SHRINK(rn, rt, wv) \
+    hipLaunchKernelGGL((shrink_kernel<XT, WT, ACROSS, rn, rt, wv>), grid, dim3(64 * wv), 0, s, a)
     switch (tiles16(a.R) * 8 + p.row_tiles) {
-        case 9: TBN_SHRINK(1, 1); break;
-        case 12: TBN_SHRINK(1, 4); break;
-        case 17: TBN_SHRINK(2, 1); break;
-        case 20: TBN_SHRINK(2, 4); break;
-        case 33: TBN_SHRINK(4, 1); break;
-        case 34: TBN_SHRINK(4, 2); break;
-        default: TBN_SHRINK(8, 1);
+        case 9: TBN_SHRINK(1, 1, 4); break;
+        case 12: TBN_SHRINK(1, 4, 16); break;
+        case 17: TBN_SHRINK(2, 1, 4); break;
+        case 18: TBN_SHRINK(2, 2, 16); break;
+        case 33: TBN_SHRINK(4, 1, 4); break;
+        case 34: TBN_SHRINK(4, 2, 8); break;
+        default: TBN_SHRINK(8, 1, 8);
     }
 #undef TBN_SHRINK
 }
 
 template <typename WT, typename OT, bool ACROSS>
-void expand(const AdapterArgs& a, hipStream_t s) {
-    const int64_t blocks = (a.C + 255) / 256, tiles = (a.rows + 15) / 16;
-    int64_t y = 2048 / blocks;  // eight blocks of a CU at once
-    y = y < 1 ? 1 : y > tiles ? tiles : y;
-    if (y > 65535) y = 65535;
-    const dim3 grid((unsigned)blocks, (unsigned)y);
-#define TBN_EXPAND(rk) hipLaunchKernelGGL((expand_kernel<WT, OT, ACROSS, rk>), grid, dim3(256), 0, s, a)
-    if (a.R <= 32) TBN_EXPAND(1);
-    else if (a.R <= 64) TBN_EXPAND(2);
-    else TBN_EXPAND(4);
+void expand(const AdapterArgs& args, hipStream_t s) {
+    AdapterArgs a = args;
+    const int64_t tiles = (a.rows + 15) / 16;
+    if (a.rows <= kAdapterFewRows) {
+        const int64_t slots = a.S < 16 ? a.S : 16;  // no tile holds more adapters
+        const dim3 grid((unsigned)((a.C + 256 * kGroups - 1) / (256 * kGroups)), (unsigned)tiles,
+                        (unsigned)(slots < a.rows ? slots : a.rows));
+#define TBN_EXPAND(rk)                                                                                                 \
+    if (a.R % 8 == 0 && a.C % (64 * kGroups) == 0)                                                                     \
+        hipLaunchKernelGGL((expand_few_kernel<WT, OT, ACROSS, true, rk>), grid, dim3(256), 0, s, a);                   \
+    else hipLaunchKernelGGL((expand_few_kernel<WT, OT, ACROSS, false, rk>), grid, dim3(256), 0, s, a)
+        if (a.R <= 32) {
+            TBN_EXPAND(1);
+        } else if (a.R <= 64) {
+            TBN_EXPAND(2);
+        } else {
+            TBN_EXPAND(4);
+        }
+#undef TBN_EXPAND
+        return;
+    }
+    // the factors of 128 columns fit a wave's registers for ranks up to 32 in bf16
+    constexpr int kWide = sizeof(WT) == 2 ? 2 : 1;
+    const int wide = a.R <= 32 ? kWide : 1;
+    const int64_t blocks = (a.C + 256 * wide - 1) / (256 * wide);
+    // runs of eight tiles, whose adapter's factors are loaded once, unless that leaves the chip empty
+    int64_t per = blocks * tiles / 1024;
+    per = per < 1 ? 1 : per > 8 ? 8 : per;
+    if ((tiles + per - 1) / per > 65535) per = (tiles + 65534) / 65535;
+    a.per_split = per;
+    const dim3 grid((unsigned)blocks, (unsigned)((tiles + per - 1) / per));
+#define TBN_EXPAND(rk, nc)                                                                                             \
+    if (a.R % 8 == 0 && a.C % (64 * nc) == 0)                                                                          \
+        hipLaunchKernelGGL((expand_kernel<WT, OT, ACROSS, true, rk, nc>), grid, dim3(256), 0, s, a);                   \
+    else hipLaunchKernelGGL((expand_kernel<WT, OT, ACROSS, false, rk, nc>), grid, dim3(256), 0, s, a)
+    if (a.R <= 32) {
+        TBN_EXPAND(1, kWide);
+    } else if (a.R <= 64) {
+        TBN_EXPAND(2, 1);
+    } else {
+        TBN_EXPAND(4, 1);
+    }
 #undef TBN_EXPAND
 }
 
-template <typename VT, bool COLS>
-void outer(const AdapterArgs& a, int32_t splits, hipStream_t s) {
-    const dim3 grid((unsigned)((a.C + 63) / 64), (unsigned)splits, (unsigned)a.S);
-#define TBN_OUTER(rn) hipLaunchKernelGGL((outer_kernel<VT, COLS, rn>), grid, dim3(256), 0, s, a)
-    switch (tiles16(a.R)) {
+template <typename VT>
+void outer(const AdapterOuter& o, int32_t S, int32_t splits, hipStream_t s) {
+    const dim3 grid(o.blocks0 + (unsigned)(o.job[1].out ? (o.job[1].C + 63) / 64 : 0), (unsigned)splits, (unsigned)S);
+#define TBN_OUTER(rn) hipLaunchKernelGGL((outer_kernel<VT, rn>), grid, dim3(64 * kOuterWaves), 0, s, o)
+    switch (tiles16(o.R)) {
         case 1: TBN_OUTER(1); break;
         case 2: TBN_OUTER(2); break;
         case 4: TBN_OUTER(4); break;
@@ -538,32 +900,34 @@ void outer(const AdapterArgs& a, int32_t splits, hipStream_t s) {
 AdapterPlan plan_adapter_shrink(int64_t rows, int32_t C, int32_t R, int32_t S) {
     AdapterPlan p;
     const bool few = rows <= kAdapterFewRows;
-    p.row_tiles = few ? 1 : R <= 32 ? 4 : R <= 64 ? 2 : 1;
-    p.slots = few ? (int32_t)(S < 16 ? S : 16) : 1;
+    p.row_tiles = few ? 1 : R <= 16 ? 4 : R <= 64 ? 2 : 1;
+    p.slots = few ? (S < 16 ? S : 16) : S < 4 ? S : 4;  // a long batch's tiles hold few, mostly one
     if (p.slots > rows) p.slots = (int32_t)rows;
-    const int64_t tiles = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles) * p.slots;
-    int64_t splits = 1024 / tiles;
-    const int64_t most = (C + 255) / 256;  // two rounds of the four waves at least
+    const int waves = few && R <= 64 ? 4 : R <= 32 ? 16 : 8;
+    const int64_t tiles = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles) * (few ? p.slots : 1);
+    int64_t splits = (few ? 512 : 256) / tiles;
+    const int64_t step = 64 * waves, most = (C + 2 * step - 1) / (2 * step);  // two rounds of the waves at least
     if (splits > most) splits = most;
     if (splits < 1) splits = 1;
-    p.per_split = (int32_t)(((C + splits - 1) / splits + 127) / 128 * 128);
+    p.per_split = (int32_t)(((C + splits - 1) / splits + step - 1) / step * step);
     p.splits = (C + p.per_split - 1) / p.per_split;
     return p;
 }
 
-int32_t adapter_outer_splits(int64_t rows, int32_t C, int32_t S, int64_t* per_split) {
-    const int64_t blocks = (int64_t)((C + 63) / 64) * S;
-    int64_t splits = 1024 / blocks;
-    const int64_t most = (rows + 511) / 512;
+int32_t adapter_outer_splits(int64_t rows, int32_t C, int32_t K, int32_t S) {
+    const int64_t blocks = (int64_t)((C + 63) / 64 + (K + 63) / 64) * S;
+    int64_t splits = 2048 / blocks;
+    const int64_t most = (rows + 255) / 256;  // two tiles a wave at least
     if (splits > most) splits = most;
-    if (splits < 1) splits = 1;
-    *per_split = ((rows + splits - 1) / splits + 31) / 32 * 32;
-    return (int32_t)((rows + *per_split - 1) / *per_split);
+    return (int32_t)(splits < 1 ? 1 : splits);
 }
 
-hipError_t launch_adapter_shrink(const AdapterArgs& args, const AdapterPlan& p, int across, hipStream_t s) {
-    AdapterArgs a = args;
-    a.per_split = p.per_split;
+hipError_t launch_adapter_order(const AdapterArgs& a, hipStream_t s) {
+    hipLaunchKernelGGL(order_kernel, dim3((unsigned)a.S), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_adapter_shrink(const AdapterArgs& a, const AdapterPlan& p, int across, hipStream_t s) {
     if (across) {
         if (a.x_f32) a.w_f32 ? shrink<float, float, true>(a, p, s) : shrink<float, uint16_t, true>(a, p, s);
         else a.w_f32 ? shrink<uint16_t, float, true>(a, p, s) : shrink<uint16_t, uint16_t, true>(a, p, s);
@@ -592,17 +956,17 @@ hipError_t launch_adapter_expand(const AdapterArgs& a, int across, hipStream_t s
     return hipGetLastError();
 }
 
-hipError_t launch_adapter_outer(const AdapterArgs& args, int32_t splits, int64_t per_split, int cols, float* partial,
-                                float* out, hipStream_t s) {
-    AdapterArgs a = args;
-    a.per_split = per_split;
-    a.out = splits > 1 ? partial : out;
-    if (cols) a.x_f32 ? outer<float, true>(a, splits, s) : outer<uint16_t, true>(a, splits, s);
-    else a.x_f32 ? outer<float, false>(a, splits, s) : outer<uint16_t, false>(a, splits, s);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || splits == 1) return e;
-    const int64_t count = (int64_t)a.S * a.R * a.C;
-    return launch_split_reduce(partial, splits, count, count, out, 0, s);
+hipError_t launch_adapter_outer(const AdapterOuter& o, int32_t S, int32_t splits, int v_f32, hipStream_t s) {
+    v_f32 ? outer<float>(o, S, splits, s) : outer<uint16_t>(o, S, splits, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_adapter_outer_sum(const float* part, int32_t splits, int64_t na, int64_t nb, float* da, float* db,
+                                    hipStream_t s) {
+    int64_t blocks = (na + nb + 255) / 256;
+    if (blocks > 8192) blocks = 8192;
+    hipLaunchKernelGGL(outer_sum_kernel, dim3((unsigned)blocks), dim3(256), 0, s, part, splits, na, nb, da, db);
+    return hipGetLastError();
 }
 
 }  // namespace tbn

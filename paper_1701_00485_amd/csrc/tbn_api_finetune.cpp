@@ -71,11 +71,12 @@ tbn_status check_adapter(const tbn_adapter_desc* d) {
     return TBN_OK;
 }
 
-// Workspace: the partial sums of t (of dt), and behind them the sums; backward also the partial gradients.
+// Workspace: the partial sums of t (of dt), behind them the sums; backward also the rows by adapter and the partial
+// gradients.
 struct AdapterWs {
     tbn::AdapterPlan plan;
-    int64_t t_off, da_off, db_off, total, da_rows, db_rows;
-    int32_t da_splits, db_splits;
+    int64_t t_off, order_off, span_off, grad_off, total;
+    int32_t grad_splits;
 };
 
 AdapterWs adapter_ws(const tbn_adapter_desc* d, bool backward) {
@@ -83,16 +84,22 @@ AdapterWs adapter_ws(const tbn_adapter_desc* d, bool backward) {
     const int64_t rr = d->rows * d->rank * 4;
     w.plan = tbn::plan_adapter_shrink(d->rows, backward ? d->k : d->c, d->rank, d->adapters);
     w.t_off = w.plan.splits > 1 ? round256(w.plan.splits * rr) : 0;
-    w.da_off = w.t_off + round256(rr);
-    w.total = w.da_off;
+    w.total = w.t_off + round256(rr);
     if (backward) {
-        const int64_t sr = (int64_t)d->adapters * d->rank * 4;
-        w.da_splits = tbn::adapter_outer_splits(d->rows, d->c, d->adapters, &w.da_rows);
-        w.db_splits = tbn::adapter_outer_splits(d->rows, d->k, d->adapters, &w.db_rows);
-        w.db_off = w.da_off + (w.da_splits > 1 ? round256(w.da_splits * sr * d->c) : 0);
-        w.total = w.db_off + (w.db_splits > 1 ? round256(w.db_splits * sr * d->k) : 0);
+        w.order_off = w.total;
+        w.span_off = w.order_off + round256(d->rows * 4);
+        w.grad_off = w.span_off + round256((int64_t)d->adapters * 8);
+        w.grad_splits = tbn::adapter_outer_splits(d->rows, d->c, d->k, d->adapters);
+        const int64_t grads = (int64_t)d->adapters * d->rank * ((int64_t)d->c + d->k) * 4;
+        w.total = w.grad_off + (w.grad_splits > 1 ? round256(w.grad_splits * grads) : 0);
     }
     return w;
+}
+
+// Whether the expanding kernel adds the partial sums itself (every block of 256 columns reads them all) rather than a
+// launch of its own, which takes 2 us and more: up to 16 MB read.
+bool expand_sums(int32_t splits, int64_t rows, int32_t rank, int32_t cols) {
+    return splits > 1 && (cols + 255) / 256 * (rows * rank * 4) * splits <= (16 << 20);
 }
 
 tbn_status check_ws(const void* ws, size_t bytes, int64_t need) {
@@ -194,7 +201,7 @@ tbn_status tbn_adamw_step(const tbn_adamw_tensor* tensors, int32_t n, tbn_state 
         if (!t.w || !t.m || !t.v || !t.g || (eight && (!t.m_scale || !t.v_scale)))
             return fail(TBN_ERR_NULL, "w, m, v, g and, for 8-bit states, the scales are required");
         if (t.count <= 0) return fail(TBN_ERR_SHAPE, "count must be positive");
-        if (t.count > kMostBlocks * tbn::adamw_chunk()) return fail(TBN_ERR_SHAPE, "count too large");
+        if (t.count > kMostBlocks * tbn::kAdamwRound) return fail(TBN_ERR_SHAPE, "count too large");
         if (!std::isfinite(t.weight_decay)) return fail(TBN_ERR_SHAPE, "weight_decay must be finite");
         const uintptr_t s = eight ? 1 : 4;
         if (!aligned(t.w, 4) || !aligned(t.m, s) || !aligned(t.v, s) || !aligned(t.g, gt == TBN_F32 ? 4 : 2) ||
@@ -216,6 +223,11 @@ tbn_status tbn_adamw_step(const tbn_adamw_tensor* tensors, int32_t n, tbn_state 
         b.c1 = -std::expm1(h->step * std::log(h->beta1));
         b.c2 = -std::expm1(h->step * std::log(h->beta2));
     }
+    // a block takes four rounds, whose loads it issues together, unless that leaves CUs without a block
+    int64_t all = 0;
+    for (int32_t i = 0; i < n; ++i) all += (tensors[i].count + tbn::kAdamwRound - 1) / tbn::kAdamwRound;
+    b.rounds = all >= 1024 ? 4 : all >= 512 ? 2 : 1;
+    const int64_t chunk = (int64_t)b.rounds * tbn::kAdamwRound;
     int64_t blocks = 0;
     auto flush = [&]() {
         if (b.n == 0) return hipSuccess;
@@ -226,7 +238,7 @@ tbn_status tbn_adamw_step(const tbn_adamw_tensor* tensors, int32_t n, tbn_state 
     };
     for (int32_t i = 0; i < n; ++i) {
         const tbn_adamw_tensor& t = tensors[i];
-        const int64_t need = (t.count + tbn::adamw_chunk() - 1) / tbn::adamw_chunk();
+        const int64_t need = (t.count + chunk - 1) / chunk;
         if (b.n == tbn::kAdamwTensors || blocks + need > kMostBlocks) {
             const hipError_t e = flush();
             if (e != hipSuccess) return done(e, "tbn_adamw_step");
@@ -283,7 +295,7 @@ tbn_status tbn_adapter_fwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
     p.C = desc->k;
     p.part = sum;
     if (w.plan.splits > 1) {
-        if (desc->rows <= tbn::kAdapterFewRows) {  // a launch less: the expanding kernel adds the partial sums
+        if (expand_sums(w.plan.splits, desc->rows, desc->rank, desc->k)) {
             p.part = part;
             p.splits = w.plan.splits;
             p.t = t;
@@ -314,10 +326,15 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
     char* base = reinterpret_cast<char*>(ws);
     float* part = reinterpret_cast<float*>(base);
     float* dt = reinterpret_cast<float*>(base + w.t_off);
+    int32_t* order = reinterpret_cast<int32_t*>(base + w.order_off);
+    int2* span = reinterpret_cast<int2*>(base + w.span_off);
     hipError_t e;
 
+    tbn::AdapterArgs s = adapter_args(desc, index, wt);
+    s.order = da || db ? order : nullptr;
+    s.span = span;
+    bool summed = true;  // dt holds the sums
     if (dx || da) {
-        tbn::AdapterArgs s = adapter_args(desc, index, wt);
         s.x = dy;
         s.x_f32 = dyt == TBN_F32;
         s.w = b;
@@ -326,10 +343,15 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
         s.part = w.plan.splits > 1 ? part : dt;
         e = tbn::launch_adapter_shrink(s, w.plan, 1, stream);
         if (e != hipSuccess) return done(e, "tbn_adapter_bwd (shrink)");
-        if (w.plan.splits > 1) {
+        summed = w.plan.splits == 1;
+        if (!summed && !(dx && expand_sums(w.plan.splits, desc->rows, desc->rank, desc->c))) {
             e = tbn::launch_adapter_finish(part, desc->rows * desc->rank, w.plan.splits, dt, stream);
             if (e != hipSuccess) return done(e, "tbn_adapter_bwd (sum)");
+            summed = true;
         }
+    } else {
+        e = tbn::launch_adapter_order(s, stream);
+        if (e != hipSuccess) return done(e, "tbn_adapter_bwd (order)");
     }
     if (dx) {
         tbn::AdapterArgs p = adapter_args(desc, index, wt);
@@ -338,30 +360,37 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
         p.y = dx;
         p.y_f32 = dxt == TBN_F32;
         p.C = desc->c;
-        p.part = dt;
+        p.part = summed ? dt : part;
+        p.splits = summed ? 1 : w.plan.splits;
+        p.t = summed ? nullptr : dt;
         e = tbn::launch_adapter_expand(p, 1, stream);
         if (e != hipSuccess) return done(e, "tbn_adapter_bwd (expand)");
     }
-    if (da) {
-        tbn::AdapterArgs o = adapter_args(desc, index, wt);
-        o.x = x;
-        o.x_f32 = xt == TBN_F32;
-        o.C = desc->c;
-        o.part = dt;
-        e = tbn::launch_adapter_outer(o, w.da_splits, w.da_rows, 0, reinterpret_cast<float*>(base + w.da_off), da, stream);
-        if (e != hipSuccess) return done(e, "tbn_adapter_bwd (da)");
+    if (!da && !db) return TBN_OK;
+
+    const int64_t na = da ? (int64_t)desc->adapters * desc->rank * desc->c : 0;
+    const int64_t nb = db ? (int64_t)desc->adapters * desc->rank * desc->k : 0;
+    float* grads = reinterpret_cast<float*>(base + w.grad_off);
+    const bool split = w.grad_splits > 1;
+    tbn::AdapterOuterJob jobs[2] = {{x, dt, nullptr, split ? grads : da, desc->c, 0},
+                                    {dy, t, scale, split ? grads + na : db, desc->k, 1}};
+    const int f32[2] = {xt == TBN_F32, dyt == TBN_F32};
+    tbn::AdapterOuter o = {};
+    o.order = order;
+    o.span = span;
+    o.split_stride = na + nb;
+    o.R = desc->rank;
+    const bool together = da && db && f32[0] == f32[1];
+    for (int k = 0; k < 2; ++k) {
+        if (!(k ? db : da) || (together && k)) continue;
+        o.job[0] = jobs[k];
+        o.job[1] = together ? jobs[1] : tbn::AdapterOuterJob{};
+        o.blocks0 = (uint32_t)((jobs[k].C + 63) / 64);
+        e = tbn::launch_adapter_outer(o, desc->adapters, w.grad_splits, f32[k], stream);
+        if (e != hipSuccess) return done(e, "tbn_adapter_bwd (gradients)");
     }
-    if (db) {
-        tbn::AdapterArgs o = adapter_args(desc, index, wt);
-        o.x = dy;
-        o.x_f32 = dyt == TBN_F32;
-        o.C = desc->k;
-        o.scale = scale;
-        o.part = const_cast<float*>(t);
-        e = tbn::launch_adapter_outer(o, w.db_splits, w.db_rows, 1, reinterpret_cast<float*>(base + w.db_off), db, stream);
-        if (e != hipSuccess) return done(e, "tbn_adapter_bwd (db)");
-    }
-    return TBN_OK;
+    if (!split) return TBN_OK;
+    return done(tbn::launch_adapter_outer_sum(grads, w.grad_splits, na, nb, da, db, stream), "tbn_adapter_bwd (sum)");
 }
 
 }  // extern "C"

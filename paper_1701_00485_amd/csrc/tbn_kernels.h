@@ -364,7 +364,7 @@ struct AdamwTensor {
     float weight_decay;
     int32_t first_block;
 };
-constexpr int kAdamwTensors = 56;  // 64 bytes each: below the 4 KiB of kernel arguments
+constexpr int kAdamwTensors = 62;  // 64 bytes each: what the 4 KiB of kernel arguments hold
 struct AdamwBatch {
     AdamwTensor t[kAdamwTensors];
     int32_t n, first;  // tensors, place of the first one in the caller's list
@@ -372,8 +372,10 @@ struct AdamwBatch {
     const int32_t* step_dev;
     const float* lr_dev;
     double lr, beta1, beta2, eps, c1, c2;
+    int32_t rounds;  // of kAdamwRound elements that a block takes
 };
-int64_t adamw_chunk();  // elements a block takes
+static_assert(sizeof(AdamwBatch) <= 4096, "kernel arguments");
+constexpr int kAdamwRound = 1024, kAdamwRounds = 4;
 hipError_t launch_adamw(const AdamwBatch& b, int64_t blocks, int g_bf16, int eight, hipStream_t stream);
 
 // Layer normalisation; partial: [2][layernorm_bwd_blocks][C] fp32.
@@ -398,31 +400,51 @@ int64_t layernorm_bwd_blocks(int64_t rows, int32_t C);
 hipError_t launch_layernorm_fwd(const LnArgs& a, hipStream_t stream);
 hipError_t launch_layernorm_bwd(const LnArgs& a, hipStream_t stream);
 
-// Low-rank adapters: operands of the three kernels.
+// Low-rank adapters: operands of the kernels.
 struct AdapterArgs {
-    const void* x;         // shrink: rows of C values; outer: the same
+    const void* x;         // shrink: rows of C values
     const void* w;         // shrink, expand: the adapters
     const int32_t* index;  // [rows]
     const float* scale;    // [S] or null
     const void* residual;  // expand: [rows][C] or null
     void* y;               // expand: [rows][C]
     float* t;              // expand: the summed partials are written here, or null
-    float* part;           // shrink: out [splits][rows][R]; expand, outer: in
-    float* out;            // outer
-    int64_t rows, per_split;
+    float* part;           // shrink: out [splits][rows][R]; expand: in
+    int32_t* order;        // the rows by adapter [rows] and each one's begin and count [S]; null: not wanted
+    int2* span;
+    int64_t rows;
+    int64_t per_split;     // shrink: values a split; expand: tiles a block
     int32_t C, R, S, splits;
     int32_t x_f32, w_f32, y_f32;
+    uint32_t row_blocks;   // shrink: blocks in front of the ordering ones
+};
+struct AdapterOuterJob {
+    const void* v;   // rows of C values
+    const float* u;  // rows of R values
+    const float* scale;
+    float* out;      // null: no such job
+    int32_t C, cols;
+};
+struct AdapterOuter {
+    AdapterOuterJob job[2];
+    const int32_t* order;
+    const int2* span;
+    int64_t split_stride;
+    int32_t R;
+    uint32_t blocks0;  // of the first job
 };
 constexpr int64_t kAdapterFewRows = 64;  // up to here each row may well have an adapter of its own
 struct AdapterPlan {
     int32_t row_tiles, slots, splits, per_split;
 };
 AdapterPlan plan_adapter_shrink(int64_t rows, int32_t C, int32_t R, int32_t S);
-int32_t adapter_outer_splits(int64_t rows, int32_t C, int32_t S, int64_t* per_split);
+int32_t adapter_outer_splits(int64_t rows, int32_t C, int32_t K, int32_t S);
+hipError_t launch_adapter_order(const AdapterArgs& a, hipStream_t s);
 hipError_t launch_adapter_shrink(const AdapterArgs& a, const AdapterPlan& p, int across, hipStream_t s);
 hipError_t launch_adapter_finish(const float* part, int64_t count, int32_t splits, float* t, hipStream_t s);
 hipError_t launch_adapter_expand(const AdapterArgs& a, int across, hipStream_t s);
-hipError_t launch_adapter_outer(const AdapterArgs& a, int32_t splits, int64_t per_split, int cols, float* partial,
-                                float* out, hipStream_t s);
+hipError_t launch_adapter_outer(const AdapterOuter& o, int32_t S, int32_t splits, int v_f32, hipStream_t s);
+hipError_t launch_adapter_outer_sum(const float* part, int32_t splits, int64_t na, int64_t nb, float* da, float* db,
+                                    hipStream_t s);
 
 }  // namespace tbn
