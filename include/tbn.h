@@ -470,7 +470,7 @@ tbn_status tbn_softmax_xent(const float* logits, const int32_t* labels, int32_t 
  *   dx, da and db are each optional; one has to be given.
  * Products are exact (of fp32 factors but for 2^-23 of them), sums and t are fp32 in a fixed order.
  * ws: tbn_adapter_workspace_size bytes for TBN_OP_FWD (forward) or TBN_OP_BWD_DATA (backward).
- * Limits: rows <= 2^27, C and K <= 2^24, S R C and S R K < 2^31 (TBN_ERR_SHAPE).
+ * Limits: rows <= 2^27, C and K <= 2^24, rows C and rows K <= 2^36, S R C and S R K < 2^31 (TBN_ERR_SHAPE).
  */
 typedef struct tbn_adapter_desc {
     int64_t rows;

@@ -138,6 +138,19 @@ __device__ __forceinline__ f32x4 product(const Frag<float>& a, const Frag<float>
     return mfma16(a.hi, b.hi, mfma16(a.mid, b.hi, mfma16(a.hi, b.mid, c)));
 }
 
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
+
+// 8 rows of 16 columns of an LDS tile, a column a lane.  Of 16 lanes each names the 8 bytes of 4 neighbouring columns of one of
+// 4 rows (lane i those of columns 4 (i % 4) .. + 3 of row i / 4) and gets the 4 rows of column i; the 4 rows behind likewise.
+__device__ __forceinline__ bf16x8 read_columns(const uint16_t* p, int pitch) {
+    const v4i16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)p);
+    const v4i16 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(p + 4 * pitch));
+    typedef short v8i16 __attribute__((ext_vector_type(8)));
+    const v8i16 v = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    return __builtin_bit_cast(bf16x8, v);
+}
+
 // Nothing moves across: left alone, the compiler turns a loop that multiplies what the round before has loaded back
 // into one that loads and waits.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
@@ -204,10 +217,14 @@ __global__ __launch_bounds__(256) void order_kernel(const AdapterArgs a) {
 
 // ---- shrink ------------------------------------------------------------------------------
 // out[split][row][r] = scale sum over the split's c of x[row][c] W[r][c], W = the row's adapter: [R][C], or with ACROSS
-// [C][R].  A block has a tile of 16 RT rows and one split; its WV waves take the 64 values of c (whole 128-byte lines of
-// bf16 rows) in turn, the next ones in flight, and add through LDS.  With gridDim.z > 1 (few rows, each with its own
-// adapter) the tile's adapters are dealt over z.  In the backward pass S more blocks order the rows for the gradients
-// beside it.
+// [C][R].  A block has a tile of 16 RT rows and one split; its WV waves take 64 values of c each (whole 128-byte lines of
+// bf16 rows), then the same again behind those of all splits, the next ones in flight, and add through LDS.  Blocks next to
+// each other are the splits of one tile: what runs at the same time reads long runs of a row (with the tiles next to
+// each other, all at the same columns of rows that are a power of two apart, a 134 MB batch took 50 us instead of 37).
+// With gridDim.y > 1 the tile's adapters are dealt over y.  In the backward pass S more blocks order the rows for the
+// gradients beside it.
+constexpr int kShrinkWaves = 4;
+
 template <bool ACROSS, typename WT>
 __device__ __forceinline__ Raw<WT> across_or_along(const WT* w, int c, int R, int left) {
     if constexpr (ACROSS) {
@@ -220,38 +237,50 @@ __device__ __forceinline__ Raw<WT> across_or_along(const WT* w, int c, int R, in
 
 template <typename XT, typename WT, bool ACROSS, int RN, int RT, int WV>
 __global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
-    constexpr int STEP = 64 * WV;
     __shared__ f32x4 red[WV][RN * RT * 64];
     if (blockIdx.x >= a.row_blocks) {
-        if (blockIdx.y == 0 && blockIdx.z == 0)
+        if (blockIdx.y == 0)
             order_rows<WV>(a.index, a.rows, a.S, (int32_t)(blockIdx.x - a.row_blocks), a.order, a.span,
-                       reinterpret_cast<int*>(red));
+                           reinterpret_cast<int*>(red));
         return;
     }
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4;
     const XT* x = reinterpret_cast<const XT*>(a.x);
     const WT* w = reinterpret_cast<const WT*>(a.w);
-    const int64_t row0 = (int64_t)blockIdx.x * (16 * RT);
+    const uint32_t tile = blockIdx.x / (uint32_t)a.splits, split = blockIdx.x - tile * (uint32_t)a.splits;
+    const int64_t row0 = (int64_t)tile * (16 * RT);
     const int rows = a.rows - row0 < 16 * RT ? (int)(a.rows - row0) : 16 * RT;
     const int32_t C = a.C, R = a.R;
-    const int c_lo = blockIdx.y * (int)a.per_split;
-    const int c_hi = C - c_lo < a.per_split ? C : c_lo + (int)a.per_split;
-    float* out = a.part + ((int64_t)blockIdx.y * a.rows + row0) * R;
+    const int step = 64 * WV * a.splits;
+    const int c0 = 64 * (WV * (int)split + wave);
+    float* out = a.part + ((int64_t)split * a.rows + row0) * R;
 
-    const int mine = lane < rows ? adapter_of(a.index, row0 + lane, a.S) : -1;
-    uint64_t todo = __ballot(mine >= 0);
     const XT* xr[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
         const int r = 16 * t + i < rows ? 16 * t + i : rows - 1;
         xr[t] = x + (row0 + r) * C + 8 * g;
     }
+    Raw<XT> xv[2][RT];
+    Raw<WT> wv[2][RN];
+    auto load_x = [&](int h, int c, int left) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) xv[h][t] = load_raw(xr[t] + c, left);
+    };
+    const bool ahead = c0 + 64 <= C;  // the first rows' values need no adapter
+    if (ahead) {
+        load_x(0, c0, 8);
+        load_x(1, c0 + 32, 8);
+    }
+    const int mine = lane < rows ? adapter_of(a.index, row0 + lane, a.S) : -1;
+    uint64_t todo = __ballot(mine >= 0);
+    bool first = true;
     for (uint32_t slot = 0; todo; ++slot) {
         const int aid = __builtin_amdgcn_readfirstlane(__shfl(mine, __ffsll((unsigned long long)todo) - 1, kWave));
         const uint64_t same = __ballot(mine == aid);
         todo &= ~same;
-        if (slot % gridDim.z != blockIdx.z) continue;
+        if (slot % gridDim.y != blockIdx.y) continue;
         const WT* wr[RN];
 #pragma unroll
         for (int n = 0; n < RN; ++n) {
@@ -263,13 +292,9 @@ __global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
         for (int n = 0; n < RN; ++n)
 #pragma unroll
             for (int t = 0; t < RT; ++t) acc[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        Raw<WT> wv[2][RN];
-        Raw<XT> xv[2][RT];
-        auto load = [&](int h, int c, int left) {
+        auto load_w = [&](int h, int c, int left) {
 #pragma unroll
             for (int n = 0; n < RN; ++n) wv[h][n] = across_or_along<ACROSS>(wr[n], c, R, left);
-#pragma unroll
-            for (int t = 0; t < RT; ++t) xv[h][t] = load_raw(xr[t] + c, left);
         };
         auto multiply = [&](int h) {
             Frag<WT> wf[RN];
@@ -282,28 +307,38 @@ __global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
                 for (int n = 0; n < RN; ++n) acc[n][t] = product(wf[n], xf, acc[n][t]);
             }
         };
-        int c = c_lo + 64 * wave;
-        if (c + 64 <= c_hi) {
-            load(0, c, 8);
-            load(1, c + 32, 8);
-            for (; c + STEP + 64 <= c_hi; c += STEP) {
+        int c = c0;
+        if (ahead) {
+            load_w(0, c, 8);
+            load_w(1, c + 32, 8);
+            if (!first) {
+                load_x(0, c, 8);
+                load_x(1, c + 32, 8);
+            }
+            for (; c + step + 64 <= C; c += step) {
                 multiply(0);
-                load(0, c + STEP, 8);
+                load_w(0, c + step, 8);
+                load_x(0, c + step, 8);
                 in_order();
                 multiply(1);
-                load(1, c + STEP + 32, 8);
+                load_w(1, c + step + 32, 8);
+                load_x(1, c + step + 32, 8);
                 in_order();
             }
             multiply(0);
             multiply(1);
-            c += STEP;
+            c += step;
         }
-        if (c < c_hi) {  // the last, shorter 64 values
-            load(0, c, C - c - 8 * g);
-            load(1, c + 32, C - c - 32 - 8 * g);
+        if (c < C) {  // the last, shorter 64 values
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                load_w(h, c + 32 * h, C - c - 32 * h - 8 * g);
+                load_x(h, c + 32 * h, C - c - 32 * h - 8 * g);
+            }
             multiply(0);
             multiply(1);
         }
+        first = false;
 #pragma unroll
         for (int n = 0; n < RN; ++n)
 #pragma unroll
@@ -324,7 +359,7 @@ __global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
         }
         __syncthreads();
     }
-    if (blockIdx.z == 0 && wave == 0) {  // rows without an adapter
+    if (blockIdx.y == 0 && wave == 0) {  // rows without an adapter
         uint64_t none = __ballot(lane < rows && mine < 0);
         while (none) {
             const int row = __ffsll((unsigned long long)none) - 1;
@@ -346,10 +381,8 @@ __global__ __launch_bounds__(256) void finish_kernel(const float* __restrict__ p
 
 // ---- expand ------------------------------------------------------------------------------
 // y[row][k] = residual[row][k] + scale sum_r t[row][r] W[k][r], W = the row's adapter: [K][R], or with ACROSS [R][K];
-// t = the sum of `splits` partial ones.  A wave has 64 columns, whose factors stay in registers from one tile of 16
-// rows to the next while the adapter does; the next tile's rows are in flight meanwhile.  Rows of the MFMA's result are
-// dealt to columns so that the four lanes of a row read and store 64 neighbouring bytes at a time.
-//
+// for few rows t is the sum of `splits` partial ones.  Rows of the MFMA's result are dealt to columns so that the four
+// lanes of a row read and store 64 neighbouring bytes at a time.
 // The 16 outputs of lane group g: for bf16 columns 32 p + 8 g + 0..7 (p = 0, 1), for fp32 16 q + 4 g + 0..3 (q = 0..3);
 // result q of the MFMAs, row 4 g + j, is the lane's output 4 q + j.
 template <typename T>
@@ -474,106 +507,143 @@ __device__ __forceinline__ Frag<float> scaled(const Raw<float>& t, float scale) 
 // WHOLE: every wave's columns are inside and R is a multiple of 8, so that no load has a branch (whose other side would wait
 // for the loads of this one).
 
-// A wave has NC groups of 64 columns, whose factors stay in registers from one tile of 16 rows to the next while the
-// adapter does; the next tile's rows are in flight meanwhile.
-template <typename WT, typename OT, bool ACROSS, bool WHOLE, int RK, int NC>
-__global__ __launch_bounds__(256) void expand_kernel(const AdapterArgs a) {
+// Long batches: a block has 64 NC columns of 128 rows, 16 a wave.  Residual (128 NC bytes a row) and t are in flight while
+// the block puts an adapter's factors into LDS, as bf16 parts (so that fp32 ones are split once for 128 rows; [R][K] ones are
+// turned by the transposing LDS read); then every wave that has rows of this adapter multiplies and stores them.
+// Usually all of a block's rows have one adapter.  The chain index, factors, LDS, product, store is long, so what counts is
+// how much each wave has in flight: with 64 columns instead of 256 the kernel ran at half the copy rate.
+constexpr int kExpandWaves = 8;
+
+// The parts of fp32 factors lie `part` values apart.
+__device__ __forceinline__ void put_factors(uint16_t* to, int, const Frag<uint16_t>& f) { *reinterpret_cast<bf16x8*>(to) = f.hi; }
+__device__ __forceinline__ void put_factors(uint16_t* to, int part, const Frag<float>& f) {
+    *reinterpret_cast<bf16x8*>(to) = f.hi;
+    *reinterpret_cast<bf16x8*>(to + part) = f.mid;
+    *reinterpret_cast<bf16x8*>(to + 2 * part) = f.lo;
+}
+__device__ __forceinline__ void get_factors(const uint16_t* from, int, Frag<uint16_t>& f) {
+    f.hi = *reinterpret_cast<const bf16x8*>(from);
+}
+__device__ __forceinline__ void get_factors(const uint16_t* from, int part, Frag<float>& f) {
+    f.hi = *reinterpret_cast<const bf16x8*>(from);
+    f.mid = *reinterpret_cast<const bf16x8*>(from + part);
+    f.lo = *reinterpret_cast<const bf16x8*>(from + 2 * part);
+}
+
+__device__ __forceinline__ void get_across(const uint16_t* from, int pitch, int, Frag<uint16_t>& f) {
+    f.hi = read_columns(from, pitch);
+}
+__device__ __forceinline__ void get_across(const uint16_t* from, int pitch, int part, Frag<float>& f) {
+    f.hi = read_columns(from, pitch);
+    f.mid = read_columns(from + part, pitch);
+    f.lo = read_columns(from + 2 * part, pitch);
+}
+
+template <typename WT, typename OT, bool ACROSS, int RK, int NC>
+__global__ __launch_bounds__(64 * kExpandWaves) void expand_kernel(const AdapterArgs a) {
+    // in LDS as they lie in memory: [columns][R], or with ACROSS [R][columns]
+    constexpr int COLS = 64 * NC, PITCH = (ACROSS ? COLS : 32 * RK) + 8, PART = (ACROSS ? 32 * RK : COLS) * PITCH;
+    __shared__ __attribute__((aligned(16))) uint16_t wt[(sizeof(WT) == 4 ? 3 : 1) * PART];
+    __shared__ int next[kExpandWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4;
     const int32_t K = a.C, R = a.R;
-    const int col0 = (blockIdx.x * 4 + wave) * (64 * NC);
-    if (col0 >= K) return;
-    const int lc = Outputs<OT>::kLane * g;  // the lane group's first column
+    const uint32_t blocks = (uint32_t)(K + COLS - 1) / COLS, row_block = blockIdx.x / blocks;
+    const int col0 = (int)(blockIdx.x - row_block * blocks) * COLS;
+    const int lc = Outputs<OT>::kLane * g;
+    const bool whole = col0 + COLS <= K, whole_r = R % 8 == 0;
     const WT* w = reinterpret_cast<const WT*>(a.w);
-    const int64_t tiles = (a.rows + 15) / 16, rank_stride = a.rows * R;
-    const int64_t t_lo = (int64_t)blockIdx.y * a.per_split;  // tiles of this block
-    const int64_t t_hi = t_lo + a.per_split < tiles ? t_lo + a.per_split : tiles;
-    const bool writes_t = a.t && col0 == 0;
-    const OT* res = a.residual ? reinterpret_cast<const OT*>(a.residual) + col0 + lc : nullptr;
-    OT* y = reinterpret_cast<OT*>(a.y) + col0 + lc;
+    int64_t row = (int64_t)row_block * (16 * kExpandWaves) + 16 * wave + i;
+    const bool in = row < a.rows;
+    if (!in) row = a.rows - 1;  // loaded for nothing, not stored
 
-    {
-        struct Tile {
-            int mine;  // the row's adapter, -1: none
-            Outputs<OT> out[NC];
-            Raw<float> t[RK];
-        };
-        auto load = [&](Tile& n, int64_t tile) {
-            int64_t row = tile * 16 + i;
-            const bool in = row < a.rows;
-            row = in ? row : a.rows - 1;  // loaded for nothing, not stored
-            n.mine = in ? adapter_of(a.index, row, a.S) : -1;
-            if (res) {
+    const int mine = in ? adapter_of(a.index, row, a.S) : -1;
+    Outputs<OT> res[NC] = {};
+    if (a.residual) {
+        const OT* p = reinterpret_cast<const OT*>(a.residual) + row * K + col0 + lc;
+        if (whole) {
 #pragma unroll
-                for (int c = 0; c < NC; ++c)
-                    if (WHOLE || col0 + 64 * c + lc < K)
-                        n.out[c].load(res + row * K + 64 * c, WHOLE, K - col0 - 64 * c - lc);
-            }
-#pragma unroll
-            for (int k = 0; k < RK; ++k) n.t[k] = sum_t<WHOLE>(a.part + row * R, rank_stride, a.splits, 32 * k + 8 * g, R);
-        };
-        Frag<WT> wf[NC][4][RK];
-        int held = -1;
-        Tile cur, next = {};
-        load(next, t_lo);
-        for (int64_t tile = t_lo; tile < t_hi; ++tile) {
-            cur = next;
-            if (tile + 1 < t_hi) load(next, tile + 1);
-            in_order();
-            const int64_t row = tile * 16 + i;
-            const bool in = row < a.rows;
-            if (writes_t && in) {
-#pragma unroll
-                for (int k = 0; k < RK; ++k) store_t(a.t + row * R, cur.t[k], 32 * k + 8 * g, R);
-            }
-            f32x4 out[NC][4];
+            for (int c = 0; c < NC; ++c) res[c].load(p + 64 * c, true, 64);
+        } else {
 #pragma unroll
             for (int c = 0; c < NC; ++c)
+                if (col0 + 64 * c + lc < K) res[c].load(p + 64 * c, false, K - col0 - 64 * c - lc);
+        }
+    }
+    Raw<float> t[RK];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) out[c][j >> 2][j & 3] = cur.out[c].get(j);
-            const uint32_t rows = (uint32_t)__ballot(in) & 0xFFFFu;
-            uint32_t todo = (uint32_t)__ballot(cur.mine >= 0) & 0xFFFFu;
-            while (todo) {
-                const int aid = __builtin_amdgcn_readfirstlane(__shfl(cur.mine, __ffs(todo) - 1, kWave));
-                const uint32_t same = (uint32_t)__ballot(cur.mine == aid) & 0xFFFFu;
-                todo &= ~same;
-                if (aid != held) {
-                    held = aid;
+    for (int k = 0; k < RK; ++k) {
+        if (whole_r) t[k] = rank_raw<true>(a.part + row * R, 32 * k + 8 * g, R);
+        else t[k] = rank_raw<false>(a.part + row * R, 32 * k + 8 * g, R);
+    }
+    OT* y = reinterpret_cast<OT*>(a.y) + row * K + col0 + lc;
+    auto store = [&](int c, const f32x4 (&out)[4]) {
+        if (whole) Outputs<OT>::store(y + 64 * c, true, 64, out);
+        else Outputs<OT>::store(y + 64 * c, false, K - col0 - 64 * c - lc, out);
+    };
+
+    uint32_t todo = (uint32_t)__ballot(mine >= 0) & 0xFFFFu;
+    while (true) {
+        // the next adapter that a wave has rows of left
+        if (lane == 0) next[wave] = todo ? __builtin_amdgcn_readlane(mine, __ffs(todo) - 1) : -1;
+        __syncthreads();
+        int aid = -1;
 #pragma unroll
-                    for (int c = 0; c < NC; ++c)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-#pragma unroll
-                            for (int k = 0; k < RK; ++k)
-                                wf[c][q][k] = frag(factors<ACROSS, WHOLE>(w, aid, col0 + 64 * c + Outputs<OT>::column(q, i),
-                                                                          32 * k + 8 * g, K, R));
+        for (int k = kExpandWaves - 1; k >= 0; --k) aid = next[k] >= 0 ? next[k] : aid;
+        aid = __builtin_amdgcn_readfirstlane(aid);
+        if (aid < 0) break;
+        for (int p = threadIdx.x; p < COLS * 4 * RK; p += 64 * kExpandWaves) {
+            if constexpr (ACROSS) {
+                const int r = p / (8 * NC), c = 8 * (p % (8 * NC));
+                Raw<WT> v = {};
+                if (r < R) {
+                    const WT* from = w + ((int64_t)aid * R + r) * K + col0 + c;
+                    v = whole ? load_raw(from, 8) : load_raw(from, K - col0 - c);
                 }
-                // (the adapter's scale by a scalar load: a vector load's wait would be one for the next tile as well)
-                const float scale = a.scale ? a.scale[aid] : 1.0f;
-                Frag<float> tf[RK];
+                put_factors(wt + r * PITCH + c, PART, frag(v));
+            } else {
+                const int c = p / (4 * RK), r = 8 * (p % (4 * RK));
+                const WT* from = w + ((int64_t)aid * K + (col0 + c < K ? col0 + c : K - 1)) * R;
+                put_factors(wt + c * PITCH + r, PART, frag(whole_r ? rank_raw<true>(from, r, R) : rank_raw<false>(from, r, R)));
+            }
+        }
+        __syncthreads();
+        const uint32_t same = (uint32_t)__ballot(mine == aid) & 0xFFFFu;
+        if (same) {
+            todo &= ~same;
+            const float scale = a.scale ? a.scale[aid] : 1.0f;
+            Frag<float> tf[RK];
 #pragma unroll
-                for (int k = 0; k < RK; ++k) tf[k] = scaled(cur.t[k], scale);
-                const bool all = same == rows;  // of the tile's rows: the products on top of the residual
+            for (int k = 0; k < RK; ++k) tf[k] = scaled(t[k], scale);
 #pragma unroll
-                for (int c = 0; c < NC; ++c)
+            for (int c = 0; c < NC; ++c) {
+                f32x4 out[4];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        f32x4 acc = out[c][q];
+                for (int q = 0; q < 4; ++q) {
 #pragma unroll
-                        for (int k = 0; k < RK; ++k) acc = product(wf[c][q][k], tf[k], acc);
-                        if (all) {
-                            out[c][q] = acc;
-                        } else {
+                    for (int j = 0; j < 4; ++j) out[q][j] = res[c].get(4 * q + j);
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) out[c][q][j] = cur.mine == aid ? acc[j] : out[c][q][j];
-                        }
+                    for (int k = 0; k < RK; ++k) {
+                        Frag<WT> wf;
+                        if constexpr (ACROSS)
+                            get_across(wt + (32 * k + 8 * g + (i >> 2)) * PITCH + 64 * c + Outputs<OT>::column(q, 4 * (i & 3)),
+                                       PITCH, PART, wf);
+                        else get_factors(wt + (64 * c + Outputs<OT>::column(q, i)) * PITCH + 32 * k + 8 * g, PART, wf);
+                        out[q] = product(wf, tf[k], out[q]);
                     }
+                }
+                if (mine == aid) store(c, out);
             }
-            if (in) {
+        }
+        __syncthreads();  // before the next adapter's factors
+    }
+    if (in && mine < 0) {  // rows without an adapter
 #pragma unroll
-                for (int c = 0; c < NC; ++c)
-                    Outputs<OT>::store(y + row * K + 64 * c, WHOLE, K - col0 - 64 * c - lc, out[c]);
-            }
+        for (int c = 0; c < NC; ++c) {
+            f32x4 out[4];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) out[j >> 2][j & 3] = res[c].get(j);
+            store(c, out);
         }
     }
 }
@@ -668,23 +738,14 @@ __global__ __launch_bounds__(256) void expand_few_kernel(const AdapterArgs a) {
 constexpr int kPitch = 72;  // elements of a tile's row in LDS: 64 and a shift of the banks
 constexpr int kOuterWaves = 8;
 
-typedef short v4i16 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) v4i16 lds_v4i16;
-
 __device__ __forceinline__ void put_tile(uint16_t* to, const Raw<uint16_t>& r) { *reinterpret_cast<u32x4*>(to) = r.v; }
 __device__ __forceinline__ void put_tile(float* to, const Raw<float>& r) {
     reinterpret_cast<f32x4*>(to)[0] = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
     reinterpret_cast<f32x4*>(to)[1] = f32x4{r.v[4], r.v[5], r.v[6], r.v[7]};
 }
-// Rows 8 g .. 8 g + 7 of column col0 + i.  16 lanes read 4 rows of 16 columns, lane i the 8 bytes of columns 4 (i % 4) .. + 3
-// of row i / 4, and get the 4 rows of column i each.
+// Rows 8 g .. 8 g + 7 of column col0 + i.
 __device__ __forceinline__ Frag<uint16_t> get_tile(const uint16_t* tile, int g, int i, int col0) {
-    const uint16_t* p = tile + (8 * g + (i >> 2)) * kPitch + col0 + 4 * (i & 3);
-    const v4i16 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)p);
-    const v4i16 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16*)(p + 4 * kPitch));
-    typedef short v8i16 __attribute__((ext_vector_type(8)));
-    const v8i16 v = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-    return Frag<uint16_t>{__builtin_bit_cast(bf16x8, v)};
+    return Frag<uint16_t>{read_columns(tile + (8 * g + (i >> 2)) * kPitch + col0 + 4 * (i & 3), kPitch)};
 }
 __device__ __forceinline__ Frag<float> get_tile(const float* tile, int g, int i, int col0) {
     return frag(gather_raw(tile + 8 * g * kPitch + col0 + i, kPitch, 8));
@@ -819,29 +880,27 @@ int tiles16(int32_t R) { return R <= 16 ? 1 : R <= 32 ? 2 : R <= 64 ? 4 : 8; }
 template <typename XT, typename WT, bool ACROSS>
 void shrink(const AdapterArgs& args, const AdapterPlan& p, hipStream_t s) {
     AdapterArgs a = args;
-    a.per_split = p.per_split;
-    a.row_blocks = (uint32_t)((a.rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
-    const dim3 grid(a.row_blocks + (a.order ? (uint32_t)a.S : 0u), (unsigned)p.splits, (unsigned)p.slots);
-#define TBN_SHRINK(rn, rt, wv) \
-    hipLaunchKernelGGL((shrink_kernel<XT, WT, ACROSS, rn, rt, wv>), grid, dim3(64 * wv), 0, s, a)
+    a.splits = p.splits;
+    a.row_blocks = (uint32_t)((a.rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles) * p.splits);
+    const dim3 grid(a.row_blocks + (a.order ? (uint32_t)a.S : 0u), (unsigned)p.slots);
+#define TBN_SHRINK(rn, rt) \
+    hipLaunchKernelGGL((shrink_kernel<XT, WT, ACROSS, rn, rt, kShrinkWaves>), grid, dim3(64 * kShrinkWaves), 0, s, a)
     switch (tiles16(a.R) * 8 + p.row_tiles) {
-        case 9: TBN_SHRINK(1, 1, 4); break;
-        case 12: TBN_SHRINK(1, 4, 16); break;
-        case 17: TBN_SHRINK(2, 1, 4); break;
-        case 18: TBN_SHRINK(2, 2, 16); break;
-        case 33: TBN_SHRINK(4, 1, 4); break;
-        case 34: TBN_SHRINK(4, 2, 8); break;
-        default: TBN_SHRINK(8, 1, 8);
+        case 9: TBN_SHRINK(1, 1); break;
+        case 12: TBN_SHRINK(1, 4); break;
+        case 17: TBN_SHRINK(2, 1); break;
+        case 20: TBN_SHRINK(2, 4); break;
+        case 33: TBN_SHRINK(4, 1); break;
+        case 34: TBN_SHRINK(4, 2); break;
+        default: TBN_SHRINK(8, 1);
     }
 #undef TBN_SHRINK
 }
 
 template <typename WT, typename OT, bool ACROSS>
-void expand(const AdapterArgs& args, hipStream_t s) {
-    AdapterArgs a = args;
-    const int64_t tiles = (a.rows + 15) / 16;
+void expand(const AdapterArgs& a, hipStream_t s) {
     if (a.rows <= kAdapterFewRows) {
-        const int64_t slots = a.S < 16 ? a.S : 16;  // no tile holds more adapters
+        const int64_t tiles = (a.rows + 15) / 16, slots = a.S < 16 ? a.S : 16;  // no tile holds more adapters
         const dim3 grid((unsigned)((a.C + 256 * kGroups - 1) / (256 * kGroups)), (unsigned)tiles,
                         (unsigned)(slots < a.rows ? slots : a.rows));
 #define TBN_EXPAND(rk)                                                                                                 \
@@ -858,27 +917,16 @@ void expand(const AdapterArgs& args, hipStream_t s) {
 #undef TBN_EXPAND
         return;
     }
-    // the factors of 128 columns fit a wave's registers for ranks up to 32 in bf16
-    constexpr int kWide = sizeof(WT) == 2 ? 2 : 1;
-    const int wide = a.R <= 32 ? kWide : 1;
-    const int64_t blocks = (a.C + 256 * wide - 1) / (256 * wide);
-    // runs of eight tiles, whose adapter's factors are loaded once, unless that leaves the chip empty
-    int64_t per = blocks * tiles / 1024;
-    per = per < 1 ? 1 : per > 8 ? 8 : per;
-    if ((tiles + per - 1) / per > 65535) per = (tiles + 65534) / 65535;
-    a.per_split = per;
-    const dim3 grid((unsigned)blocks, (unsigned)((tiles + per - 1) / per));
-#define TBN_EXPAND(rk, nc)                                                                                             \
-    if (a.R % 8 == 0 && a.C % (64 * nc) == 0)                                                                          \
-        hipLaunchKernelGGL((expand_kernel<WT, OT, ACROSS, true, rk, nc>), grid, dim3(256), 0, s, a);                   \
-    else hipLaunchKernelGGL((expand_kernel<WT, OT, ACROSS, false, rk, nc>), grid, dim3(256), 0, s, a)
-    if (a.R <= 32) {
-        TBN_EXPAND(1, kWide);
-    } else if (a.R <= 64) {
-        TBN_EXPAND(2, 1);
-    } else {
-        TBN_EXPAND(4, 1);
-    }
+    // groups of 64 columns a wave: as many as 64 KB of LDS hold factors for
+    constexpr int kNarrow = 1, kWide = sizeof(WT) == 2 ? 4 : 2, kMiddle = sizeof(WT) == 2 ? 2 : 1;
+    const int nc = a.R <= 32 ? kWide : a.R <= 64 ? kMiddle : kNarrow;
+    const int64_t rows = 16 * kExpandWaves, cols = 64 * nc;
+    const dim3 grid((unsigned)((a.C + cols - 1) / cols * ((a.rows + rows - 1) / rows)));
+#define TBN_EXPAND(rk, n) \
+    hipLaunchKernelGGL((expand_kernel<WT, OT, ACROSS, rk, n>), grid, dim3(64 * kExpandWaves), 0, s, a)
+    if (a.R <= 32) TBN_EXPAND(1, kWide);
+    else if (a.R <= 64) TBN_EXPAND(2, kMiddle);
+    else TBN_EXPAND(4, kNarrow);
 #undef TBN_EXPAND
 }
 
@@ -900,17 +948,17 @@ void outer(const AdapterOuter& o, int32_t S, int32_t splits, hipStream_t s) {
 AdapterPlan plan_adapter_shrink(int64_t rows, int32_t C, int32_t R, int32_t S) {
     AdapterPlan p;
     const bool few = rows <= kAdapterFewRows;
-    p.row_tiles = few ? 1 : R <= 16 ? 4 : R <= 64 ? 2 : 1;
-    p.slots = few ? (S < 16 ? S : 16) : S < 4 ? S : 4;  // a long batch's tiles hold few, mostly one
+    p.row_tiles = few ? 1 : R <= 32 ? 4 : R <= 64 ? 2 : 1;
+    p.slots = few ? (S < 16 ? S : 16) : 1;
     if (p.slots > rows) p.slots = (int32_t)rows;
-    const int waves = few && R <= 64 ? 4 : R <= 32 ? 16 : 8;
-    const int64_t tiles = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles) * (few ? p.slots : 1);
-    int64_t splits = (few ? 512 : 256) / tiles;
-    const int64_t step = 64 * waves, most = (C + 2 * step - 1) / (2 * step);  // two rounds of the waves at least
+    const int64_t tiles = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles) * p.slots;
+    // enough blocks to fill the chip, and for long batches (see the kernel's note) eight splits, four where their partial
+    // sums are a larger share of the traffic; two steps of the waves each at least
+    const int64_t least = few ? 1 : R <= 32 ? 8 : 4, most = C / (2 * 64 * kShrinkWaves);
+    int64_t splits = (few ? 512 : 640) / tiles;
+    if (splits < least) splits = least;
     if (splits > most) splits = most;
-    if (splits < 1) splits = 1;
-    p.per_split = (int32_t)(((C + splits - 1) / splits + step - 1) / step * step);
-    p.splits = (C + p.per_split - 1) / p.per_split;
+    p.splits = (int32_t)(splits < 1 ? 1 : splits);
     return p;
 }
 

@@ -66,7 +66,8 @@ tbn_status check_adapter(const tbn_adapter_desc* d) {
     if (d->rank > 128) return fail(TBN_ERR_UNSUPPORTED, "ranks up to 128");
     if (d->adapters > 65535) return fail(TBN_ERR_UNSUPPORTED, "up to 65535 adapters");
     const int64_t most = 0x7FFFFFFF, sr = (int64_t)d->adapters * d->rank;
-    if (d->rows > (1 << 27) || d->c > (1 << 24) || d->k > (1 << 24) || sr * d->c > most || sr * d->k > most)
+    const int64_t wide = d->c > d->k ? d->c : d->k;
+    if (d->rows > (1 << 27) || wide > (1 << 24) || sr * wide > most || d->rows > ((int64_t)1 << 36) / wide)
         return fail(TBN_ERR_SHAPE, "tensor too large");
     return TBN_OK;
 }
@@ -96,11 +97,8 @@ AdapterWs adapter_ws(const tbn_adapter_desc* d, bool backward) {
     return w;
 }
 
-// Whether the expanding kernel adds the partial sums itself (every block of 256 columns reads them all) rather than a
-// launch of its own, which takes 2 us and more: up to 16 MB read.
-bool expand_sums(int32_t splits, int64_t rows, int32_t rank, int32_t cols) {
-    return splits > 1 && (cols + 255) / 256 * (rows * rank * 4) * splits <= (16 << 20);
-}
+// Whether the expanding kernel adds the partial sums itself, which saves few rows a launch of 2 us.
+bool expand_sums(int32_t splits, int64_t rows) { return splits > 1 && rows <= tbn::kAdapterFewRows; }
 
 tbn_status check_ws(const void* ws, size_t bytes, int64_t need) {
     if (!ws || bytes < (size_t)need) return fail(TBN_ERR_WORKSPACE, "workspace too small");
@@ -295,7 +293,7 @@ tbn_status tbn_adapter_fwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
     p.C = desc->k;
     p.part = sum;
     if (w.plan.splits > 1) {
-        if (expand_sums(w.plan.splits, desc->rows, desc->rank, desc->k)) {
+        if (expand_sums(w.plan.splits, desc->rows)) {
             p.part = part;
             p.splits = w.plan.splits;
             p.t = t;
@@ -344,7 +342,7 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
         e = tbn::launch_adapter_shrink(s, w.plan, 1, stream);
         if (e != hipSuccess) return done(e, "tbn_adapter_bwd (shrink)");
         summed = w.plan.splits == 1;
-        if (!summed && !(dx && expand_sums(w.plan.splits, desc->rows, desc->rank, desc->c))) {
+        if (!summed && !(dx && expand_sums(w.plan.splits, desc->rows))) {
             e = tbn::launch_adapter_finish(part, desc->rows * desc->rank, w.plan.splits, dt, stream);
             if (e != hipSuccess) return done(e, "tbn_adapter_bwd (sum)");
             summed = true;

@@ -413,8 +413,8 @@ struct AdapterArgs {
     int32_t* order;        // the rows by adapter [rows] and each one's begin and count [S]; null: not wanted
     int2* span;
     int64_t rows;
-    int64_t per_split;     // shrink: values a split; expand: tiles a block
-    int32_t C, R, S, splits;
+    int32_t C, R, S;
+    int32_t splits;        // shrink: of the values; expand: partial sums in `part`
     int32_t x_f32, w_f32, y_f32;
     uint32_t row_blocks;   // shrink: blocks in front of the ordering ones
 };
@@ -435,7 +435,7 @@ struct AdapterOuter {
 };
 constexpr int64_t kAdapterFewRows = 64;  // up to here each row may well have an adapter of its own
 struct AdapterPlan {
-    int32_t row_tiles, slots, splits, per_split;
+    int32_t row_tiles, slots, splits;
 };
 AdapterPlan plan_adapter_shrink(int64_t rows, int32_t C, int32_t R, int32_t S);
 int32_t adapter_outer_splits(int64_t rows, int32_t C, int32_t K, int32_t S);
