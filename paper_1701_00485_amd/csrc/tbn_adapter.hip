@@ -248,7 +248,9 @@ __global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
     const int i = lane & 15, g = lane >> 4;
     const XT* x = reinterpret_cast<const XT*>(a.x);
     const WT* w = reinterpret_cast<const WT*>(a.w);
-    const uint32_t tile = blockIdx.x / (uint32_t)a.splits, split = blockIdx.x - tile * (uint32_t)a.splits;
+    const uint32_t slices = (uint32_t)(a.R + 63) / 64, all = (uint32_t)a.splits * slices;
+    const uint32_t tile = blockIdx.x / all, split = (blockIdx.x - tile * all) / slices;
+    const int r0 = 64 * (int)(blockIdx.x % slices);  // of ranks above 64 a block has 64
     const int64_t row0 = (int64_t)tile * (16 * RT);
     const int rows = a.rows - row0 < 16 * RT ? (int)(a.rows - row0) : 16 * RT;
     const int32_t C = a.C, R = a.R;
@@ -284,7 +286,7 @@ __global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
         const WT* wr[RN];
 #pragma unroll
         for (int n = 0; n < RN; ++n) {
-            const int r = 16 * n + i < R ? 16 * n + i : R - 1;
+            const int r = r0 + 16 * n + i < R ? r0 + 16 * n + i : R - 1;
             wr[n] = w + (int64_t)aid * R * C + (ACROSS ? (int64_t)8 * g * R + r : (int64_t)r * C + 8 * g);
         }
         f32x4 acc[RN][RT];
@@ -353,7 +355,7 @@ __global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
             if (!(same >> row & 1)) continue;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int r = 16 * n + 4 * (l >> 4) + j;
+                const int r = r0 + 16 * n + 4 * (l >> 4) + j;
                 if (r < R) out[(int64_t)row * R + r] = sc * s[j];
             }
         }
@@ -364,7 +366,7 @@ __global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
         while (none) {
             const int row = __ffsll((unsigned long long)none) - 1;
             none &= none - 1;
-            for (int r = lane; r < R; r += 64) out[(int64_t)row * R + r] = 0.0f;
+            if (r0 + lane < R) out[(int64_t)row * R + r0 + lane] = 0.0f;
         }
     }
 }
@@ -650,7 +652,7 @@ __global__ __launch_bounds__(64 * kExpandWaves) void expand_kernel(const Adapter
 
 // Few rows, each likely with an adapter of its own: the adapters of a tile of 16 rows are dealt over z (never more of
 // them than gridDim.z), so that a block streams the factors of one adapter, kGroups groups of 64 columns a wave, the
-// next group in flight, and touches that adapter's rows alone (z = 0 also those without one).
+// next ones in flight, and touches that adapter's rows alone (z = 0 also those without one).
 constexpr int kGroups = 4;
 
 template <typename WT, typename OT, bool ACROSS, bool WHOLE, int RK>
@@ -679,53 +681,48 @@ __global__ __launch_bounds__(256) void expand_few_kernel(const AdapterArgs a) {
     const OT* res = a.residual && touch ? reinterpret_cast<const OT*>(a.residual) + row * K + lc : nullptr;
     OT* y = reinterpret_cast<OT*>(a.y) + row * K + lc;
 
-    {
-        struct Group {
-            Raw<WT> w[4][RK];
-            Outputs<OT> out;
-        };
-        auto load = [&](Group& n, int col0) {
+    // step 4 n + q: quarter q of group n, whose factors were loaded AHEAD steps before, its residual with its first quarter's.
+    // For ranks above 32 one step ahead: a step has as many loads there as four have below.
+    constexpr int STEPS = 4 * kGroups, AHEAD = RK == 1 ? 4 : 1;
+    Raw<WT> wv[AHEAD + 1][RK];
+    Outputs<OT> out[2] = {};
+    auto load = [&](int step) {
+        const int n = step / 4, q = step % 4, col0 = col_lo + 64 * n;
+        if (!WHOLE && col0 >= K) return;
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+        for (int k = 0; k < RK; ++k)
+            wv[step % (AHEAD + 1)][k] = factors<ACROSS, WHOLE>(w, aid, col0 + Outputs<OT>::column(q, i), 32 * k + 8 * g, K, R);
+        if (q == 0 && res && (WHOLE || col0 + lc < K)) out[n % 2].load(res + col0, WHOLE, K - col0 - lc);
+    };
 #pragma unroll
-                for (int k = 0; k < RK; ++k)
-                    n.w[q][k] = factors<ACROSS, WHOLE>(w, aid, col0 + Outputs<OT>::column(q, i), 32 * k + 8 * g, K, R);
-            if (res && (WHOLE || col0 + lc < K)) n.out.load(res + col0, WHOLE, K - col0 - lc);
-        };
-        Group cur, next = {};
-        load(next, col_lo);
-        Frag<float> tf[RK];
-        const float scale = a.scale ? a.scale[aid] : 1.0f;
-        const float* part = a.part + (in ? row : a.rows - 1) * R;
+    for (int step = 0; step < AHEAD; ++step) load(step);
+    Frag<float> tf[RK];
+    const float scale = a.scale ? a.scale[aid] : 1.0f;
+    const float* part = a.part + (in ? row : a.rows - 1) * R;
 #pragma unroll
-        for (int k = 0; k < RK; ++k) {
-            Raw<float> t = {};
-            if (touch) {
-                t = sum_t<WHOLE>(part, a.rows * R, a.splits, 32 * k + 8 * g, R);
-                if (a.t && col_lo == 0) store_t(a.t + row * R, t, 32 * k + 8 * g, R);
-            }
-            tf[k] = scaled(t, scale);
+    for (int k = 0; k < RK; ++k) {
+        Raw<float> t = {};
+        if (touch) {
+            t = sum_t<WHOLE>(part, a.rows * R, a.splits, 32 * k + 8 * g, R);
+            if (a.t && col_lo == 0) store_t(a.t + row * R, t, 32 * k + 8 * g, R);
         }
+        tf[k] = scaled(t, scale);
+    }
+    f32x4 y4[4];
 #pragma unroll
-        for (int n = 0; n < kGroups; ++n) {
-            const int col0 = col_lo + 64 * n;
-            if (!WHOLE && col0 >= K) break;
-            cur = next;
-            if (n + 1 < kGroups && (WHOLE || col0 + 64 < K)) load(next, col0 + 64);
-            in_order();
-            f32x4 out[4];
+    for (int step = 0; step < STEPS; ++step) {
+        const int n = step / 4, q = step % 4, col0 = col_lo + 64 * n;
+        if (!WHOLE && col0 >= K) break;
+        if (step + AHEAD < STEPS) load(step + AHEAD);
+        in_order();
+        f32x4 acc;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+        for (int j = 0; j < 4; ++j) acc[j] = y4[q][j] = out[n % 2].get(4 * q + j);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) out[q][j] = cur.out.get(4 * q + j);
-                f32x4 acc = out[q];
+        for (int k = 0; k < RK; ++k) acc = product(frag(wv[step % (AHEAD + 1)][k]), tf[k], acc);
 #pragma unroll
-                for (int k = 0; k < RK; ++k) acc = product(frag(cur.w[q][k]), tf[k], acc);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) out[q][j] = mine >= 0 ? acc[j] : out[q][j];
-            }
-            if (touch) Outputs<OT>::store(y + col0, WHOLE, K - col0 - lc, out);
-        }
+        for (int j = 0; j < 4; ++j) y4[q][j] = mine >= 0 ? acc[j] : y4[q][j];
+        if (q == 3 && touch) Outputs<OT>::store(y + col0, WHOLE, K - col0 - lc, y4);
     }
 }
 
@@ -758,12 +755,14 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
     __shared__ __attribute__((aligned(16))) char lds[WV * kTile > kOuterWaves * kRed ? WV * kTile : kOuterWaves * kRed];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4;
-    const bool second = blockIdx.x >= o.blocks0;
+    const uint32_t slices = (uint32_t)(o.R + 63) / 64, block = blockIdx.x / slices;
+    const int r0 = 64 * (int)(blockIdx.x % slices);  // of ranks above 64 a block has 64
+    const bool second = block >= o.blocks0;
     const AdapterOuterJob& job = o.job[second ? 1 : 0];
     const VT* v = reinterpret_cast<const VT*>(job.v);
     const float* u = job.u;
     const int32_t C = job.C, R = o.R;
-    const int col0 = (int)(blockIdx.x - (second ? o.blocks0 : 0)) * 64;
+    const int col0 = (int)(block - (second ? o.blocks0 : 0)) * 64;
     const int aid = blockIdx.z;
     const float sc = job.scale ? job.scale[aid] : 1.0f;
     const int2 span = o.span[aid];
@@ -797,7 +796,7 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
             for (int j = 0; j < 8; ++j) {
                 const float* ux = u + (int64_t)__shfl(rows, 8 * g + j, kWave) * R;
 #pragma unroll
-                for (int m = 0; m < RN; ++m) ur[m].v[j] = ux[16 * m + i < R ? 16 * m + i : R - 1];
+                for (int m = 0; m < RN; ++m) ur[m].v[j] = ux[r0 + 16 * m + i < R ? r0 + 16 * m + i : R - 1];
             }
         };
         constexpr int STEP = 32 * WV;
@@ -815,7 +814,7 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
             for (int m = 0; m < RN; ++m) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    ur[m].v[j] = t + 8 * g + j < n && 16 * m + i < R ? ur[m].v[j] * sc : 0.0f;
+                    ur[m].v[j] = t + 8 * g + j < n && r0 + 16 * m + i < R ? ur[m].v[j] * sc : 0.0f;
                 uf[m] = frag(ur[m]);
             }
             if (t + STEP < n) {
@@ -856,7 +855,7 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
         if (c < C) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int r = 16 * m + 4 * g + j;
+                const int r = r0 + 16 * m + 4 * g + j;
                 if (r < R) out[job.cols ? (int64_t)c * R + r : (int64_t)r * C + c] = s[j];
             }
         }
@@ -875,13 +874,13 @@ __global__ __launch_bounds__(256) void outer_sum_kernel(const float* __restrict_
 }
 
 // ---- launches ----------------------------------------------------------------------------
-int tiles16(int32_t R) { return R <= 16 ? 1 : R <= 32 ? 2 : R <= 64 ? 4 : 8; }
+int tiles16(int32_t R) { return R <= 16 ? 1 : R <= 32 ? 2 : 4; }
 
 template <typename XT, typename WT, bool ACROSS>
 void shrink(const AdapterArgs& args, const AdapterPlan& p, hipStream_t s) {
     AdapterArgs a = args;
     a.splits = p.splits;
-    a.row_blocks = (uint32_t)((a.rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles) * p.splits);
+    a.row_blocks = (uint32_t)((a.rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles) * p.splits * ((a.R + 63) / 64));
     const dim3 grid(a.row_blocks + (a.order ? (uint32_t)a.S : 0u), (unsigned)p.slots);
 #define TBN_SHRINK(rn, rt) \
     hipLaunchKernelGGL((shrink_kernel<XT, WT, ACROSS, rn, rt, kShrinkWaves>), grid, dim3(64 * kShrinkWaves), 0, s, a)
@@ -891,8 +890,7 @@ void shrink(const AdapterArgs& args, const AdapterPlan& p, hipStream_t s) {
         case 17: TBN_SHRINK(2, 1); break;
         case 20: TBN_SHRINK(2, 4); break;
         case 33: TBN_SHRINK(4, 1); break;
-        case 34: TBN_SHRINK(4, 2); break;
-        default: TBN_SHRINK(8, 1);
+        default: TBN_SHRINK(4, 2);
     }
 #undef TBN_SHRINK
 }
@@ -932,13 +930,13 @@ void expand(const AdapterArgs& a, hipStream_t s) {
 
 template <typename VT>
 void outer(const AdapterOuter& o, int32_t S, int32_t splits, hipStream_t s) {
-    const dim3 grid(o.blocks0 + (unsigned)(o.job[1].out ? (o.job[1].C + 63) / 64 : 0), (unsigned)splits, (unsigned)S);
+    const unsigned slices = (unsigned)(o.R + 63) / 64;
+    const dim3 grid((o.blocks0 + (unsigned)(o.job[1].out ? (o.job[1].C + 63) / 64 : 0)) * slices, (unsigned)splits, (unsigned)S);
 #define TBN_OUTER(rn) hipLaunchKernelGGL((outer_kernel<VT, rn>), grid, dim3(64 * kOuterWaves), 0, s, o)
     switch (tiles16(o.R)) {
         case 1: TBN_OUTER(1); break;
         case 2: TBN_OUTER(2); break;
-        case 4: TBN_OUTER(4); break;
-        default: TBN_OUTER(8);
+        default: TBN_OUTER(4);
     }
 #undef TBN_OUTER
 }
@@ -948,7 +946,7 @@ void outer(const AdapterOuter& o, int32_t S, int32_t splits, hipStream_t s) {
 AdapterPlan plan_adapter_shrink(int64_t rows, int32_t C, int32_t R, int32_t S) {
     AdapterPlan p;
     const bool few = rows <= kAdapterFewRows;
-    p.row_tiles = few ? 1 : R <= 32 ? 4 : R <= 64 ? 2 : 1;
+    p.row_tiles = few ? 1 : R <= 32 ? 4 : 2;
     p.slots = few ? (S < 16 ? S : 16) : 1;
     if (p.slots > rows) p.slots = (int32_t)rows;
     const int64_t tiles = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles) * p.slots;

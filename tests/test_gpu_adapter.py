@@ -162,6 +162,26 @@ def test_long_batch(tbn):
     assert all(torch.equal(p, q) for p, q in zip(out, again))
 
 
+@pytest.mark.parametrize("rank", [8, 40, 64, 72, 128])
+@pytest.mark.parametrize("wt", [BF, F])
+@pytest.mark.parametrize("rows", [3, 33, 130])
+def test_whole_columns(tbn, rank, wt, rows):
+    # both widths multiples of 256 and ranks of 8: no load has a branch
+    run(tbn, make(rows, 512, 768, rank, 3, wt, BF, BF))
+
+
+def test_repeatable(tbn):
+    # the same bits from every call, ragged and whole (a wait too few would show here)
+    for rank, c, k in ((100, 200, 136), (128, 512, 768), (65, 136, 200), (5, 72, 40)):
+        for rows in (5, 90):
+            d = gpu(make(rows, c, k, rank, 3))
+            outs = []
+            for _ in range(4):
+                y, t = tbn.adapter_fwd(d["x"], d["index"], d["a"], d["b"], scale=d["scale"], residual=d["res_y"])
+                outs.append((y, t) + tbn.adapter_bwd(d["x"], d["dy"], d["index"], d["a"], d["b"], t, scale=d["scale"]))
+            assert all(torch.equal(p, q) for o in outs[1:] for p, q in zip(outs[0], o))
+
+
 def test_wide(tbn):
     # many splits of the long sums, single tokens
     for rows in (1, 20):
