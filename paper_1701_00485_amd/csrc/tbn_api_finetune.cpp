@@ -149,7 +149,7 @@ tbn_status tbn_layernorm_workspace_size(int64_t rows, int32_t c, size_t* bytes) 
     if (!bytes) return fail(TBN_ERR_NULL, "bytes is NULL");
     tbn_status st = check_ln(rows, c);
     if (st != TBN_OK) return st;
-    *bytes = (size_t)tbn::layernorm_bwd_blocks(rows, c) * (size_t)c * 8;
+    *bytes = tbn::layernorm_bwd_bytes(rows, c);
     return TBN_OK;
 }
 

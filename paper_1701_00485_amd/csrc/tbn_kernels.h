@@ -378,7 +378,8 @@ static_assert(sizeof(AdamwBatch) <= 4096, "kernel arguments");
 constexpr int kAdamwRound = 1024, kAdamwRounds = 4;
 hipError_t launch_adamw(const AdamwBatch& b, int64_t blocks, int g_bf16, int eight, hipStream_t stream);
 
-// Layer normalisation; partial: [2][layernorm_bwd_blocks][C] fp32.
+// Layer normalisation; partial: [2][layernorm_bwd_blocks][C] fp32, behind it for the longest rows two means a row:
+// layernorm_bwd_bytes in all.
 struct LnArgs {
     const void* x;
     const void* dy;
@@ -397,6 +398,7 @@ struct LnArgs {
     int32_t x_f32, y_f32;
 };
 int64_t layernorm_bwd_blocks(int64_t rows, int32_t C);
+size_t layernorm_bwd_bytes(int64_t rows, int32_t C);
 hipError_t launch_layernorm_fwd(const LnArgs& a, hipStream_t stream);
 hipError_t launch_layernorm_bwd(const LnArgs& a, hipStream_t stream);
 

@@ -415,60 +415,110 @@ __global__ __launch_bounds__(BLOCK) void ln_bwd_kernel(const XT* __restrict__ x,
     }
 }
 
-// Rows that no team holds in registers: a block per row, two passes over it; the sums of dgamma and dbeta live
-// in the block's own row of `partial` (read and written by the thread that owns the columns).
+// Rows that no team holds in registers, in two kernels.  The first, a block a row, leaves mean(h) and mean(h xhat) of
+// each row; in the second a thread has 8 columns and walks down a share of the rows, kDown at a time, with the sums of
+// dgamma and dbeta in registers.  x and dy are read twice, so 4096 rows of 16384, which a team does hold, stay with
+// it; 2048 rows of 32768 bf16 values take 72 + 74 us and 13 for the last sums (those in registers 92 + 15).  One kernel, a
+// block a row, would read and write its sums of dgamma and dbeta in memory for every row: 283 + 39 us.
+constexpr int kDown = 4;
+
 template <typename XT, typename YT>
-__global__ __launch_bounds__(1024) void ln_bwd_long_kernel(const XT* __restrict__ x, const YT* __restrict__ dy,
-                                                           int64_t rows, int32_t C, const float* __restrict__ mean,
-                                                           const float* __restrict__ inv_std,
-                                                           const float* __restrict__ gamma, XT* __restrict__ dx,
-                                                           float* __restrict__ partial) {
+__global__ __launch_bounds__(1024) void ln_bwd_means_kernel(const XT* __restrict__ x, const YT* __restrict__ dy, int64_t rows,
+                                                            int32_t C, const float* __restrict__ mean,
+                                                            const float* __restrict__ inv_std,
+                                                            const float* __restrict__ gamma, float2* __restrict__ means) {
     __shared__ float sh[64];
     int turn = 0;
-    const float inv_c = 1.0f / (float)C;
-    float* pg = partial + (int64_t)blockIdx.x * C;
-    float* pb = partial + (int64_t)(gridDim.x + blockIdx.x) * C;
-    bool first = true;
+    const int pieces = C / 8;
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const XT* xr = x + row * C;
         const YT* dr = dy + row * C;
         const float mu = mean[row], s = inv_std[row];
         float sh1 = 0.0f, sh2 = 0.0f;
-        for (int e = threadIdx.x * 8; e < C; e += 8192) {
-            const Piece xv = load_piece(xr + e, C - e), dv = load_piece(dr + e, C - e);
-            Piece g, dg = Piece{}, db = Piece{};
-            if (gamma) g = load_piece(gamma + e, C - e);
-            if (!first) {
-                dg = load_piece(pg + e, C - e);
-                db = load_piece(pb + e, C - e);
+        for (int first = threadIdx.x; first < pieces; first += 1024 * 2) {
+            Raw<XT> xv[2];
+            Raw<YT> dv[2];
+            Raw<float> gv[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {  // the last piece again behind the end
+                const int e = 8 * (first + 1024 * k < pieces ? first + 1024 * k : pieces - 1);
+                xv[k].load(xr + e);
+                dv[k].load(dr + e);
+                if (gamma) gv[k].load(gamma + e);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (e + j < C) {
-                    const float xh = (xv.v[j] - mu) * s, d = dv.v[j], h = gamma ? d * g.v[j] : d;
-                    dg.v[j] += d * xh;
-                    db.v[j] += d;
-                    sh1 += h;
-                    sh2 += h * xh;
+            for (int k = 0; k < 2; ++k) {
+                const Piece xp = xv[k].piece(), d = dv[k].piece(), g = gv[k].piece();
+                const bool is = first + 1024 * k < pieces;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float h = gamma ? d.v[j] * g.v[j] : d.v[j], hx = h * ((xp.v[j] - mu) * s);
+                    sh1 += is ? h : 0.0f;
+                    sh2 += is ? hx : 0.0f;
                 }
             }
-            store_piece(pg + e, dg, C - e);
-            store_piece(pb + e, db, C - e);
         }
-        first = false;
-        team_sum2<1024>(sh1, sh2, sh, turn);
-        sh1 *= inv_c;
-        sh2 *= inv_c;
-        XT* dxr = dx + row * C;
-        for (int e = threadIdx.x * 8; e < C; e += 8192) {
-            Piece xv = load_piece(xr + e, C - e), dv = load_piece(dr + e, C - e), g;
-            if (gamma) g = load_piece(gamma + e, C - e);
+        if (threadIdx.x == 0 && C % 8) {
+            const Piece xp = load_piece(xr + 8 * pieces, C % 8), d = load_piece(dr + 8 * pieces, C % 8);
+            Piece g;
+            if (gamma) g = load_piece(gamma + 8 * pieces, C % 8);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                xv.v[j] = s * ((gamma ? dv.v[j] * g.v[j] : dv.v[j]) - sh1 - (xv.v[j] - mu) * s * sh2);
-            store_piece(dxr + e, xv, C - e);
+            for (int j = 0; j < 8; ++j) {
+                const float h = gamma ? d.v[j] * g.v[j] : d.v[j], hx = h * ((xp.v[j] - mu) * s);
+                sh1 += j < C % 8 ? h : 0.0f;
+                sh2 += j < C % 8 ? hx : 0.0f;
+            }
         }
+        team_sum2<1024>(sh1, sh2, sh, turn);
+        const float inv_c = 1.0f / (float)C;
+        if (threadIdx.x == 0) means[row] = float2{sh1 * inv_c, sh2 * inv_c};
     }
+}
+
+// partial: [2][gridDim.y][C]; block (i, j): columns 2048 i + 0..2047 of rows j, j + gridDim.y, ...
+template <typename XT, typename YT>
+__global__ __launch_bounds__(256) void ln_bwd_down_kernel(const XT* __restrict__ x, const YT* __restrict__ dy, int64_t rows,
+                                                          int32_t C, const float* __restrict__ mean,
+                                                          const float* __restrict__ inv_std,
+                                                          const float* __restrict__ gamma,
+                                                          const float2* __restrict__ means, XT* __restrict__ dx,
+                                                          float* __restrict__ partial) {
+    const int e = 2048 * (int)blockIdx.x + 8 * (int)threadIdx.x;
+    if (e >= C) return;
+    const int left = C - e;
+    Piece g, dg = {}, db = {};
+    if (gamma) g = load_piece(gamma + e, left);
+    auto one = [&](int64_t row, const Piece& xp, const Piece& d, int count) {
+        const float mu = mean[row], s = inv_std[row];
+        const float2 m = means[row];
+        Piece out;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float xh = (xp.v[j] - mu) * s, h = gamma ? d.v[j] * g.v[j] : d.v[j];
+            dg.v[j] += d.v[j] * xh;
+            db.v[j] += d.v[j];
+            out.v[j] = s * (h - m.x - xh * m.y);
+        }
+        store_piece(dx + row * C + e, out, count);
+    };
+    const int64_t stride = gridDim.y;
+    int64_t row = blockIdx.y;
+    if (2048 * ((int)blockIdx.x + 1) <= C)  // all of the block's columns: no load has a branch
+        for (; row + (kDown - 1) * stride < rows; row += kDown * stride) {
+            Raw<XT> xv[kDown];
+            Raw<YT> dv[kDown];
+#pragma unroll
+            for (int k = 0; k < kDown; ++k) {
+                xv[k].load(x + (row + k * stride) * C + e);
+                dv[k].load(dy + (row + k * stride) * C + e);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < kDown; ++k) one(row + k * stride, xv[k].piece(), dv[k].piece(), 8);
+        }
+    for (; row < rows; row += stride) one(row, load_piece(x + row * C + e, left), load_piece(dy + row * C + e, left), left);
+    store_piece(partial + (int64_t)blockIdx.y * C + e, dg, left);
+    store_piece(partial + (int64_t)(gridDim.y + blockIdx.y) * C + e, db, left);
 }
 
 // dgamma, dbeta = the sums of the blocks' partial rows: 32 columns a block, whose 32 groups of threads take every
@@ -579,8 +629,11 @@ void bwd(const LnArgs& a, int64_t blocks, hipStream_t stream) {
         TBN_LN(7, 256, 4, 256);
         TBN_LN(8, 512, 4, 512);
         default:
-            hipLaunchKernelGGL((ln_bwd_long_kernel<XT, YT>), dim3((unsigned)blocks), dim3(1024), 0, stream, x, dy, a.rows,
-                               a.C, a.mean, a.inv_std, a.gamma, dx, a.partial);
+            float2* means = reinterpret_cast<float2*>(a.partial + 2 * blocks * a.C);
+            hipLaunchKernelGGL((ln_bwd_means_kernel<XT, YT>), dim3((unsigned)(a.rows < 4096 ? a.rows : 4096)), dim3(1024), 0,
+                               stream, x, dy, a.rows, a.C, a.mean, a.inv_std, a.gamma, means);
+            hipLaunchKernelGGL((ln_bwd_down_kernel<XT, YT>), dim3((unsigned)((a.C + 2047) / 2048), (unsigned)blocks), dim3(256),
+                               0, stream, x, dy, a.rows, a.C, a.mean, a.inv_std, a.gamma, means, dx, a.partial);
     }
 #undef TBN_LN
 #undef TBN_LN_CALL
@@ -590,9 +643,18 @@ void bwd(const LnArgs& a, int64_t blocks, hipStream_t stream) {
 
 int64_t layernorm_bwd_blocks(int64_t rows, int32_t C) {
     const int team = bwd_team(C);
-    const int rpb = team < 0 ? 1 : kTeams[team][2] / kTeams[team][0];
+    if (team < 0) {  // shares of the rows: 2048 blocks, at least kDown rows each
+        const int64_t most = (rows + kDown - 1) / kDown, fill = 2048 / ((C + 2047) / 2048);
+        const int64_t shares = fill < most ? fill : most;
+        return shares > 1 ? shares : 1;
+    }
+    const int rpb = kTeams[team][2] / kTeams[team][0];
     const int64_t blocks = (rows + rpb - 1) / rpb;
     return blocks < 512 ? blocks : 512;
+}
+
+size_t layernorm_bwd_bytes(int64_t rows, int32_t C) {
+    return (size_t)layernorm_bwd_blocks(rows, C) * (size_t)C * 8 + (bwd_team(C) < 0 ? (size_t)rows * sizeof(float2) : 0);
 }
 
 hipError_t launch_layernorm_fwd(const LnArgs& a, hipStream_t stream) {

@@ -72,6 +72,13 @@ def test_backward(tbn, rows, c, xt, yt):
     check_backward(x, dy, mean.double(), s.double(), gamma.double(), dx, dgamma, dbeta)
 
 
+@pytest.mark.parametrize("rows,c", [(37, 16385), (75, 18432), (9, 40003), (4, 65536), (1030, 16392)])
+@pytest.mark.parametrize("xt,yt", [(BF, BF), (F, BF), (BF, F), (F, F)])
+def test_backward_long(tbn, rows, c, xt, yt):
+    # several rows a share, shares that end early, columns that end inside a block
+    test_backward(tbn, rows, c, xt, yt)
+
+
 def check_backward(x, dy, mean, s, gamma, dx, dgamma, dbeta):
     c = x.shape[1]
     xh, d = (x.double() - mean) * s, dy.double()
