@@ -542,7 +542,7 @@ __device__ __forceinline__ void get_across(const uint16_t* from, int pitch, int 
 }
 
 template <typename WT, typename OT, bool ACROSS, int RK, int NC>
-__global__ __launch_bounds__(64 * kExpandWaves) void expand_kernel(const AdapterArgs a) {
+__global__ __launch_bounds__(64 * kExpandWaves, 4) void expand_kernel(const AdapterArgs a) {
     // in LDS as they lie in memory: [columns][R], or with ACROSS [R][columns]
     constexpr int COLS = 64 * NC, PITCH = (ACROSS ? COLS : 32 * RK) + 8, PART = (ACROSS ? 32 * RK : COLS) * PITCH;
     __shared__ __attribute__((aligned(16))) uint16_t wt[(sizeof(WT) == 4 ? 3 : 1) * PART];
@@ -916,15 +916,21 @@ void expand(const AdapterArgs& a, hipStream_t s) {
         return;
     }
     // groups of 64 columns a wave: as many as 64 KB of LDS hold factors for
-    constexpr int kNarrow = 1, kWide = sizeof(WT) == 2 ? 4 : 2, kMiddle = sizeof(WT) == 2 ? 2 : 1;
-    const int nc = a.R <= 32 ? kWide : a.R <= 64 ? kMiddle : kNarrow;
-    const int64_t rows = 16 * kExpandWaves, cols = 64 * nc;
-    const dim3 grid((unsigned)((a.C + cols - 1) / cols * ((a.rows + rows - 1) / rows)));
-#define TBN_EXPAND(rk, n) \
-    hipLaunchKernelGGL((expand_kernel<WT, OT, ACROSS, rk, n>), grid, dim3(64 * kExpandWaves), 0, s, a)
-    if (a.R <= 32) TBN_EXPAND(1, kWide);
-    else if (a.R <= 64) TBN_EXPAND(2, kMiddle);
-    else TBN_EXPAND(4, kNarrow);
+    constexpr int kNarrow = 1, kWide = 4, kMiddle = sizeof(WT) == 2 ? 2 : 1;
+    const int64_t tiles = (a.rows + 16 * kExpandWaves - 1) / (16 * kExpandWaves);
+    const bool wide = tiles * ((a.C + 63) / 64) >= 1024;
+#define TBN_EXPAND(rk, n)                                                                                             \
+    hipLaunchKernelGGL((expand_kernel<WT, OT, ACROSS, rk, n>), dim3((unsigned)((a.C + 64 * n - 1) / (64 * n) * tiles)), \
+                       dim3(64 * kExpandWaves), 0, s, a)
+    if (a.R <= 32) {
+        if (wide) TBN_EXPAND(1, kWide);
+        else TBN_EXPAND(1, kNarrow);
+    } else if (a.R <= 64) {
+        if (wide) TBN_EXPAND(2, kMiddle);
+        else TBN_EXPAND(2, kNarrow);
+    } else {
+        TBN_EXPAND(4, kNarrow);
+    }
 #undef TBN_EXPAND
 }
 
