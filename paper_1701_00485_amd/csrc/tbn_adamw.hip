@@ -5,9 +5,9 @@
 //   w = w - lr decay w - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
 //
 // Bound by HBM: 28 bytes a weight with fp32 states and gradients, 16 with 8-bit states, all of it read and
-// written once.  The tensors' pointers are kernel arguments (56 tensors a launch), so that nothing is copied to
-// the device and a captured step replays with them; a block takes kChunk elements of one tensor and finds it
-// by bisecting the tensors' first blocks.
+// written once.  The tensors' pointers are kernel arguments (62 tensors a launch), so that nothing is copied to
+// the device and a captured step replays with them; a block takes 1, 2 or 4 rounds of 1024 elements of one tensor, which
+// it finds by a look at all tensors' first blocks at once.
 //
 // 8-bit states: m and r = sqrt(v) are E4M3 codes times a scale, one for every 256 elements of a tensor (the
 // largest magnitude / 448); the root, because it has half the range of v in powers of two, so that what is small
@@ -126,13 +126,11 @@ __device__ __forceinline__ float wave_top(const float (&x)[4]) {
 
 template <typename GT, bool EIGHT>
 __global__ __launch_bounds__(256) void adamw_kernel(const AdamwBatch b) {
-    // the tensor of this block: the last one whose first block is not behind it
-    int lo = 0, hi = b.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (b.t[mid].first_block <= (int32_t)blockIdx.x) lo = mid;
-        else hi = mid - 1;
-    }
+    // the tensor of this block: the last one whose first block is not behind it (a lane a tensor)
+    const int lane = threadIdx.x & 63;
+    static_assert(kAdamwTensors <= 64, "a lane a tensor");
+    const uint64_t begun = __ballot(lane < b.n && b.t[lane < b.n ? lane : 0].first_block <= (int32_t)blockIdx.x);
+    const int lo = __builtin_amdgcn_readfirstlane(63 - __clzll((long long)begun));
     const AdamwTensor& t = b.t[lo];
     const int64_t count = t.count;
     const int64_t base = (int64_t)((int32_t)blockIdx.x - t.first_block) * ((int64_t)b.rounds * kAdamwRound);
@@ -179,13 +177,23 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwBatch b) {
                 *reinterpret_cast<f32x4_a4*>(pw + i) = f32x4{w.x, w.y, w.z, w.w};
                 *reinterpret_cast<f32x4_a4*>(pm + i) = f32x4{m.x, m.y, m.z, m.w};
                 *reinterpret_cast<f32x4_a4*>(pv + i) = f32x4{v.x, v.y, v.z, v.w};
-            } else {
-                for (int64_t e = i; e < count; ++e) {
-                    float w = pw[e], m = pm[e], v = pv[e], r;
-                    update(w, m, v, r, load1(pg + e), f);
-                    pw[e] = w;
-                    pm[e] = m;
-                    pv[e] = v;
+            } else if (i < count) {  // the last 1 to 3: their loads go out together, the last one's again
+                float w[3], m[3], v[3], g[3], r;
+#pragma unroll
+                for (int j = 0; j < 3; ++j) {
+                    const int64_t e = i + j < count ? i + j : count - 1;
+                    w[j] = pw[e];
+                    m[j] = pm[e];
+                    v[j] = pv[e];
+                    g[j] = load1(pg + e);
+                }
+#pragma unroll
+                for (int j = 0; j < 3; ++j) {
+                    update(w[j], m[j], v[j], r, g[j], f);
+                    if (i + j >= count) break;
+                    pw[i + j] = w[j];
+                    pm[i + j] = m[j];
+                    pv[i + j] = v[j];
                 }
             }
         }
@@ -270,14 +278,14 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwBatch b) {
             } else {
                 r.ms = t.m_scale[blk0 + 4 * k];
                 r.vs = t.v_scale[blk0 + 4 * k];
-                float w[3] = {}, g[3] = {};
+                float w[3], g[3];
 #pragma unroll
-                for (int j = 0; j < 3; ++j) {
-                    if (j >= left) break;
-                    w[j] = pw[i + j];
-                    g[j] = load1(pg + i + j);
-                    r.m |= (uint32_t)pm[i + j] << (8 * j);
-                    r.v |= (uint32_t)pv[i + j] << (8 * j);
+                for (int j = 0; j < 3; ++j) {  // behind the end the tensor's last one, not used
+                    const int64_t e = i + j < count ? i + j : count - 1;
+                    w[j] = pw[e];
+                    g[j] = load1(pg + e);
+                    r.m |= (uint32_t)pm[e] << (8 * j);
+                    r.v |= (uint32_t)pv[e] << (8 * j);
                 }
                 r.w = float4{w[0], w[1], w[2], 0.0f};
                 r.g = float4{g[0], g[1], g[2], 0.0f};

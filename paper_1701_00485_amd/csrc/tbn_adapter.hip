@@ -915,8 +915,11 @@ void expand(const AdapterArgs& a, hipStream_t s) {
 #undef TBN_EXPAND
         return;
     }
-    // groups of 64 columns a wave: as many as 64 KB of LDS hold factors for
-    constexpr int kNarrow = 1, kWide = 4, kMiddle = sizeof(WT) == 2 ? 2 : 1;
+    // Groups of 64 columns a wave: what 64 KB of LDS and 128 registers (two blocks a CU) hold.  With 64 columns up to rank 64
+    // 8192 rows of 4096 and fp32 adapters of rank 64 took 68 us instead of 57; with 128 for higher ranks, which spill,
+    // 5000 rows of 8192 took 67 instead of 54.  Small batches take 64 columns, for more blocks: 100 rows of 512, 4.7 us
+    // instead of 7.8.
+    constexpr int kNarrow = 1, kMiddle = 2, kWide = 4;
     const int64_t tiles = (a.rows + 16 * kExpandWaves - 1) / (16 * kExpandWaves);
     const bool wide = tiles * ((a.C + 63) / 64) >= 1024;
 #define TBN_EXPAND(rk, n)                                                                                             \

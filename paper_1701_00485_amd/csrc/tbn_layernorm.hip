@@ -650,7 +650,8 @@ int64_t layernorm_bwd_blocks(int64_t rows, int32_t C) {
     }
     const int rpb = kTeams[team][2] / kTeams[team][0];
     const int64_t blocks = (rows + rpb - 1) / rpb;
-    return blocks < 512 ? blocks : 512;
+    const int64_t most = kTeams[team][2] > 256 ? 256 : 512;  // the widest have a CU for themselves
+    return blocks < most ? blocks : most;
 }
 
 size_t layernorm_bwd_bytes(int64_t rows, int32_t C) {
