@@ -351,7 +351,8 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
         e = tbn::launch_adapter_order(s, stream);
         if (e != hipSuccess) return done(e, "tbn_adapter_bwd (order)");
     }
-    if (dx) {
+    auto expand = [&]() -> tbn_status {
+        if (!dx) return TBN_OK;
         tbn::AdapterArgs p = adapter_args(desc, index, wt);
         p.w = a;
         p.residual = residual;
@@ -361,10 +362,13 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
         p.part = summed ? dt : part;
         p.splits = summed ? 1 : w.plan.splits;
         p.t = summed ? nullptr : dt;
-        e = tbn::launch_adapter_expand(p, 1, stream);
-        if (e != hipSuccess) return done(e, "tbn_adapter_bwd (expand)");
+        return done(tbn::launch_adapter_expand(p, 1, stream), "tbn_adapter_bwd (expand)");
+    };
+    // The gradients first: they find the end of dy in the caches (unless dt is what the expansion sums).
+    if (!summed || (!da && !db)) {
+        st = expand();
+        if (st != TBN_OK || (!da && !db)) return st;
     }
-    if (!da && !db) return TBN_OK;
 
     const int64_t na = da ? (int64_t)desc->adapters * desc->rank * desc->c : 0;
     const int64_t nb = db ? (int64_t)desc->adapters * desc->rank * desc->k : 0;
@@ -387,8 +391,11 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
         e = tbn::launch_adapter_outer(o, desc->adapters, w.grad_splits, f32[k], stream);
         if (e != hipSuccess) return done(e, "tbn_adapter_bwd (gradients)");
     }
-    if (!split) return TBN_OK;
-    return done(tbn::launch_adapter_outer_sum(grads, w.grad_splits, na, nb, da, db, stream), "tbn_adapter_bwd (sum)");
+    if (split) {
+        e = tbn::launch_adapter_outer_sum(grads, w.grad_splits, na, nb, da, db, stream);
+        if (e != hipSuccess) return done(e, "tbn_adapter_bwd (sum)");
+    }
+    return summed ? expand() : TBN_OK;
 }
 
 }  // extern "C"
