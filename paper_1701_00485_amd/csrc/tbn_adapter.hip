@@ -897,7 +897,7 @@ void shrink(const AdapterArgs& args, const AdapterPlan& p, hipStream_t s) {
 
 template <typename WT, typename OT, bool ACROSS>
 void expand(const AdapterArgs& a, hipStream_t s) {
-    if (a.rows <= kAdapterFewRows) {
+    if (adapter_few_rows(a.rows, a.S)) {
         const int64_t tiles = (a.rows + 15) / 16, slots = a.S < 16 ? a.S : 16;  // no tile holds more adapters
         const dim3 grid((unsigned)((a.C + 256 * kGroups - 1) / (256 * kGroups)), (unsigned)tiles,
                         (unsigned)(slots < a.rows ? slots : a.rows));
@@ -954,7 +954,7 @@ void outer(const AdapterOuter& o, int32_t S, int32_t splits, hipStream_t s) {
 
 AdapterPlan plan_adapter_shrink(int64_t rows, int32_t C, int32_t R, int32_t S) {
     AdapterPlan p;
-    const bool few = rows <= kAdapterFewRows;
+    const bool few = adapter_few_rows(rows, S);
     p.row_tiles = few ? 1 : R <= 32 ? 4 : 2;
     p.slots = few ? (S < 16 ? S : 16) : 1;
     if (p.slots > rows) p.slots = (int32_t)rows;

@@ -98,7 +98,9 @@ AdapterWs adapter_ws(const tbn_adapter_desc* d, bool backward) {
 }
 
 // Whether the expanding kernel adds the partial sums itself, which saves few rows a launch of 2 us.
-bool expand_sums(int32_t splits, int64_t rows) { return splits > 1 && rows <= tbn::kAdapterFewRows; }
+bool expand_sums(int32_t splits, const tbn_adapter_desc* d) {
+    return splits > 1 && tbn::adapter_few_rows(d->rows, d->adapters);
+}
 
 tbn_status check_ws(const void* ws, size_t bytes, int64_t need) {
     if (!ws || bytes < (size_t)need) return fail(TBN_ERR_WORKSPACE, "workspace too small");
@@ -293,7 +295,7 @@ tbn_status tbn_adapter_fwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
     p.C = desc->k;
     p.part = sum;
     if (w.plan.splits > 1) {
-        if (expand_sums(w.plan.splits, desc->rows)) {
+        if (expand_sums(w.plan.splits, desc)) {
             p.part = part;
             p.splits = w.plan.splits;
             p.t = t;
@@ -342,7 +344,7 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
         e = tbn::launch_adapter_shrink(s, w.plan, 1, stream);
         if (e != hipSuccess) return done(e, "tbn_adapter_bwd (shrink)");
         summed = w.plan.splits == 1;
-        if (!summed && !(dx && expand_sums(w.plan.splits, desc->rows))) {
+        if (!summed && !(dx && expand_sums(w.plan.splits, desc))) {
             e = tbn::launch_adapter_finish(part, desc->rows * desc->rank, w.plan.splits, dt, stream);
             if (e != hipSuccess) return done(e, "tbn_adapter_bwd (sum)");
             summed = true;

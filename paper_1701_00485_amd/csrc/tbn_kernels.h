@@ -435,7 +435,13 @@ struct AdapterOuter {
     int32_t R;
     uint32_t blocks0;  // of the first job
 };
-constexpr int64_t kAdapterFewRows = 64;  // up to here each row may well have an adapter of its own
+// Whether each row may well have an adapter of its own: the adapters of 16 rows are then dealt over blocks instead of taken in
+// turn by one.  8192 -> 16384, rank 16, 64 adapters: 128 rows of 128 requests 28 us (in turn 189), 1024 of 1024 154 (278), of 8
+// 41 (39); 512 rows of 8 requests over 8 adapters 29 (39); 512 rows of one adapter 28, but 24 where it is taken for
+// all rows at once (4096 -> 4096, rank 64: 30 and 17).
+inline bool adapter_few_rows(int64_t rows, int32_t adapters) {
+    return rows <= 128 || (rows <= 1024 && rows <= 64 * (int64_t)adapters);
+}
 struct AdapterPlan {
     int32_t row_tiles, slots, splits;
 };
