@@ -346,7 +346,8 @@ tbn_status tbn_sgd_step_quantize(float* w, float* v, const float* g, int64_t k, 
  *            and lr by values in device memory, read when the kernel runs (for captured steps, which the
  *            caller advances between replays); *step_dev >= 1 is the caller's to keep.
  * w, m, v and the scales need no alignment beyond their elements' (views into flat buffers); 16-byte aligned
- * ones are faster.  No two of the written arrays may overlap (TBN_ERR_SHAPE): among them is a tensor listed twice.
+ * ones are faster.  No two of the written arrays may overlap (TBN_ERR_SHAPE): among them is a tensor listed twice;
+ * nor may g overlap them.
  */
 typedef enum tbn_state { TBN_STATE_F32 = 0, TBN_STATE_E4M3 = 1 } tbn_state;
 
@@ -427,7 +428,8 @@ tbn_status tbn_batchnorm_train_bwd(const void* x, const void* y, const void* dy,
 
 /* Layer normalisation of `rows` rows of c values: y = (x - mean) inv_std gamma + beta with the row's mean and
  * inv_std = 1/sqrt(biased var + eps), all in fp32.  x has dtype xt, y yt; gamma and beta [c] are optional (1 and
- * 0), and so are the outputs mean and inv_std [rows], which the backward pass takes.  rows * c at most 2^40. */
+ * 0), and so are the outputs mean and inv_std [rows], which the backward pass takes.  rows * c at most 2^40.
+ * Outputs may not overlap inputs, here and in the backward pass. */
 tbn_status tbn_layernorm_fwd(const void* x, tbn_dtype xt, int64_t rows, int32_t c, const float* gamma,
                              const float* beta, float eps, void* y, tbn_dtype yt, float* mean, float* inv_std,
                              hipStream_t stream);
@@ -457,20 +459,23 @@ tbn_status tbn_softmax_xent(const float* logits, const int32_t* labels, int32_t 
  * codes cannot be moved by small steps): row i of a batch has the adapter index[i] of a bank, or none.
  *   desc     rows of the batch, C inputs, K outputs, rank R (1 to 128), adapters S in the bank (1 to 65535).
  *   index    [rows] int32; a value outside [0, S) (such as -1) is no adapter: that row's product is zero.
- *            Rows may come in any order; those of one adapter side by side run fastest.
+ *            Rows may come in any order; those of one adapter side by side run fastest (beyond 64 rows an adapter of a bank of
+ *            up to 8: 5000 rows that lie by chance take three times as long).
  *   a, b     [S][R][C] and [S][K][R], dtype wt.   scale  [S] fp32, optional (1).
  *
  * tbn_adapter_fwd:  t = A x (fp32, optional output [rows][R], for the backward pass),
  *   y = residual + scale B t.  x [rows][C] dtype xt; residual (optional) and y [rows][K] dtype yt; residual may be y.
- *   Given to tbn_conv2d_fwd as its epilogue's residual, y adds the adapters to the projection before bias-free
+ *   Given to tbn_conv2d_fwd as its epilogue's residual, y adds the adapters to the projection before the
  *   activation: act(alpha_k (x W~) + bias + y).
  * tbn_adapter_bwd:  dt = scale B^T dy, dx = residual + A^T dt (residual: the projection's own gradient, optional; it may be
  *   dx), da = sum over the adapter's rows of dt x, db = scale * sum of dy t, fp32, shaped as a and b and overwritten (zero
  *   for an adapter without rows).  dy [rows][K] dtype dyt; dx and residual [rows][C] dtype dxt; t from the forward pass.
  *   dx, da and db are each optional; one has to be given.
- * Products are exact (of fp32 factors but for 2^-23 of them), sums and t are fp32 in a fixed order.
+ * Products are exact (of fp32 factors but for 2^-23 of them), sums and t are fp32 in a fixed order.  NaN and infinities reach
+ * their own row and adapter alone; an fp32 factor that is infinite, or rounds to infinity as bf16, gives NaN.
+ * Outputs may not overlap inputs but where said above.
  * ws: tbn_adapter_workspace_size bytes for TBN_OP_FWD (forward) or TBN_OP_BWD_DATA (backward).
- * Limits: rows <= 2^27, C and K <= 2^24, rows C and rows K <= 2^36, S R C and S R K < 2^31 (TBN_ERR_SHAPE).
+ * Limits: rows <= 2^27, C and K <= 2^24, rows C and rows K <= 2^35, S R C and S R K < 2^31 (TBN_ERR_SHAPE).
  */
 typedef struct tbn_adapter_desc {
     int64_t rows;

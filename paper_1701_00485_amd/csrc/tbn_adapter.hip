@@ -155,6 +155,12 @@ __device__ __forceinline__ bf16x8 read_columns(const uint16_t* p, int pitch) {
 // into one that loads and waits.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
+// Row r of the kernels' order in the batch.
+template <bool SORTED>
+__device__ __forceinline__ int64_t batch_row(const AdapterArgs& a, int64_t r) {
+    return SORTED ? (int64_t)a.sorted[r] : r;
+}
+
 // The adapter of a row, -1 for none.
 __device__ __forceinline__ int adapter_of(const int32_t* index, int64_t row, int32_t S) {
     const int32_t a = index[row];
@@ -162,10 +168,10 @@ __device__ __forceinline__ int adapter_of(const int32_t* index, int64_t row, int
 }
 
 // ---- the rows of each adapter ------------------------------------------------------------
-// order[]: the rows that have an adapter, by adapter and ascending; span[s] = where adapter s begins and how many rows
-// it has.  One block an adapter: the rows of lower adapters counted, its own listed behind them, 16 rows a thread
+// order[]: the rows that have an adapter, by adapter and ascending, with a block S the rest behind them; span[s] = where adapter
+// s begins and how many rows it has.  One block an adapter: the rows of lower adapters counted, its own listed behind them, 16 rows a thread
 // at a time, each wave behind the rows of the waves before it.
-template <int WV>
+template <int WV, bool REST>
 __device__ void order_rows(const int32_t* __restrict__ index, int64_t rows, int32_t S, int32_t aid,
                            int32_t* __restrict__ order, int2* __restrict__ span, int* sh) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -186,7 +192,8 @@ __device__ void order_rows(const int32_t* __restrict__ index, int64_t rows, int3
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
             const int64_t row = first + 64 * k;
-            const bool is = row < rows && index[row < rows ? row : 0] == aid;
+            const int32_t of = index[row < rows ? row : 0];
+            const bool is = row < rows && (!REST || aid < S ? of == aid : (uint32_t)of >= (uint32_t)S);
             found |= (uint32_t)is << k;
             count += __popcll(__ballot(is));
         }
@@ -207,12 +214,12 @@ __device__ void order_rows(const int32_t* __restrict__ index, int64_t rows, int3
             at += __popcll(m);
         }
     }
-    if (threadIdx.x == 0) span[aid] = int2{begin, total};
+    if (threadIdx.x == 0 && (!REST || aid < S)) span[aid] = int2{begin, total};
 }
 
-__global__ __launch_bounds__(256) void order_kernel(const AdapterArgs a) {
-    __shared__ int sh[4];
-    order_rows<4>(a.index, a.rows, a.S, (int32_t)blockIdx.x, a.order, a.span, sh);
+__global__ __launch_bounds__(1024) void order_kernel(const AdapterArgs a) {
+    __shared__ int sh[16];
+    order_rows<16, true>(a.index, a.rows, a.S, (int32_t)blockIdx.x, a.order, a.span, sh);
 }
 
 // ---- shrink ------------------------------------------------------------------------------
@@ -235,12 +242,12 @@ __device__ __forceinline__ Raw<WT> across_or_along(const WT* w, int c, int R, in
     }
 }
 
-template <typename XT, typename WT, bool ACROSS, int RN, int RT, int WV>
+template <typename XT, typename WT, bool ACROSS, bool SORTED, int RN, int RT, int WV>
 __global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
     __shared__ f32x4 red[WV][RN * RT * 64];
     if (blockIdx.x >= a.row_blocks) {
         if (blockIdx.y == 0)
-            order_rows<WV>(a.index, a.rows, a.S, (int32_t)(blockIdx.x - a.row_blocks), a.order, a.span,
+            order_rows<WV, false>(a.index, a.rows, a.S, (int32_t)(blockIdx.x - a.row_blocks), a.order, a.span,
                            reinterpret_cast<int*>(red));
         return;
     }
@@ -256,13 +263,13 @@ __global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
     const int32_t C = a.C, R = a.R;
     const int step = 64 * WV * a.splits;
     const int c0 = 64 * (WV * (int)split + wave);
-    float* out = a.part + ((int64_t)split * a.rows + row0) * R;
+    float* out = a.part + ((int64_t)split * a.rows + (SORTED ? 0 : row0)) * R;
 
     const XT* xr[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
         const int r = 16 * t + i < rows ? 16 * t + i : rows - 1;
-        xr[t] = x + (row0 + r) * C + 8 * g;
+        xr[t] = x + batch_row<SORTED>(a, row0 + r) * C + 8 * g;
     }
     Raw<XT> xv[2][RT];
     Raw<WT> wv[2][RN];
@@ -275,7 +282,7 @@ __global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
         load_x(0, c0, 8);
         load_x(1, c0 + 32, 8);
     }
-    const int mine = lane < rows ? adapter_of(a.index, row0 + lane, a.S) : -1;
+    const int mine = lane < rows ? adapter_of(a.index, batch_row<SORTED>(a, row0 + lane), a.S) : -1;
     uint64_t todo = __ballot(mine >= 0);
     bool first = true;
     for (uint32_t slot = 0; todo; ++slot) {
@@ -353,10 +360,11 @@ __global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
             for (int k = 1; k < WV; ++k) s += red[k][o];
             const int l = o & 63, n = (o >> 6) / RT, row = 16 * ((o >> 6) % RT) + (l & 15);
             if (!(same >> row & 1)) continue;
+            float* to = out + (SORTED ? (int64_t)a.sorted[row0 + row] : row) * R;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int r = r0 + 16 * n + 4 * (l >> 4) + j;
-                if (r < R) out[(int64_t)row * R + r] = sc * s[j];
+                if (r < R) to[r] = sc * s[j];
             }
         }
         __syncthreads();
@@ -366,7 +374,8 @@ __global__ __launch_bounds__(64 * WV) void shrink_kernel(const AdapterArgs a) {
         while (none) {
             const int row = __ffsll((unsigned long long)none) - 1;
             none &= none - 1;
-            if (r0 + lane < R) out[(int64_t)row * R + r0 + lane] = 0.0f;
+            const int64_t at = SORTED ? (int64_t)a.sorted[row0 + row] : row;
+            if (r0 + lane < R) out[at * R + r0 + lane] = 0.0f;
         }
     }
 }
@@ -558,6 +567,7 @@ __global__ __launch_bounds__(64 * kExpandWaves, 4) void expand_kernel(const Adap
     int64_t row = (int64_t)row_block * (16 * kExpandWaves) + 16 * wave + i;
     const bool in = row < a.rows;
     if (!in) row = a.rows - 1;  // loaded for nothing, not stored
+    if (a.sorted) row = a.sorted[row];
 
     const int mine = in ? adapter_of(a.index, row, a.S) : -1;
     Outputs<OT> res[NC] = {};
@@ -881,16 +891,19 @@ void shrink(const AdapterArgs& args, const AdapterPlan& p, hipStream_t s) {
     AdapterArgs a = args;
     a.splits = p.splits;
     a.row_blocks = (uint32_t)((a.rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles) * p.splits * ((a.R + 63) / 64));
-    const dim3 grid(a.row_blocks + (a.order ? (uint32_t)a.S : 0u), (unsigned)p.slots);
-#define TBN_SHRINK(rn, rt) \
-    hipLaunchKernelGGL((shrink_kernel<XT, WT, ACROSS, rn, rt, kShrinkWaves>), grid, dim3(64 * kShrinkWaves), 0, s, a)
-    switch (tiles16(a.R) * 8 + p.row_tiles) {
-        case 9: TBN_SHRINK(1, 1); break;
-        case 12: TBN_SHRINK(1, 4); break;
-        case 17: TBN_SHRINK(2, 1); break;
-        case 20: TBN_SHRINK(2, 4); break;
-        case 33: TBN_SHRINK(4, 1); break;
-        default: TBN_SHRINK(4, 2);
+    const dim3 grid(a.row_blocks + (a.order && !a.sorted ? (uint32_t)a.S : 0u), (unsigned)p.slots);
+#define TBN_SHRINK(rn, rt, sorted) \
+    hipLaunchKernelGGL((shrink_kernel<XT, WT, ACROSS, sorted, rn, rt, kShrinkWaves>), grid, dim3(64 * kShrinkWaves), 0, s, a)
+    switch (tiles16(a.R) * 8 + p.row_tiles + (a.sorted ? 64 : 0)) {
+        case 9: TBN_SHRINK(1, 1, false); break;
+        case 12: TBN_SHRINK(1, 4, false); break;
+        case 17: TBN_SHRINK(2, 1, false); break;
+        case 20: TBN_SHRINK(2, 4, false); break;
+        case 33: TBN_SHRINK(4, 1, false); break;
+        case 34: TBN_SHRINK(4, 2, false); break;
+        case 64 + 12: TBN_SHRINK(1, 4, true); break;
+        case 64 + 20: TBN_SHRINK(2, 4, true); break;
+        default: TBN_SHRINK(4, 2, true);
     }
 #undef TBN_SHRINK
 }
@@ -958,11 +971,13 @@ AdapterPlan plan_adapter_shrink(int64_t rows, int32_t C, int32_t R, int32_t S) {
     p.row_tiles = few ? 1 : R <= 32 ? 4 : 2;
     p.slots = few ? (S < 16 ? S : 16) : 1;
     if (p.slots > rows) p.slots = (int32_t)rows;
-    const int64_t tiles = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles) * p.slots;
-    // enough blocks to fill the chip, and for long batches (see the kernel's note) eight splits, four where their partial
-    // sums are a larger share of the traffic; two steps of the waves each at least
-    const int64_t least = few ? 1 : R <= 32 ? 8 : 4, most = C / (2 * 64 * kShrinkWaves);
-    int64_t splits = (few ? 512 : 640) / tiles;
+    const int64_t tiles = (rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles);
+    // Enough blocks to fill the chip, two steps of the waves each at least.  With few rows also where each tile has one
+    // adapter: 512 rows of 8192 values of one adapter take 9 us with 4 splits, 17 with one (of 512 adapters 31 either way).
+    // For long batches (see the kernel's note) eight splits, four where their partial sums are a larger share of the traffic.
+    const int64_t one = (128 + tiles - 1) / tiles;
+    const int64_t least = few ? (one < 8 ? one : 8) : R <= 32 ? 8 : 4, most = C / (2 * 64 * kShrinkWaves);
+    int64_t splits = few ? 512 / (tiles * p.slots) : 640 / tiles;
     if (splits < least) splits = least;
     if (splits > most) splits = most;
     p.splits = (int32_t)(splits < 1 ? 1 : splits);
@@ -978,7 +993,7 @@ int32_t adapter_outer_splits(int64_t rows, int32_t C, int32_t K, int32_t S) {
 }
 
 hipError_t launch_adapter_order(const AdapterArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL(order_kernel, dim3((unsigned)a.S), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(order_kernel, dim3((unsigned)a.S + 1u), dim3(1024), 0, s, a);
     return hipGetLastError();
 }
 

@@ -67,7 +67,7 @@ tbn_status check_adapter(const tbn_adapter_desc* d) {
     if (d->adapters > 65535) return fail(TBN_ERR_UNSUPPORTED, "up to 65535 adapters");
     const int64_t most = 0x7FFFFFFF, sr = (int64_t)d->adapters * d->rank;
     const int64_t wide = d->c > d->k ? d->c : d->k;
-    if (d->rows > (1 << 27) || wide > (1 << 24) || sr * wide > most || d->rows > ((int64_t)1 << 36) / wide)
+    if (d->rows > (1 << 27) || wide > (1 << 24) || sr * wide > most || d->rows > ((int64_t)1 << 35) / wide)
         return fail(TBN_ERR_SHAPE, "tensor too large");
     return TBN_OK;
 }
@@ -78,6 +78,7 @@ struct AdapterWs {
     tbn::AdapterPlan plan;
     int64_t t_off, order_off, span_off, grad_off, total;
     int32_t grad_splits;
+    bool sorted;
 };
 
 AdapterWs adapter_ws(const tbn_adapter_desc* d, bool backward) {
@@ -86,10 +87,14 @@ AdapterWs adapter_ws(const tbn_adapter_desc* d, bool backward) {
     w.plan = tbn::plan_adapter_shrink(d->rows, backward ? d->k : d->c, d->rank, d->adapters);
     w.t_off = w.plan.splits > 1 ? round256(w.plan.splits * rr) : 0;
     w.total = w.t_off + round256(rr);
-    if (backward) {
+    w.sorted = tbn::adapter_sorted_rows(d->rows, d->adapters);
+    if (backward || w.sorted) {
         w.order_off = w.total;
         w.span_off = w.order_off + round256(d->rows * 4);
-        w.grad_off = w.span_off + round256((int64_t)d->adapters * 8);
+        w.total = w.span_off + round256((int64_t)d->adapters * 8);
+    }
+    if (backward) {
+        w.grad_off = w.total;
         w.grad_splits = tbn::adapter_outer_splits(d->rows, d->c, d->k, d->adapters);
         const int64_t grads = (int64_t)d->adapters * d->rank * ((int64_t)d->c + d->k) * 4;
         w.total = w.grad_off + (w.grad_splits > 1 ? round256(w.grad_splits * grads) : 0);
@@ -283,10 +288,19 @@ tbn_status tbn_adapter_fwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
     s.w = a;
     s.C = desc->c;
     s.part = w.plan.splits > 1 ? part : sum;
-    hipError_t e = tbn::launch_adapter_shrink(s, w.plan, 0, stream);
+    hipError_t e;
+    if (w.sorted) {
+        s.order = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(ws) + w.order_off);
+        s.span = reinterpret_cast<int2*>(reinterpret_cast<char*>(ws) + w.span_off);
+        s.sorted = s.order;
+        e = tbn::launch_adapter_order(s, stream);
+        if (e != hipSuccess) return done(e, "tbn_adapter_fwd (order)");
+    }
+    e = tbn::launch_adapter_shrink(s, w.plan, 0, stream);
     if (e != hipSuccess) return done(e, "tbn_adapter_fwd (shrink)");
 
     tbn::AdapterArgs p = adapter_args(desc, index, wt);
+    p.sorted = s.sorted;
     p.w = b;
     p.scale = scale;
     p.residual = residual;
@@ -331,8 +345,13 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
     hipError_t e;
 
     tbn::AdapterArgs s = adapter_args(desc, index, wt);
-    s.order = da || db ? order : nullptr;
+    s.order = da || db || w.sorted ? order : nullptr;
     s.span = span;
+    if (w.sorted || !(dx || da)) {
+        e = tbn::launch_adapter_order(s, stream);
+        if (e != hipSuccess) return done(e, "tbn_adapter_bwd (order)");
+        s.sorted = w.sorted ? order : nullptr;
+    }
     bool summed = true;  // dt holds the sums
     if (dx || da) {
         s.x = dy;
@@ -349,13 +368,11 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
             if (e != hipSuccess) return done(e, "tbn_adapter_bwd (sum)");
             summed = true;
         }
-    } else {
-        e = tbn::launch_adapter_order(s, stream);
-        if (e != hipSuccess) return done(e, "tbn_adapter_bwd (order)");
     }
     auto expand = [&]() -> tbn_status {
         if (!dx) return TBN_OK;
         tbn::AdapterArgs p = adapter_args(desc, index, wt);
+        p.sorted = s.sorted;
         p.w = a;
         p.residual = residual;
         p.y = dx;

@@ -414,6 +414,7 @@ struct AdapterArgs {
     float* part;           // shrink: out [splits][rows][R]; expand: in
     int32_t* order;        // the rows by adapter [rows] and each one's begin and count [S]; null: not wanted
     int2* span;
+    const int32_t* sorted;  // the rows' places in this order (behind them the rows without an adapter), or null: as they lie
     int64_t rows;
     int32_t C, R, S;
     int32_t splits;        // shrink: of the values; expand: partial sums in `part`
@@ -436,12 +437,14 @@ struct AdapterOuter {
     uint32_t blocks0;  // of the first job
 };
 // Whether each row may well have an adapter of its own: the adapters of 16 rows are then dealt over blocks instead of taken in
-// turn by one.  8192 -> 16384, rank 16, 64 adapters: 128 rows of 128 requests 28 us (in turn 189), 1024 of 1024 154 (278), of 8
-// 41 (39); 512 rows of 8 requests over 8 adapters 29 (39); 512 rows of one adapter 28, but 24 where it is taken for
-// all rows at once (4096 -> 4096, rank 64: 30 and 17).
-inline bool adapter_few_rows(int64_t rows, int32_t adapters) {
-    return rows <= 128 || (rows <= 1024 && rows <= 64 * (int64_t)adapters);
-}
+// turn by one.  8192 -> 16384, rank 16, 64 adapters: 128 rows of 128 requests 28 us (in turn 189), 1024 of 1024 154 (278), of
+// 8 35 (39), of one 31 (30).  In a small bank fewer adapters meet in a tile: 100 rows of one adapter, 512 -> 1000 backward,
+// 17.2 us against 16.3 in turn.
+inline bool adapter_few_rows(int64_t rows, int32_t adapters) { return rows <= 1024 && rows <= 64 * (int64_t)adapters; }
+// Whether the other batches are taken in the order of their adapters, which costs a launch (7 us) and, where rows lie by
+// chance, saves a pass for every further adapter of a tile.  5000 rows, 4096 -> 4096, rank 32: each row one of 64 adapters 77 us
+// (as they lie 590), of 9 62; 11 prompts 58 to 61 (50).  A small bank's rows are taken as they lie: of 8 adapters by chance 137 us.
+inline bool adapter_sorted_rows(int64_t rows, int32_t adapters) { return !adapter_few_rows(rows, adapters) && adapters > 8; }
 struct AdapterPlan {
     int32_t row_tiles, slots, splits;
 };

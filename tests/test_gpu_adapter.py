@@ -170,6 +170,49 @@ def test_whole_columns(tbn, rank, wt, rows):
     run(tbn, make(rows, 512, 768, rank, 3, wt, BF, BF))
 
 
+@pytest.mark.parametrize("rank", [1, 7, 16, 32, 33, 64, 100, 128])
+@pytest.mark.parametrize("bank", [1, 3])
+def test_many_rows_of_every_rank(tbn, rank, bank):
+    # rows beyond those whose adapters are dealt over blocks; one adapter, and rows taken in the adapters' order
+    run(tbn, make(1030, 136, 72, rank, bank))
+
+
+@pytest.mark.parametrize("wt", [BF, F])
+@pytest.mark.parametrize("xt", [BF, F])
+@pytest.mark.parametrize("ot", [BF, F])
+@pytest.mark.parametrize("rank", [16, 40])
+def test_many_rows_of_every_type(tbn, wt, xt, ot, rank):
+    run(tbn, make(300, 256, 512, rank, 2, wt, xt, ot))
+    run(tbn, make(200, 168, 90, rank, 1, wt, xt, ot))
+
+
+@pytest.mark.parametrize("c,k", [(1, 1), (7, 3), (100, 257), (513, 72), (512, 1024)])
+@pytest.mark.parametrize("rows", [129, 192, 193, 321, 1025])
+def test_many_rows_of_every_size(tbn, c, k, rows):
+    run(tbn, make(rows, c, k, 5, 2))
+
+
+def test_scattered_long_batches(tbn):
+    # every row another adapter than its neighbours, some without one, adapters without rows
+    g = torch.Generator().manual_seed(4)
+    for rows, bank in ((1100, 17), (700, 2), (200, 1), (2100, 60)):
+        index = torch.randint(-2, bank + 2, (rows,), generator=g)
+        index[index == bank // 2] = -1
+        s = make(rows, 72, 136, 8, bank, index=index)
+        _, _, _, da, db = run(tbn, s)
+        assert not da[bank // 2].any() and not db[bank // 2].any()
+
+
+def test_bits_do_not_depend_on_the_neighbours(tbn):
+    # a row's results are those of its own values, wherever it lies in the batch and whatever lies beside it
+    s = make(1200, 264, 136, 12, 3)
+    d = gpu(s)
+    y, t = tbn.adapter_fwd(d["x"], d["index"], d["a"], d["b"], scale=d["scale"], residual=d["res_y"])
+    p = torch.randperm(1200, generator=torch.Generator().manual_seed(1)).cuda()
+    y2, t2 = tbn.adapter_fwd(d["x"][p], d["index"][p], d["a"], d["b"], scale=d["scale"], residual=d["res_y"][p])
+    assert torch.equal(y[p], y2) and torch.equal(t[p], t2)
+
+
 def test_repeatable(tbn):
     # the same bits from every call, ragged and whole (a wait too few would show here)
     for rank, c, k in ((100, 200, 136), (128, 512, 768), (65, 136, 200), (5, 72, 40)):
