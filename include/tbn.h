@@ -468,7 +468,7 @@ tbn_status tbn_softmax_xent(const float* logits, const int32_t* labels, int32_t 
  *   Given to tbn_conv2d_fwd as its epilogue's residual, y adds the adapters to the projection before the
  *   activation: act(alpha_k (x W~) + bias + y).
  * tbn_adapter_bwd:  dt = scale B^T dy, dx = residual + A^T dt (residual: the projection's own gradient, optional; it may be
- *   dx), da = sum over the adapter's rows of dt x, db = scale * sum of dy t, fp32, shaped as a and b and overwritten (zero
+ *   dx, which may not overlap x or dy: TBN_ERR_SHAPE), da = sum over the adapter's rows of dt x, db = scale * sum of dy t, fp32, shaped as a and b and overwritten (zero
  *   for an adapter without rows).  dy [rows][K] dtype dyt; dx and residual [rows][C] dtype dxt; t from the forward pass.
  *   dx, da and db are each optional; one has to be given.
  * Products are exact (of fp32 factors but for 2^-23 of them), sums and t are fp32 in a fixed order.  NaN and infinities reach

@@ -113,6 +113,13 @@ tbn_status check_ws(const void* ws, size_t bytes, int64_t need) {
     return TBN_OK;
 }
 
+int64_t size_of(tbn_dtype t) { return t == TBN_F32 ? 4 : 2; }
+
+bool meet(const void* p, int64_t bytes, const void* q, int64_t qbytes) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a < b + (uintptr_t)qbytes && b < a + (uintptr_t)bytes;
+}
+
 tbn::AdapterArgs adapter_args(const tbn_adapter_desc* d, const int32_t* index, tbn_dtype wt) {
     tbn::AdapterArgs a = {};
     a.index = index;
@@ -337,6 +344,10 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
     const AdapterWs w = adapter_ws(desc, true);
     st = check_ws(ws, ws_bytes, w.total);
     if (st != TBN_OK) return st;
+    const int64_t dx_bytes = desc->rows * desc->c * size_of(dxt);
+    if (dx && (meet(dx, dx_bytes, x, desc->rows * desc->c * size_of(xt)) ||
+               meet(dx, dx_bytes, dy, desc->rows * desc->k * size_of(dyt))))
+        return fail(TBN_ERR_SHAPE, "dx overlaps x or dy");
     char* base = reinterpret_cast<char*>(ws);
     float* part = reinterpret_cast<float*>(base);
     float* dt = reinterpret_cast<float*>(base + w.t_off);

@@ -375,7 +375,7 @@ struct AdamwBatch {
     int32_t rounds;  // of kAdamwRound elements that a block takes
 };
 static_assert(sizeof(AdamwBatch) <= 4096, "kernel arguments");
-constexpr int kAdamwRound = 1024, kAdamwRounds = 4;
+constexpr int kAdamwRound = 1024;
 hipError_t launch_adamw(const AdamwBatch& b, int64_t blocks, int g_bf16, int eight, hipStream_t stream);
 
 // Layer normalisation; partial: [2][layernorm_bwd_blocks][C] fp32, behind it for the longest rows two means a row:

@@ -4,7 +4,9 @@
 //   backward  xh = (x - mu) s, h = dy gamma,  dx = s (h - mean_c h - xh mean_c(h xh)),
 //             dgamma = sum_rows dy xh,  dbeta = sum_rows dy
 //
-// Bound by HBM: each tensor is read or written once.  A team of T threads (8 to 64 lanes of a wave, or a
+// Bound by HBM: each tensor is read or written once (rows beyond 16384 values are read twice backward).  Measured: forward 8192
+// rows of 8192 bf16 values 51 us (5.2 TB/s), one row of 512 2.3 us of kernel; backward 16384 rows of 4096 82 us (4.9 TB/s), of
+// which the last sums are 6; 777 rows of 1000 6 + 4 us, launch and one row's latency.  A team of T threads (8 to 64 lanes of a wave, or a
 // whole block) keeps a row in registers, NV pieces of 8 neighbouring values per thread, so that the centred
 // sum of squares is a second pass over registers.  Teams walk the rows with the stride of the grid and keep
 // what belongs to their columns in registers over all of them: gamma and beta, and in the backward pass the
@@ -554,7 +556,8 @@ int team_of(int32_t C) {
     return -1;
 }
 
-// The widest team only where its registers suffice: forward, rows of whole pieces.
+// The widest team only where its registers suffice: forward, rows of whole pieces (2048 rows of 32768 67 us, the long
+// kernel, which reads them again from the caches, for the others).
 int fwd_team(int32_t C) {
     const int team = team_of(C);
     return team == kNumTeams - 1 && C % 8 ? -1 : team;

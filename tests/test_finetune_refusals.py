@@ -99,6 +99,22 @@ def test_adapters():
     assert bwd(ws=None) == WORKSPACE and bwd(bytes=sizes[1] - 1) == WORKSPACE
 
 
+def test_adapters_backward_over_its_inputs():
+    # dx over the whole of x or dy, or over their last value alone: 1000 x 4096 and 1000 x 512 of bf16, 512 of fp32
+    d = _desc(rows=1000, c=4096, k=512)
+    n = tbn.adapter_workspace_size(tbn.OP_BWD_DATA, d)
+    x, dy = 0x10000000, 0x20000000
+
+    def bwd(dx, dyt=0):
+        return tbn.load().tbn_adapter_bwd(ctypes.byref(d), x, 0, dy, dyt, GOOD, GOOD, GOOD, 0, None, GOOD, None, dx, 0, GOOD, GOOD,
+                                          GOOD, n, None)
+
+    assert bwd(x) == bwd(dy) == bwd(x - 16) == bwd(dy + 16) == SHAPE
+    assert bwd(x + 1000 * 4096 * 2 - 16) == bwd(x - 1000 * 4096 * 2 + 16) == SHAPE
+    assert bwd(dy + 1000 * 512 * 2 - 16) == bwd(dy + 1000 * 512 * 4 - 16, dyt=1) == SHAPE
+    assert bwd(dy + 1000 * 512 * 2 + 16, dyt=1) == SHAPE
+
+
 # ---- the Python calls, on host tensors (whose device is refused last) and on the GPU's (the native code declines) ----
 def _calls(dev):
     bf = torch.bfloat16
