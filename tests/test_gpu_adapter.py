@@ -326,3 +326,31 @@ def test_other_stream_and_captured(tbn):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(out, step()))
+
+
+@pytest.mark.parametrize("rows,bank", [(300, 1), (1500, 12), (40, 12)])
+def test_in_place_and_captured_at_every_length(tbn, rows, bank):
+    # residuals overwritten by the results, by few rows, by rows as they lie and by sorted ones; replays with other adapters
+    s = make(rows, 256, 192, 8, bank)
+    d = gpu(s)
+
+    def step(y, dx):
+        _, t = tbn.adapter_fwd(d["x"], d["index"], d["a"], d["b"], scale=d["scale"], residual=y, y=y)
+        dx, da, db = tbn.adapter_bwd(d["x"], d["dy"], d["index"], d["a"], d["b"], t, scale=d["scale"], residual=dx)
+        return y, t, dx, da, db
+
+    apart = lambda: tbn.adapter_fwd(d["x"], d["index"], d["a"], d["b"], scale=d["scale"], residual=d["res_y"])  # noqa: E731
+    assert torch.equal(apart()[0], step(d["res_y"].clone(), d["res_x"])[0])
+    y = d["res_y"].clone()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = step(y, d["res_x"])
+    for seed in (1, 2, 3):
+        new = make(rows, 256, 192, 8, bank, seed=seed)
+        d["x"].copy_(new["x"])
+        d["index"].copy_(torch.flip(new["index"], [0]) if seed == 2 else new["index"])
+        y.copy_(d["res_y"])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, step(d["res_y"].clone(), d["res_x"])))
