@@ -974,7 +974,9 @@ void outer(const AdapterOuter& o, int32_t S, int32_t splits, hipStream_t s) {
 
 AdapterPlan plan_adapter_shrink(int64_t rows, int32_t C, int32_t R, int32_t S) {
     AdapterPlan p;
-    const bool few = adapter_few_rows(rows, S);
+    // Tiles of 16 rows also where a small bank's rows are expanded 128 at a time: 100 rows of 1000 values, rank 8, 5.7 us instead
+    // of 7.1; 128 of 8192, rank 64, 6.1 instead of 7.3 (512 of 8192, one adapter of rank 16, 9 instead of 7).
+    const bool few = rows <= 128 || adapter_few_rows(rows, S);
     p.row_tiles = few ? 1 : R <= 32 ? 4 : 2;
     p.slots = few ? (S < 16 ? S : 16) : 1;
     if (p.slots > rows) p.slots = (int32_t)rows;

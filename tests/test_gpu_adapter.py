@@ -192,6 +192,13 @@ def test_many_rows_of_every_size(tbn, c, k, rows):
     run(tbn, make(rows, c, k, 5, 2))
 
 
+@pytest.mark.parametrize("rows", [65, 100, 128])
+@pytest.mark.parametrize("c,k,rank", [(512, 1000, 8), (2056, 1032, 20), (72, 3000, 70)])
+def test_one_adapter(tbn, rows, c, k, rank):
+    # small tiles on the way in, 128 rows at once on the way out
+    run(tbn, make(rows, c, k, rank, 1, F, BF, BF))
+
+
 def test_scattered_long_batches(tbn):
     # every row another adapter than its neighbours, some without one, adapters without rows
     g = torch.Generator().manual_seed(4)
