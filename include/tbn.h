@@ -346,8 +346,8 @@ tbn_status tbn_sgd_step_quantize(float* w, float* v, const float* g, int64_t k, 
  *            and lr by values in device memory, read when the kernel runs (for captured steps, which the
  *            caller advances between replays); *step_dev >= 1 is the caller's to keep.
  * w, m, v and the scales need no alignment beyond their elements' (views into flat buffers); 16-byte aligned
- * ones are faster.  No two of the written arrays may overlap (TBN_ERR_SHAPE): among them is a tensor listed twice;
- * nor may g overlap them.
+ * ones are faster.  No two of the written arrays may overlap (among them is a tensor listed twice), nor may any g
+ * overlap one of them: TBN_ERR_SHAPE.
  */
 typedef enum tbn_state { TBN_STATE_F32 = 0, TBN_STATE_E4M3 = 1 } tbn_state;
 

@@ -37,22 +37,28 @@ struct Span {
     bool operator<(const Span& o) const { return begin < o.begin; }
 };
 
-bool overlap(const tbn_adamw_tensor* t, int32_t n, bool eight) {
+// Whether arrays that are written overlap one another, or a gradient one of them.
+bool overlap(const tbn_adamw_tensor* t, int32_t n, bool eight, int64_t g_size) {
     std::vector<Span> s;
     s.reserve((size_t)n * (eight ? 5 : 3));
-    auto add = [&](const void* p, int64_t bytes) {
-        s.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes});
+    auto span = [](const void* p, int64_t bytes) {
+        return Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes};
     };
-    for (int32_t i = 0; i < n; ++i) add(t[i].w, t[i].count * 4);
-    for (int32_t i = 0; i < n; ++i) add(t[i].m, t[i].count * (eight ? 1 : 4));
-    for (int32_t i = 0; i < n; ++i) add(t[i].v, t[i].count * (eight ? 1 : 4));
+    for (int32_t i = 0; i < n; ++i) s.push_back(span(t[i].w, t[i].count * 4));
+    for (int32_t i = 0; i < n; ++i) s.push_back(span(t[i].m, t[i].count * (eight ? 1 : 4)));
+    for (int32_t i = 0; i < n; ++i) s.push_back(span(t[i].v, t[i].count * (eight ? 1 : 4)));
     for (int32_t i = 0; eight && i < n; ++i) {
-        add(t[i].m_scale, (t[i].count + 255) / 256 * 4);
-        add(t[i].v_scale, (t[i].count + 255) / 256 * 4);
+        s.push_back(span(t[i].m_scale, (t[i].count + 255) / 256 * 4));
+        s.push_back(span(t[i].v_scale, (t[i].count + 255) / 256 * 4));
     }
     std::sort(s.begin(), s.end());
     for (size_t i = 1; i < s.size(); ++i)
         if (s[i].begin < s[i - 1].end) return true;
+    for (int32_t i = 0; i < n; ++i) {  // s is in order and apart: the last one that begins before the gradient's end
+        const Span g = span(t[i].g, t[i].count * g_size);
+        const auto next = std::lower_bound(s.begin(), s.end(), Span{g.end, 0});
+        if (next != s.begin() && g.begin < (next - 1)->end) return true;
+    }
     return false;
 }
 
@@ -220,7 +226,8 @@ tbn_status tbn_adamw_step(const tbn_adamw_tensor* tensors, int32_t n, tbn_state 
             (eight && (!aligned(t.m_scale, 4) || !aligned(t.v_scale, 4))))
             return fail(TBN_ERR_ALIGN, "misaligned pointer");
     }
-    if (overlap(tensors, n, eight)) return fail(TBN_ERR_SHAPE, "arrays that are written overlap (or a tensor is listed twice)");
+    if (overlap(tensors, n, eight, gt == TBN_F32 ? 4 : 2))
+        return fail(TBN_ERR_SHAPE, "arrays that are written overlap (or a tensor is listed twice), or a gradient overlaps one");
 
     tbn::AdamwBatch b = {};
     b.step = (uint32_t)h->step;

@@ -207,3 +207,20 @@ def test_python_refusals_of_gpu_tensors():
         tbn.adamw_step([x], [x.clone()], [x.clone()], [x], 0)
     with pytest.raises(tbn.TbnError, match="workspace too small"):
         tbn.layernorm_bwd(x, x, i.float(), i.float(), ws=torch.empty(8, device="cuda"))
+
+
+# ---- operands that overlap: refused before anything is launched (each call here differs from an accepted one in this alone) ----
+def test_adamw_gradients_over_what_is_written():
+    # 1000 elements: w, fp32 states and gradients of 4000 bytes each, codes of 1000 and scales of 16
+    w, m, v = 0x100000, 0x200000, 0x300000
+    kw = dict(count=1000, gt=1, w=w, m=m, v=v)
+    for p, size in ((w, 4000), (m, 4000), (v, 4000)):
+        assert _adamw(g=p, **kw) == _adamw(g=p + size - 4, **kw) == _adamw(g=p - 4000 + 4, **kw) == SHAPE
+    # bf16 gradients end after 2000 bytes
+    bf16 = dict(kw, gt=0)
+    assert _adamw(g=w - 2000 + 4, **bf16) == _adamw(g=w + 3996, **bf16) == SHAPE
+    eight = dict(kw, state=1, ms=0x500000, vs=0x600000)
+    for p, size in ((w, 4000), (m, 1000), (v, 1000), (0x500000, 16), (0x600000, 16)):
+        assert _adamw(g=p, **eight) == _adamw(g=p + size - 4, **eight) == _adamw(g=p - 4000 + 4, **eight) == SHAPE
+    # the gradients of one tensor over another's w
+    assert _adamw(n=3, g=w + 2 * 0x1000 + 8, **kw) == SHAPE
