@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -23,6 +24,33 @@ tbn_status done(hipError_t e, const char* where) {
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 bool known(tbn_dtype t) { return t == TBN_BF16 || t == TBN_F32; }
 int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
+int64_t size_of(tbn_dtype t) { return t == TBN_F32 ? 4 : 2; }
+
+tbn_status check_ws(const void* ws, size_t bytes, int64_t need) {
+    if (!ws || bytes < (size_t)need) return fail(TBN_ERR_WORKSPACE, "workspace too small");
+    if (!aligned(ws, 16)) return fail(TBN_ERR_ALIGN, "workspace must be 16-byte aligned");
+    return TBN_OK;
+}
+
+// Whether an output shares a byte with an input or with another output (operands that are not given are NULL).
+struct Operand {
+    const void* p;
+    int64_t bytes;
+};
+bool meet(const void* p, int64_t bytes, const void* q, int64_t qbytes) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a < b + (uintptr_t)qbytes && b < a + (uintptr_t)bytes;
+}
+bool overlap(std::initializer_list<Operand> outputs, std::initializer_list<Operand> inputs) {
+    for (const Operand* o = outputs.begin(); o != outputs.end(); ++o) {
+        if (!o->p) continue;
+        for (const Operand& i : inputs)
+            if (i.p && meet(o->p, o->bytes, i.p, i.bytes)) return true;
+        for (const Operand* k = outputs.begin(); k != o; ++k)
+            if (k->p && meet(o->p, o->bytes, k->p, k->bytes)) return true;
+    }
+    return false;
+}
 
 // ---- layer normalisation -----------------------------------------------------------------
 tbn_status check_ln(int64_t rows, int32_t c) {
@@ -113,19 +141,6 @@ bool expand_sums(int32_t splits, const tbn_adapter_desc* d) {
     return splits > 1 && tbn::adapter_few_rows(d->rows, d->adapters);
 }
 
-tbn_status check_ws(const void* ws, size_t bytes, int64_t need) {
-    if (!ws || bytes < (size_t)need) return fail(TBN_ERR_WORKSPACE, "workspace too small");
-    if (!aligned(ws, 16)) return fail(TBN_ERR_ALIGN, "workspace must be 16-byte aligned");
-    return TBN_OK;
-}
-
-int64_t size_of(tbn_dtype t) { return t == TBN_F32 ? 4 : 2; }
-
-bool meet(const void* p, int64_t bytes, const void* q, int64_t qbytes) {
-    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-    return a < b + (uintptr_t)qbytes && b < a + (uintptr_t)bytes;
-}
-
 tbn::AdapterArgs adapter_args(const tbn_adapter_desc* d, const int32_t* index, tbn_dtype wt) {
     tbn::AdapterArgs a = {};
     a.index = index;
@@ -150,6 +165,10 @@ tbn_status tbn_layernorm_fwd(const void* x, tbn_dtype xt, int64_t rows, int32_t 
     if (!aligned(x, 16) || !aligned(y, 16) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) ||
         !aligned(inv_std, 4))
         return fail(TBN_ERR_ALIGN, "misaligned pointer");
+    const int64_t stats = rows * 4, params = (int64_t)c * 4;
+    if (overlap({{y, rows * c * size_of(yt)}, {mean, stats}, {inv_std, stats}},
+                {{x, rows * c * size_of(xt)}, {gamma, params}, {beta, params}}))
+        return fail(TBN_ERR_SHAPE, "an output overlaps an input or another output");
     tbn::LnArgs a = {};
     a.x = x;
     a.y = y;
@@ -186,6 +205,10 @@ tbn_status tbn_layernorm_bwd(const void* x, tbn_dtype xt, const void* dy, tbn_dt
         return fail(TBN_ERR_ALIGN, "misaligned pointer");
     st = check_ws(ws, ws_bytes, (int64_t)need);
     if (st != TBN_OK) return st;
+    const int64_t x_bytes = rows * c * size_of(xt), stats = rows * 4, params = (int64_t)c * 4;
+    if (overlap({{dx, x_bytes}, {dgamma, params}, {dbeta, params}, {ws, (int64_t)need}},
+                {{x, x_bytes}, {dy, rows * c * size_of(yt)}, {mean, stats}, {inv_std, stats}, {gamma, params}}))
+        return fail(TBN_ERR_SHAPE, "an output or the workspace overlaps another operand");
     tbn::LnArgs a = {};
     a.x = x;
     a.dy = dy;

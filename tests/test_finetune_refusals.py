@@ -224,3 +224,37 @@ def test_adamw_gradients_over_what_is_written():
         assert _adamw(g=p, **eight) == _adamw(g=p + size - 4, **eight) == _adamw(g=p - 4000 + 4, **eight) == SHAPE
     # the gradients of one tensor over another's w
     assert _adamw(n=3, g=w + 2 * 0x1000 + 8, **kw) == SHAPE
+
+
+def _apart(f, places, sizes, outputs, may_meet=()):
+    """f(place of every operand) with one output's first, last or whole bytes over another operand: SHAPE, for each pair but those."""
+    for out in outputs:
+        for other in places:
+            if other == out or (out, other) in may_meet or (other, out) in may_meet:
+                continue
+            at = places[other]
+            for p in (at, at - sizes[out] + 16, at + (sizes[other] - 1) // 16 * 16):
+                print(out, "over", other, flush=True)
+                assert f(**dict(places, **{out: p})) == SHAPE, (out, other, hex(p))
+
+
+def _places(**sizes):
+    return {name: 0x10000000 * (i + 1) for i, name in enumerate(sizes)}, sizes
+
+
+def test_layernorm_outputs_over_operands():
+    # 50 rows of 72: x bf16, y and dy fp32 (and the other way round), 4 bytes a row or column of the statistics and parameters
+    lib, rows, c = tbn.load(), 50, 72
+    n = rows * c
+
+    def fwd(x, y, gamma, beta, mean, inv_std):
+        return lib.tbn_layernorm_fwd(x, 0, rows, c, gamma, beta, ctypes.c_float(1e-5), y, 1, mean, inv_std, None)
+
+    _apart(fwd, *_places(x=2 * n, y=4 * n, gamma=4 * c, beta=4 * c, mean=4 * rows, inv_std=4 * rows), ("y", "mean", "inv_std"))
+    need = tbn.layernorm_workspace_size(rows, c)
+
+    def bwd(x, dy, mean, inv_std, gamma, dx, dgamma, dbeta, ws):
+        return lib.tbn_layernorm_bwd(x, 1, dy, 0, rows, c, mean, inv_std, gamma, dx, dgamma, dbeta, ws, need, None)
+
+    _apart(bwd, *_places(x=4 * n, dy=2 * n, mean=4 * rows, inv_std=4 * rows, gamma=4 * c, dx=4 * n, dgamma=4 * c, dbeta=4 * c, ws=need),
+           ("dx", "dgamma", "dbeta", "ws"))
