@@ -427,8 +427,9 @@ tbn_status tbn_batchnorm_train_bwd(const void* x, const void* y, const void* dy,
                                    float* dgamma, float* dbeta, void* dx, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* Layer normalisation of `rows` rows of c values: y = (x - mean) inv_std gamma + beta with the row's mean and
- * inv_std = 1/sqrt(biased var + eps), all in fp32.  x has dtype xt, y yt; gamma and beta [c] are optional (1 and
- * 0), and so are the outputs mean and inv_std [rows], which the backward pass takes.  rows * c at most 2^40.
+ * inv_std = 1/sqrt(biased var + eps), all in fp32; eps finite and >= 0 (TBN_ERR_SHAPE).  x has dtype xt, y yt; gamma and
+ * beta [c] are optional (1 and 0), and so are the outputs mean and inv_std [rows], which the backward pass takes.
+ * rows * c at most 2^40.
  * An output may not overlap an input or another output, here and in the backward pass, where the same holds for ws:
  * TBN_ERR_SHAPE. */
 tbn_status tbn_layernorm_fwd(const void* x, tbn_dtype xt, int64_t rows, int32_t c, const float* gamma,

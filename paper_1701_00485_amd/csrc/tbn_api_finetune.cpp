@@ -162,6 +162,7 @@ tbn_status tbn_layernorm_fwd(const void* x, tbn_dtype xt, int64_t rows, int32_t 
     tbn_status st = check_ln(rows, c);
     if (st != TBN_OK) return st;
     if (!known(xt) || !known(yt)) return fail(TBN_ERR_UNSUPPORTED, "unknown dtype");
+    if (!(eps >= 0) || !std::isfinite(eps)) return fail(TBN_ERR_SHAPE, "eps has to be finite and not negative");
     if (!aligned(x, 16) || !aligned(y, 16) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) ||
         !aligned(inv_std, 4))
         return fail(TBN_ERR_ALIGN, "misaligned pointer");

@@ -258,3 +258,10 @@ def test_layernorm_outputs_over_operands():
 
     _apart(bwd, *_places(x=4 * n, dy=2 * n, mean=4 * rows, inv_std=4 * rows, gamma=4 * c, dx=4 * n, dgamma=4 * c, dbeta=4 * c, ws=need),
            ("dx", "dgamma", "dbeta", "ws"))
+
+
+def test_layernorm_eps():
+    # below zero a row of little variance has no root; NaN and infinity leave no value at all
+    x, y = ctypes.c_void_p(0x100000), ctypes.c_void_p(0x200000)
+    for eps in (-1e-5, -1e-30, float("nan"), float("inf"), float("-inf")):
+        assert tbn.load().tbn_layernorm_fwd(x, 0, 4, 8, None, None, ctypes.c_float(eps), y, 0, None, None, None) == SHAPE, eps
