@@ -470,12 +470,12 @@ tbn_status tbn_softmax_xent(const float* logits, const int32_t* labels, int32_t 
  *   Given to tbn_conv2d_fwd as its epilogue's residual, y adds the adapters to the projection before the
  *   activation: act(alpha_k (x W~) + bias + y).
  * tbn_adapter_bwd:  dt = scale B^T dy, dx = residual + A^T dt (residual: the projection's own gradient, optional; it may be
- *   dx, which may not overlap x or dy: TBN_ERR_SHAPE), da = sum over the adapter's rows of dt x, db = scale * sum of dy t, fp32, shaped as a and b and overwritten (zero
+ *   dx), da = sum over the adapter's rows of dt x, db = scale * sum of dy t, fp32, shaped as a and b and overwritten (zero
  *   for an adapter without rows).  dy [rows][K] dtype dyt; dx and residual [rows][C] dtype dxt; t from the forward pass.
  *   dx, da and db are each optional; one has to be given.
  * Products are exact (of fp32 factors but for 2^-23 of them), sums and t are fp32 in a fixed order.  NaN and infinities reach
  * their own row and adapter alone; an fp32 factor that is infinite, or rounds to infinity as bf16, gives NaN.
- * Outputs may not overlap inputs but where said above.
+ * But for a residual that is y (dx) itself, an output or ws may not overlap an input or another output: TBN_ERR_SHAPE.
  * ws: tbn_adapter_workspace_size bytes for TBN_OP_FWD (forward) or TBN_OP_BWD_DATA (backward).
  * Limits: rows <= 2^27, C and K <= 2^24, rows C and rows K <= 2^35, S R C and S R K < 2^31 (TBN_ERR_SHAPE).
  */

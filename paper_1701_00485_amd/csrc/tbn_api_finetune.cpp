@@ -136,6 +136,15 @@ AdapterWs adapter_ws(const tbn_adapter_desc* d, bool backward) {
     return w;
 }
 
+// Sizes of the operands: values of x and of y, of a bank's a and b; bytes of the others.
+struct AdapterBytes {
+    int64_t rc, rk, rank_c, rank_k, t, index, scale, a, b;
+    AdapterBytes(const tbn_adapter_desc* d, tbn_dtype wt)
+        : rc(d->rows * d->c), rk(d->rows * d->k), rank_c((int64_t)d->adapters * d->rank * d->c),
+          rank_k((int64_t)d->adapters * d->rank * d->k), t(d->rows * d->rank * 4), index(d->rows * 4), scale((int64_t)d->adapters * 4),
+          a(rank_c * size_of(wt)), b(rank_k * size_of(wt)) {}
+};
+
 // Whether the expanding kernel adds the partial sums itself, which saves few rows a launch of 2 us.
 bool expand_sums(int32_t splits, const tbn_adapter_desc* d) {
     return splits > 1 && tbn::adapter_few_rows(d->rows, d->adapters);
@@ -319,6 +328,11 @@ tbn_status tbn_adapter_fwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
     const AdapterWs w = adapter_ws(desc, false);
     st = check_ws(ws, ws_bytes, w.total);
     if (st != TBN_OK) return st;
+    const AdapterBytes n(desc, wt);
+    const int64_t y_bytes = n.rk * size_of(yt);
+    if (overlap({{y, y_bytes}, {t, n.t}, {ws, w.total}}, {{x, n.rc * size_of(xt)}, {index, n.index}, {a, n.a}, {b, n.b}, {scale, n.scale},
+                                                           {residual == y ? nullptr : residual, y_bytes}}))
+        return fail(TBN_ERR_SHAPE, "an output or the workspace overlaps another operand");
     float* part = reinterpret_cast<float*>(ws);
     float* sum = t ? t : reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + w.t_off);
 
@@ -377,10 +391,12 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
     const AdapterWs w = adapter_ws(desc, true);
     st = check_ws(ws, ws_bytes, w.total);
     if (st != TBN_OK) return st;
-    const int64_t dx_bytes = desc->rows * desc->c * size_of(dxt);
-    if (dx && (meet(dx, dx_bytes, x, desc->rows * desc->c * size_of(xt)) ||
-               meet(dx, dx_bytes, dy, desc->rows * desc->k * size_of(dyt))))
-        return fail(TBN_ERR_SHAPE, "dx overlaps x or dy");
+    const AdapterBytes n(desc, wt);
+    const int64_t dx_bytes = n.rc * size_of(dxt);
+    if (overlap({{dx, dx_bytes}, {da, n.rank_c * 4}, {db, n.rank_k * 4}, {ws, w.total}},
+                {{x, n.rc * size_of(xt)}, {dy, n.rk * size_of(dyt)}, {index, n.index}, {a, n.a}, {b, n.b}, {scale, n.scale}, {t, n.t},
+                 {residual == dx || !dx ? nullptr : residual, dx_bytes}}))
+        return fail(TBN_ERR_SHAPE, "an output or the workspace overlaps another operand");
     char* base = reinterpret_cast<char*>(ws);
     float* part = reinterpret_cast<float*>(base);
     float* dt = reinterpret_cast<float*>(base + w.t_off);
@@ -433,8 +449,7 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
         if (st != TBN_OK || (!da && !db)) return st;
     }
 
-    const int64_t na = da ? (int64_t)desc->adapters * desc->rank * desc->c : 0;
-    const int64_t nb = db ? (int64_t)desc->adapters * desc->rank * desc->k : 0;
+    const int64_t na = da ? n.rank_c : 0, nb = db ? n.rank_k : 0;
     float* grads = reinterpret_cast<float*>(base + w.grad_off);
     const bool split = w.grad_splits > 1;
     tbn::AdapterOuterJob jobs[2] = {{x, dt, nullptr, split ? grads : da, desc->c, 0},

@@ -265,3 +265,29 @@ def test_layernorm_eps():
     x, y = ctypes.c_void_p(0x100000), ctypes.c_void_p(0x200000)
     for eps in (-1e-5, -1e-30, float("nan"), float("inf"), float("-inf")):
         assert tbn.load().tbn_layernorm_fwd(x, 0, 4, 8, None, None, ctypes.c_float(eps), y, 0, None, None, None) == SHAPE, eps
+
+
+def test_adapter_outputs_over_operands():
+    # 96 rows, 64 -> 48, 3 adapters of rank 8: x fp32, dy and y bf16, adapters fp32.  A residual may be y (dx) itself, nothing
+    # that lies across it
+    lib, d = tbn.load(), _desc(rows=96, c=64, k=48, rank=8)
+    rc, rk, rr = 96 * 64, 96 * 48, 96 * 8
+    need = [tbn.adapter_workspace_size(op, d) for op in (tbn.OP_FWD, tbn.OP_BWD_DATA)]
+
+    def fwd(x, index, a, b, scale, residual, y, t, ws):
+        return lib.tbn_adapter_fwd(ctypes.byref(d), x, 1, index, a, b, 1, scale, residual, y, 0, t, ws, need[0], None)
+
+    places, sizes = _places(x=4 * rc, index=4 * 96, a=3 * 8 * 64 * 4, b=3 * 8 * 48 * 4, scale=12, residual=2 * rk, y=2 * rk, t=4 * rr,
+                            ws=need[0])
+    _apart(fwd, places, sizes, ("y", "t", "ws"), {("y", "residual")})
+    for p in (16, -16, 2 * rk - 16, 16 - 2 * rk):
+        assert fwd(**dict(places, residual=places["y"] + p)) == SHAPE
+
+    def bwd(x, dy, index, a, b, scale, t, residual, dx, da, db, ws):
+        return lib.tbn_adapter_bwd(ctypes.byref(d), x, 1, dy, 0, index, a, b, 1, scale, t, residual, dx, 0, da, db, ws, need[1], None)
+
+    places, sizes = _places(x=4 * rc, dy=2 * rk, index=4 * 96, a=3 * 8 * 64 * 4, b=3 * 8 * 48 * 4, scale=12, t=4 * rr, residual=2 * rc,
+                            dx=2 * rc, da=3 * 8 * 64 * 4, db=3 * 8 * 48 * 4, ws=need[1])
+    _apart(bwd, places, sizes, ("dx", "da", "db", "ws"), {("dx", "residual")})
+    for p in (16, -16, 2 * rc - 16, 16 - 2 * rc):
+        assert bwd(**dict(places, residual=places["dx"] + p)) == SHAPE
