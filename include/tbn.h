@@ -478,6 +478,9 @@ tbn_status tbn_softmax_xent(const float* logits, const int32_t* labels, int32_t 
  * But for a residual that is y (dx) itself, an output or ws may not overlap an input or another output: TBN_ERR_SHAPE.
  * ws: tbn_adapter_workspace_size bytes for TBN_OP_FWD (forward) or TBN_OP_BWD_DATA (backward).
  * Limits: rows <= 2^27, C and K <= 2^24, rows C and rows K <= 2^35, S R C and S R K < 2^31 (TBN_ERR_SHAPE).
+ * rows S <= 2^38 (TBN_ERR_UNSUPPORTED): the backward pass, and the forward pass of large batches over more than 8
+ * adapters, order the rows in a time that grows with rows S (7 us for 5000 rows and 64 adapters, 660 for 131072 and 4096,
+ * 20 ms for 2^20 and 2^14).
  */
 typedef struct tbn_adapter_desc {
     int64_t rows;

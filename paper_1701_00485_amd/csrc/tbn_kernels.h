@@ -441,9 +441,11 @@ struct AdapterOuter {
 // 8 35 (39), of one 31 (30).  In a small bank fewer adapters meet in a tile: 100 rows of one adapter, 512 -> 1000 backward,
 // 17.2 us against 14.9 in turn.
 inline bool adapter_few_rows(int64_t rows, int32_t adapters) { return rows <= 1024 && rows <= 64 * (int64_t)adapters; }
-// Whether the other batches are taken in the order of their adapters, which costs a launch (7 us) and, where rows lie by
-// chance, saves a pass for every further adapter of a tile.  5000 rows, 4096 -> 4096, rank 32: each row one of 64 adapters 77 us
+// Whether the other batches are taken in the order of their adapters, which costs a launch and, where rows lie by chance,
+// saves a pass for every further adapter of a tile.  5000 rows, 4096 -> 4096, rank 32: each row one of 64 adapters 77 us
 // (as they lie 590), of 9 62; 11 prompts 58 to 61 (50).  A small bank's rows are taken as they lie: of 8 adapters by chance 137 us.
+// The launch takes 7 us for a few thousand rows and tens of adapters; a block an adapter, each reading the whole index, it grows
+// with rows times adapters: 8192 rows and 64 adapters 7, 32768 and 4096 175, 131072 and 4096 656, 2^20 and 2^14 20 ms.
 inline bool adapter_sorted_rows(int64_t rows, int32_t adapters) { return !adapter_few_rows(rows, adapters) && adapters > 8; }
 struct AdapterPlan {
     int32_t row_tiles, slots, splits;

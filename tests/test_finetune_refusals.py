@@ -291,3 +291,14 @@ def test_adapter_outputs_over_operands():
     _apart(bwd, places, sizes, ("dx", "da", "db", "ws"), {("dx", "residual")})
     for p in (16, -16, 2 * rc - 16, 16 - 2 * rc):
         assert bwd(**dict(places, residual=places["dx"] + p)) == SHAPE
+
+
+def test_adapter_rows_times_adapters():
+    # rows times adapters beyond 2^38, which the ordering of the rows by adapter grows with; 2^38 itself is taken
+    b = ctypes.c_size_t()
+    f = tbn.load().tbn_adapter_workspace_size
+    for rows, adapters, want in ((1 << 27, 2048, 0), ((1 << 27) - 2047, 2049, UNSUPPORTED), (1 << 27, 65535, UNSUPPORTED),
+                                 (1 << 22, 65535, 0), ((1 << 22) + 66, 65535, UNSUPPORTED), (1 << 27, 1, 0)):
+        for op in (tbn.OP_FWD, tbn.OP_BWD_DATA):
+            d = _desc(rows=rows, c=16, k=16, rank=1, adapters=adapters)
+            assert f(op, ctypes.byref(d), ctypes.byref(b)) == want, (rows, adapters)
