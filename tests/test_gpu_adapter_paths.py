@@ -1,0 +1,55 @@
+"""Low-rank adapters on the paths that a batch's length, its bank and its widths choose, against the formulas in 64 bits: rows taken in
+the order of their adapters (more than 8 adapters, more than 1024 rows) at every rank and type and with several splits, and the
+widest tiles of the expansion.
+
+test_gpu_adapter.py has the tolerances of the long sums; its batches over banks of 1 to 3 are taken as they lie.
+"""
+import pytest
+import torch
+
+import test_gpu_adapter as base
+from test_gpu_adapter import BF, F
+
+pytestmark = pytest.mark.gpu
+
+
+def scattered(rows, bank, seed=0):
+    """Each row an adapter by chance, some none, one adapter (bank // 2) without rows."""
+    index = torch.randint(-2, bank + 2, (rows,), generator=torch.Generator().manual_seed(seed))
+    index[index == bank // 2] = -1
+    return index
+
+
+def run_sorted(tbn, rows, c, k, rank, bank, wt=BF, xt=BF, ot=BF):
+    s = base.make(rows, c, k, rank, bank, wt, xt, ot, index=scattered(rows, bank, rank))
+    _, _, _, da, db = base.run(tbn, s)
+    assert not da[bank // 2].any() and not db[bank // 2].any()
+
+
+@pytest.mark.parametrize("rank", [1, 7, 16, 17, 32, 33, 64, 65, 100, 128])
+@pytest.mark.parametrize("wt", [BF, F])
+def test_sorted_rows_of_every_rank(tbn, rank, wt):
+    run_sorted(tbn, 1030, 136, 72, rank, 12, wt)
+
+
+@pytest.mark.parametrize("wt", [BF, F])
+@pytest.mark.parametrize("xt", [BF, F])
+@pytest.mark.parametrize("ot", [BF, F])
+@pytest.mark.parametrize("rank", [16, 32, 40])
+def test_sorted_rows_of_every_type(tbn, wt, xt, ot, rank):
+    run_sorted(tbn, 1100, 168, 90, rank, 17, wt, xt, ot)
+
+
+@pytest.mark.parametrize("rank,wt,xt", [(16, BF, BF), (32, F, BF), (40, BF, F), (64, F, F), (72, BF, BF), (128, F, BF)])
+def test_sorted_rows_with_splits(tbn, rank, wt, xt):
+    # both long sums split over blocks (512 values a block at least), the widths ragged and whole
+    run_sorted(tbn, 1030, 2056, 2560, rank, 12, wt, xt)
+
+
+@pytest.mark.parametrize("rank", [8, 40])
+@pytest.mark.parametrize("wt", [BF, F])
+@pytest.mark.parametrize("bank,c,k", [(1, 7304, 7424), (12, 7424, 7304)])
+def test_widest_tiles(tbn, rank, wt, bank, c, k):
+    # 9 tiles of 128 rows times 115 or 116 groups of 64 columns, from 1024 on: 256 columns a block up to rank 32, 128 up to 64
+    index = scattered(1030, bank, rank) if bank > 1 else None  # runs of rows with and without the one adapter
+    base.run(tbn, base.make(1030, c, k, rank, bank, wt, index=index))
