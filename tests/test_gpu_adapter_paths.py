@@ -1,6 +1,6 @@
 """Low-rank adapters on the paths that a batch's length, its bank and its widths choose, against the formulas in 64 bits: rows taken in
-the order of their adapters (more than 8 adapters, more than 1024 rows) at every rank and type and with several splits, and the
-widest tiles of the expansion.
+the order of their adapters (more than 8 adapters, more than 1024 rows) at every rank and type and with several splits, the
+widest tiles of the expansion, and few rows at high ranks for equal bits.
 
 test_gpu_adapter.py has the tolerances of the long sums; its batches over banks of 1 to 3 are taken as they lie.
 """
@@ -53,3 +53,20 @@ def test_widest_tiles(tbn, rank, wt, bank, c, k):
     # 9 tiles of 128 rows times 115 or 116 groups of 64 columns, from 1024 on: 256 columns a block up to rank 32, 128 up to 64
     index = scattered(1030, bank, rank) if bank > 1 else None  # runs of rows with and without the one adapter
     base.run(tbn, base.make(1030, c, k, rank, bank, wt, index=index))
+
+
+@pytest.mark.parametrize("rank", [65, 96, 97, 100, 127, 128])
+@pytest.mark.parametrize("wt", [BF, F])
+@pytest.mark.parametrize("xt,ot", [(BF, BF), (F, F)])
+def test_few_rows_of_high_ranks_repeat(tbn, rank, wt, xt, ot):
+    # right, and the same bits from every call, with other work on the card between them
+    for rows, c, k in ((5, 200, 136), (40, 513, 72), (90, 136, 1001), (48, 512, 768)):
+        s = base.make(rows, c, k, rank, 5, wt, xt, ot, index=scattered(rows, 5, rows))
+        d = base.gpu(s)
+        first = base.run(tbn, s)
+        for n in range(6):
+            torch.randn(1000 * (n + 1), device="cuda").sort()
+            y, t = tbn.adapter_fwd(d["x"], d["index"], d["a"], d["b"], scale=d["scale"], residual=d["res_y"], out_dtype=ot)
+            out = (y, t) + tbn.adapter_bwd(d["x"], d["dy"], d["index"], d["a"], d["b"], t, scale=d["scale"], residual=d["res_x"],
+                                           out_dtype=ot)
+            assert all(torch.equal(p, q) for p, q in zip(first, out)), (rows, c, k, n)
