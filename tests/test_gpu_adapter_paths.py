@@ -1,6 +1,7 @@
 """Low-rank adapters on the paths that a batch's length, its bank and its widths choose, against the formulas in 64 bits: rows taken in
 the order of their adapters (more than 8 adapters, more than 1024 rows) at every rank and type and with several splits, the
-widest tiles of the expansion, and few rows at high ranks for equal bits.
+widest tiles of the expansion, few rows at high ranks for equal bits, and contractions so short that every part of a 32-bit
+factor shows.
 
 test_gpu_adapter.py has the tolerances of the long sums; its batches over banks of 1 to 3 are taken as they lie.
 """
@@ -8,7 +9,7 @@ import pytest
 import torch
 
 import test_gpu_adapter as base
-from test_gpu_adapter import BF, F
+from test_gpu_adapter import BF, F, U
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +71,55 @@ def test_few_rows_of_high_ranks_repeat(tbn, rank, wt, xt, ot):
             out = (y, t) + tbn.adapter_bwd(d["x"], d["dy"], d["index"], d["a"], d["b"], t, scale=d["scale"], residual=d["res_x"],
                                            out_dtype=ot)
             assert all(torch.equal(p, q) for p, q in zip(first, out)), (rows, c, k, n)
+
+
+# Short contractions.  A 32-bit factor is the sum of three bf16 numbers, each at most 2^-8 of the one before, exactly (24 bits are
+# 8 + 8 + 8); the product of two leaves out mid lo, lo mid and lo lo: 2 * 2^-24 + 2^-32 of it, 2.1 U.  The parts' products are
+# added smallest first, so that only the last MFMA's additions count in full, n + 1 of them (the parts before have 2^-8 of
+# its size, six MFMAs of them: 6 (n + 1) 2^-8 of a rounding), each off by a whole step at most, 2 U, of the sum of magnitudes.  With the scale's
+# rounding and the sums over waves and tiles (n / 16 and 4 at most): below (2 (min(n, 32) + 1) + n / 16 + 12) U.
+# Without its third part a factor is off by up to 2^-16, 256 U, which for n up to 8 this sees in some of many sums (asserted below).
+def off(n):
+    return (2 * (min(n, 32) + 1) + n / 16 + 12) * U
+
+
+def two_parts(v):
+    hi = v.bfloat16().float()
+    return hi.double() + (v - hi).bfloat16().double()
+
+
+@pytest.mark.parametrize("rows,bank", [(48, 6), (130, 1), (1100, 12)])  # few rows, as they lie, in the adapters' order
+@pytest.mark.parametrize("n", [1, 3, 8])
+@pytest.mark.parametrize("wt,xt", [(F, F), (F, BF), (BF, F), (BF, BF)])
+def test_every_part_of_32_bit_factors(tbn, rows, bank, n, wt, xt):
+    s = base.make(rows, n, n, n, bank, wt, xt, F, index=torch.arange(rows) % bank)
+    d = base.gpu(s)
+    i = s["index"].long()
+    x, dy, a, b = s["x"].double(), s["dy"].double(), s["a"].double()[i], s["b"].double()[i]
+    sc = s["scale"].double()[i][:, None]
+
+    def times(m, v):  # row by row
+        return (m @ v[:, :, None])[:, :, 0]
+
+    y, t = tbn.adapter_fwd(d["x"], d["index"], d["a"], d["b"], scale=d["scale"], out_dtype=F)
+    want, tol = times(a, x), off(n) * times(a.abs(), x.abs())
+    base.check(t, want, tol, "t")
+    if F in (wt, xt):
+        short = times(two_parts(s["a"].float())[i], two_parts(s["x"].float()))
+        assert ((short - want).abs() > tol).any()
+    t = t.cpu()  # y from the t that the call gives
+    want, tol = sc * times(b, t.double()), sc * off(n) * times(b.abs(), t.double().abs())
+    base.check(y, want, tol, "y")
+    if n > 1 or F in (wt, xt):  # (t is one product of two bf16 numbers otherwise: 16 bits)
+        assert ((sc * times(b, two_parts(t)) - want).abs() > tol).any()
+
+    dx, da, db = tbn.adapter_bwd(d["x"], d["dy"], d["index"], d["a"], d["b"], t.cuda(), scale=d["scale"], out_dtype=F)
+    bt, at = b.transpose(1, 2), a.transpose(1, 2)
+    dt, e_dt = sc * times(bt, dy), sc * off(n) * times(bt.abs(), dy.abs())
+    base.check(dx, times(at, dt), times(at.abs(), e_dt + off(n) * dt.abs()), "dx")
+    own = torch.nn.functional.one_hot(i, bank).double()
+    m = int(own.sum(0).max())  # rows of an adapter
+    outer = lambda u, v: torch.einsum("nb,nr,nc->brc", own, u, v)  # noqa: E731
+    base.check(da, outer(dt, x), outer(e_dt + off(m) * dt.abs(), x.abs()), "da")
+    ts = sc * t.double()
+    base.check(db, outer(dy, ts), outer(dy.abs(), off(m) * ts.abs()), "db")
