@@ -474,7 +474,8 @@ tbn_status tbn_softmax_xent(const float* logits, const int32_t* labels, int32_t 
  *   for an adapter without rows).  dy [rows][K] dtype dyt; dx and residual [rows][C] dtype dxt; t from the forward pass.
  *   dx, da and db are each optional; one has to be given.
  * Products are exact (of fp32 factors but for 2^-23 of them), sums and t are fp32 in a fixed order.  NaN and infinities reach
- * their own row and adapter alone; an fp32 factor that is infinite, or rounds to infinity as bf16, gives NaN.
+ * their own row and adapter alone; an fp32 factor that is infinite, or rounds to infinity as bf16, gives NaN, and an infinite
+ * bf16 factor of an fp32 one (t and dt are such) may.
  * But for a residual that is y (dx) itself, an output or ws may not overlap an input or another output: TBN_ERR_SHAPE.
  * ws: tbn_adapter_workspace_size bytes for TBN_OP_FWD (forward) or TBN_OP_BWD_DATA (backward).
  * Limits: rows <= 2^27, C and K <= 2^24, rows C and rows K <= 2^35, S R C and S R K < 2^31 (TBN_ERR_SHAPE).

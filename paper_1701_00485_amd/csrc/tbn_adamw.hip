@@ -4,10 +4,11 @@
 //   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,
 //   w = w - lr decay w - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
 //
-// Bound by HBM: 28 bytes a weight with fp32 states and gradients, 16 to 18 with 8-bit states, all of it read and
-// written once.  Measured: 268 M weights with fp32 states 1405 us (5.35 TB/s), with 8-bit ones and bf16 gradients 785 us (4.8 TB/s;
-// 890 with a round's loads at a time); ResNet-18's 62 tensors, 8 bits, 42 us (4.5 TB/s);
-// 1.7 M weights in 4 tensors 9 us, 1000 weights 2.4.  The tensors' pointers are kernel arguments (62 tensors a launch), so that nothing is copied to
+// Bound by HBM: 28 bytes a weight with fp32 states and gradients; with 8-bit states 12 (the weight and two codes, read
+// and written; the scales are 16 bytes for 256 weights) and the gradient's 2 or 4; all of it read and written once.
+// Measured: 268 M weights with fp32 states 1400 us (5.4 TB/s), with 8-bit ones and bf16 gradients 780 us (4.8 TB/s;
+// 890 with a round's loads at a time); ResNet-18's 62 tensors, 8 bits, 42 us (4.5 TB/s); 1.7 M weights in 4 tensors 9 us,
+// 1000 weights 2.4.  The tensors' pointers are kernel arguments (62 tensors a launch), so that nothing is copied to
 // the device and a captured step replays with them; a block takes 1, 2 or 4 rounds of 1024 elements of one tensor, which
 // it finds by a look at all tensors' first blocks at once.
 //

@@ -8,9 +8,10 @@
 //   shrink  rows of C values -> R values: bound by reading the rows (long batches) or the adapters (one token each)
 //   expand  rows of R values -> K values, added to the residual: bound by the residual and the output
 //   outer   the gradients: for each adapter the products of its rows' R values with their C values, summed
-// Measured: 48 tokens of 48 requests, 8192 -> 32768, rank 16, 7.4 + 16 us (70 MB of adapters, 3.6 TB/s in one pass of 19.5 us);
-// 5000 rows of 11 prompts, 4096 -> 4096, rank 32, 20 + 5 + 25 us (floor 26); backward of 8192 rows, 4096 -> 8192, four fp32
-// adapters of rank 16, 42 + 5 (dt) + 45 + 6 (gradients) + 44 us (dx), floor 71: dy is read twice.
+// Measured: 48 tokens of 48 requests, 8192 -> 32768, rank 16, 8 + 16 us (70 MB of adapters, 3.2 TB/s in one pass of 22 us);
+// 5000 rows of 11 prompts, 4096 -> 4096, rank 32, 21 + 5 + 25 us (floor 26; fp32 rows 34 + 5 + 24, fp32 factors 27 + 5 + 28, rank 64
+// 35 + 5 + 30, rank 128 48 + 5 + 54); backward of 8192 rows, 4096 -> 8192, four fp32 adapters of rank 16, 43 + 5 (dt) + 44 + 6
+// (gradients) + 43 us (dx), floor 71, 28 us more for reading dy twice.
 // All run on v_mfma_f32_16x16x32_bf16.  What has 32 bits (t, dt, fp32 weights or rows) enters exactly, as the sum of three
 // bf16 numbers (8 bits each), and a product of two such factors leaves out only the parts below 2^-23 of it: every result is
 // one of fp32 sums, a bf16 one rounded once.  Two parts, 16 bits, would save a third of these MFMAs, which do not
@@ -232,7 +233,8 @@ __global__ __launch_bounds__(1024) void order_kernel(const AdapterArgs a) {
 // each other are the splits of one tile: what runs at the same time reads long runs of a row (with the tiles next to
 // each other, all at the same columns of rows that are a power of two apart, a 134 MB batch took 50 us instead of 37).
 // 8192 rows of 8192 bf16 values: 42 us, 3.2 TB/s (a tile's every further adapter adds about 5); with 4 splits
-// 49, with 2 56.  What bounds it is the chain index, adapter, product at the few rounds a block has.
+// 49, with 2 56.  What bounds it is the chain index, adapter, product at the few rounds a block has.  fp32 rows 74 us, rank 64 81,
+// rank 128, in two slices that both read the rows, 128.
 // With gridDim.y > 1 the tile's adapters are dealt over y.  In the backward pass S more blocks order the rows for the
 // gradients beside it.
 constexpr int kShrinkWaves = 4;
@@ -528,7 +530,9 @@ __device__ __forceinline__ Frag<float> scaled(const Raw<float>& t, float scale) 
 // turned by the transposing LDS read); then every wave that has rows of this adapter multiplies and stores them.
 // Usually all of a block's rows have one adapter.  The chain index, factors, LDS, product, store is long, so what counts is
 // how much each wave has in flight, and two blocks a CU.  8192 rows of 4096 bf16 values: 34 us with bf16 adapters of rank
-// 16 (4.0 TB/s), 43 with fp32 ones (50 with 128 columns a block instead of 256, 46 with one block a CU).
+// 16 (4.0 TB/s), 43 with fp32 ones (50 with 128 columns a block instead of 256, 46 with one block a CU).  Two blocks a CU are
+// 128 registers a lane: the forms that turn [R][K] factors spill there, 256 columns a block 20 bytes a lane with bf16 factors and 52
+// with fp32 ones, ranks above 64 52 and 68.
 constexpr int kExpandWaves = 8;
 
 // The parts of fp32 factors lie `part` values apart.
@@ -668,7 +672,8 @@ __global__ __launch_bounds__(64 * kExpandWaves, 4) void expand_kernel(const Adap
 
 // Few rows, each likely with an adapter of its own: the adapters of a tile of 16 rows are dealt over z (never more of
 // them than gridDim.z), so that a block streams the factors of one adapter, kGroups groups of 64 columns a wave, the
-// next ones in flight (48 adapters 8192 -> 32768 of rank 16 16 us, 3.1 TB/s, of rank 64 46, 4.4), and touches that adapter's rows alone (z = 0 also those without one).
+// next ones in flight (48 adapters 8192 -> 32768 of rank 16 16 us, 3.1 TB/s, of rank 64 46, 4.4), and touches that adapter's
+// rows alone (z = 0 also those without one).
 constexpr int kGroups = 4;
 
 template <typename WT, typename OT, bool ACROSS, bool WHOLE, int RK>
@@ -748,7 +753,8 @@ __global__ __launch_bounds__(256) void expand_few_kernel(const AdapterArgs a) {
 // its eight waves take in tiles of 32.  A wave copies a tile's rows (whole 128-byte pieces of bf16 ones) into LDS and
 // reads the MFMA's operand, 8 rows of a column, by the transposing LDS read, the next tile's rows in flight and the rows of the
 // one after that known.  The waves add through LDS at the end.  Both gradients are one launch.  Bound by reading the rows: 8192
-// of 4096 and 8192 bf16 values 45 us (4.5 TB/s, part of them still in the caches), rank 64 106.
+// of 4096 and 8192 bf16 values 44 us (4.5 TB/s, part of them still in the caches), of fp32 ones 94; rank 64 100, rank 128 180 (the
+// splits into bf16 parts and the gathers of u grow with the rank).
 constexpr int kPitch = 72;  // elements of a tile's row in LDS: 64 and a shift of the banks
 constexpr int kOuterWaves = 8;
 
@@ -936,7 +942,7 @@ void expand(const AdapterArgs& a, hipStream_t s) {
         return;
     }
     // Groups of 64 columns a wave: what 64 KB of LDS and 128 registers (two blocks a CU) hold.  With 64 columns up to rank 64
-    // 8192 rows of 4096 and fp32 adapters of rank 64 took 68 us instead of 57; with 128 for higher ranks, which spill,
+    // 8192 rows of 4096 and fp32 adapters of rank 64 took 68 us instead of 57; with 128 for higher ranks, which spills more,
     // 5000 rows of 8192 took 67 instead of 54.  Small batches take 64 columns, for more blocks: 100 rows of 512, 4.7 us
     // instead of 7.8.
     constexpr int kNarrow = 1, kMiddle = 2, kWide = 4;

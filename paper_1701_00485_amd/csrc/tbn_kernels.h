@@ -437,13 +437,15 @@ struct AdapterOuter {
     uint32_t blocks0;  // of the first job
 };
 // Whether each row may well have an adapter of its own: the adapters of 16 rows are then dealt over blocks instead of taken in
-// turn by one.  8192 -> 16384, rank 16, 64 adapters: 128 rows of 128 requests 28 us (in turn 189), 1024 of 1024 154 (278), of
-// 8 35 (39), of one 31 (30).  In a small bank fewer adapters meet in a tile: 100 rows of one adapter, 512 -> 1000 backward,
+// turn by one.  8192 -> 16384, rank 16, 64 adapters: 128 rows of 128 requests 30 us (in turn 189), 1024 of 1024 185 (278), of
+// 8 35 (39), of one 31 (30).  Where the rows lie by chance the order of the adapters (below) is the faster one well before this
+// border: 1025 rows of 1025 requests 72 us.  In a small bank fewer adapters meet in a tile: 100 rows of one adapter, 512 -> 1000 backward,
 // 17.2 us against 14.9 in turn.
 inline bool adapter_few_rows(int64_t rows, int32_t adapters) { return rows <= 1024 && rows <= 64 * (int64_t)adapters; }
 // Whether the other batches are taken in the order of their adapters, which costs a launch and, where rows lie by chance,
-// saves a pass for every further adapter of a tile.  5000 rows, 4096 -> 4096, rank 32: each row one of 64 adapters 77 us
-// (as they lie 590), of 9 62; 11 prompts 58 to 61 (50).  A small bank's rows are taken as they lie: of 8 adapters by chance 137 us.
+// saves a pass for every further adapter of a tile.  5000 rows, 4096 -> 4096, rank 32: each row one of 64 adapters 71 us
+// (as they lie 590), of 9 58; 11 prompts over 9 adapters 55, over 8, as they lie, 50.  A small bank's rows are taken as they lie,
+// which suits rows in runs and costs others: of 8 adapters by chance 133 us.  The bank's size does not say which a batch has.
 // The launch takes 7 us for a few thousand rows and tens of adapters; a block an adapter, each reading the whole index, it grows
 // with rows times adapters: 8192 rows and 64 adapters 7, 32768 and 4096 175, 131072 and 4096 656, 2^20 and 2^14 20 ms.
 inline bool adapter_sorted_rows(int64_t rows, int32_t adapters) { return !adapter_few_rows(rows, adapters) && adapters > 8; }

@@ -6,13 +6,14 @@
 //
 // Bound by HBM: each tensor is read or written once (rows beyond 16384 values are read twice backward).  Measured: forward 8192
 // rows of 8192 bf16 values 51 us (5.2 TB/s), one row of 512 2.3 us of kernel; backward 16384 rows of 4096 82 us (4.9 TB/s), of
-// which the last sums are 6; 777 rows of 1000 6 + 4 us, launch and one row's latency.  A team of T threads (8 to 64 lanes of a wave, or a
-// whole block) keeps a row in registers, NV pieces of 8 neighbouring values per thread, so that the centred
-// sum of squares is a second pass over registers.  Teams walk the rows with the stride of the grid and keep
-// what belongs to their columns in registers over all of them: gamma and beta, and in the backward pass the
-// sums of dgamma and dbeta, which are added over the teams of a block and written as one row of partial
+// which the last sums are 6; 777 rows of 1000 6 + 4 us: launch and one row's latency, then 195 rows of partial sums, 7 loads in turn.
+// A team of T threads (8 to 64 lanes of a wave, or a whole block) keeps a row in registers, NV pieces of 8 neighbouring
+// values per thread, so that the centred sum of squares is a second pass over registers.  Teams walk the rows with the
+// stride of the grid and keep what belongs to their columns in registers over all of them: gamma and beta, and in the
+// backward pass the sums of dgamma and dbeta, which are added over the teams of a block and written as one row of partial
 // sums per block; a second kernel adds those in a fixed order (no atomics: the same bits every time).
-// Rows longer than the registers hold are read again from the caches (the *_long kernels).
+// Rows longer than the registers hold are read again, forward in ln_fwd_long_kernel (2048 rows of 65536 bf16 values 190 us, 2.8 TB/s
+// of x and y; of 20001 72 us, 2.3), backward in two kernels.
 //
 // All sums and statistics are fp32; a value is rounded once, where a bf16 output is stored.  Pieces are
 // loaded as 16-byte words at the alignment of an element, so odd C needs no other path than its last piece.
@@ -556,8 +557,11 @@ int team_of(int32_t C) {
     return -1;
 }
 
-// The widest team only where its registers suffice: forward, rows of whole pieces (2048 rows of 32768 67 us, the long
-// kernel, which reads them again from the caches, for the others).
+// The widest team only where its registers suffice: forward, rows of whole pieces (2048 rows of 32768 65 us, the long
+// kernel, which reads them again from the caches, for the others).  Backward the next one, of 512 threads and rows of 8193 to
+// 16384 values, spills where they are no whole pieces, 344 to 472 bytes a lane (whole fp32 rows and gradients 68).  It and the two
+// kernels for longer rows: 2048 rows of 16383 bf16 values 97 and 105 us, of 12001 83 and 88, 8192 of those 252 and 302; with few
+// rows or fp32 on both sides the two kernels: 300 of 12001 37 and 23, 2048 of 8201 fp32 values 116 and 90.
 int fwd_team(int32_t C) {
     const int team = team_of(C);
     return team == kNumTeams - 1 && C % 8 ? -1 : team;

@@ -19,7 +19,6 @@ WALKS = [(70000, 40, BF, BF), (70001, 39, F, BF), (33000, 100, BF, F), (33003, 1
          (1100, 32768, BF, BF), (600, 20001, F, BF), (4200, 16392, BF, BF)]
 
 
-
 def close(got, want, tol, what):
     off = (got.double() - want).abs() - tol
     assert not torch.isnan(off).any() and off.max() <= 0, "%s: %g over the tolerance" % (what, off.max())
