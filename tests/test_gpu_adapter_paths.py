@@ -123,3 +123,40 @@ def test_every_part_of_32_bit_factors(tbn, rows, bank, n, wt, xt):
     base.check(da, outer(dt, x), outer(e_dt + off(m) * dt.abs(), x.abs()), "da")
     ts = sc * t.double()
     base.check(db, outer(dy, ts), outer(dy.abs(), off(m) * ts.abs()), "db")
+
+
+@pytest.mark.parametrize("rows", [1, 50, 1500])  # few rows, and rows in the adapters' order
+def test_largest_bank(tbn, rows):
+    # 65535 adapters of rank 2, 24 -> 40, the first and the last among those in use, a row beyond the bank's end; the gradients of
+    # all others are zero
+    bank, rank, c, k = 65535, 2, 24, 40
+    g = torch.Generator().manual_seed(rows)
+    index = torch.randint(0, bank, (rows,), generator=g)
+    index[:5] = torch.tensor([bank - 1, 0, bank, bank - 1, bank - 2])[:rows]
+    x, dy = torch.randn(rows, c, generator=g).to(BF), torch.randn(rows, k, generator=g).to(BF)
+    a, b = torch.randn(bank, rank, c, generator=g).to(BF), torch.randn(bank, k, rank, generator=g).to(BF)
+    scale = torch.rand(bank, generator=g) + 0.5
+    d = [v.cuda() for v in (x, dy, index.int(), a, b, scale)]
+    y, t = tbn.adapter_fwd(d[0], d[2], d[3], d[4], scale=d[5], out_dtype=F)
+    dx, da, db = tbn.adapter_bwd(d[0], d[1], d[2], d[3], d[4], t, scale=d[5], out_dtype=F)
+    has = (index < bank).double()[:, None]
+    i = index.clamp(max=bank - 1)
+    x, dy, a, b, sc = x.double(), dy.double(), a[i].double(), b[i].double(), scale[i].double()[:, None] * has
+
+    def times(m, v):
+        return (m @ v[:, :, None])[:, :, 0]
+
+    want, tol = times(a, x) * has, off(c) * times(a.abs(), x.abs())
+    base.check(t, want, tol, "t")
+    t = t.cpu().double()
+    base.check(y, sc * times(b, t), sc * off(rank) * times(b.abs(), t.abs()), "y")
+    bt, at = b.transpose(1, 2), a.transpose(1, 2)
+    dt, e_dt = sc * times(bt, dy), sc * off(k) * times(bt.abs(), dy.abs())
+    base.check(dx, times(at, dt), times(at.abs(), e_dt + off(rank) * dt.abs()), "dx")
+    m = int(torch.bincount(i).max())
+
+    def bank_sum(u, v):
+        return torch.zeros(bank, u.shape[1], v.shape[1], dtype=torch.float64).index_add_(0, i, u[:, :, None] * v[:, None, :])
+
+    base.check(da, bank_sum(dt, x), bank_sum(e_dt + off(m) * dt.abs(), x.abs()), "da")
+    base.check(db, bank_sum(dy, sc * t), bank_sum(dy.abs(), off(m) * sc * t.abs()), "db")

@@ -61,3 +61,34 @@ def test_layer_norm_teams_of_several_rows(tbn, rows, c, xt, yt):
     want = s * (h - h.mean(1, keepdim=True) - xh * (h * xh).mean(1, keepdim=True))
     m1, m2 = h.abs().mean(1, keepdim=True), (h * xh).abs().mean(1, keepdim=True)
     close(dx, want, s * U * (6 * h.abs() + 70 * m1 + 80 * xh.abs() * m2) * 1.001 + HALF[xt] * want.abs() * 1.001, "dx")
+
+
+@pytest.mark.parametrize("rows,c,xt,yt", [(1, 65537, F, F), (2, (1 << 20) + 8, BF, BF), (1, 3000001, F, BF)],
+                         ids=lambda v: str(v).split(".")[-1])
+def test_layer_norm_of_very_long_rows(tbn, rows, c, xt, yt):
+    # a thread of 1024 adds c / 1024 values in turn, a tree of 10 and 16 waves follow: n roundings of a sum of c values; its share
+    # of the variance is twice the mean's error and n of its own
+    n = (c / 1024 + 8 + 26) * U
+    g = torch.Generator(device="cuda").manual_seed(c)
+    x, dy = (torch.randn(rows, c, generator=g, device="cuda") + 0.3).to(xt), torch.randn(rows, c, generator=g, device="cuda").to(yt)
+    gamma = 1 + 0.2 * torch.randn(c, generator=g, device="cuda")
+    y, mean, inv_std = tbn.layernorm_fwd(x, gamma, out_dtype=yt)
+    xd, d = x.double(), dy.double()
+    mu = xd.mean(1, keepdim=True)
+    s = 1 / ((xd - mu).square().mean(1, keepdim=True) + EPS).sqrt()
+    t_mu = n * xd.abs().mean(1, keepdim=True)
+    t_s = s * (2 * t_mu * s + n + 8 * U)
+    close(mean, mu[:, 0], t_mu[:, 0], "mean")
+    close(inv_std, s[:, 0], t_s[:, 0], "inv_std")
+    xh = (xd - mu) * s
+    want = xh * gamma
+    close(y, want, gamma.abs() * (t_mu * s + (xd - mu).abs() * t_s + 6 * U * xh.abs()) * 1.001 + HALF[yt] * want.abs() * 1.001, "y")
+    dx, dgamma, dbeta = tbn.layernorm_bwd(x, dy, mean, inv_std, gamma)
+    mu, s = mean.double()[:, None], inv_std.double()[:, None]
+    xh, h = (xd - mu) * s, d * gamma
+    close(dgamma, (d * xh).sum(0), 8 * U * (d * xh).abs().sum(0), "dgamma")
+    close(dbeta, d.sum(0), 2 * U * d.abs().sum(0), "dbeta")
+    want = s * (h - h.mean(1, keepdim=True) - xh * (h * xh).mean(1, keepdim=True))
+    m1, m2 = h.abs().mean(1, keepdim=True), (h * xh).abs().mean(1, keepdim=True)
+    tol = s * (6 * U * h.abs() + (n + 4 * U) * m1 + (n + 12 * U) * xh.abs() * m2)
+    close(dx, want, tol * 1.001 + HALF[xt] * want.abs() * 1.001, "dx")
