@@ -497,6 +497,100 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
                            const float* t, const void* residual, void* dx, tbn_dtype dxt, float* da, float* db, void* ws,
                            size_t ws_bytes, hipStream_t stream);
 
+/*
+ * A gated block of two-bit filters: f gates and f further filters over the same c features,
+ *   g = alpha_k (x W~) of filters 0 .. f - 1,  u = that of filters f .. 2 f - 1,  h = act(g) u,
+ * in one pass; act is g / (1 + e^-g) (SILU), g (1 + erf(g / sqrt 2)) / 2 (GELU) or max(g, 0) (RELU), in fp32.  The 2 f filters
+ * are those of one layer (tbn_quantize of a [2 f][c] matrix), so that the rest of its backward pass is that of
+ * a layer of 2 f filters.
+ *   x      [rows][c] bf16.   codes, alpha: TBN2 codes and scales of the 2 f filters.
+ *   h      [rows][f], dtype ht.
+ *   gu     optional output [rows][2 f] bf16: g and u, for the backward pass.
+ *
+ * tbn_glu_bwd: dgu [rows][2 f] bf16, the gradient of g and u from that of h:  dg = dh u act'(g),  du = dh act(g)
+ *   (RELU'(0) = 0).  dh [rows][f] bf16.  g and u are those that the forward pass kept (`gu`), or, where gu is NULL, are
+ *   computed again from x, codes and alpha (which are not read otherwise, and may be NULL).  h (optional) is written as
+ *   the forward pass wrote it (from a kept gu: from its bf16 values), for the gradient of the layer behind the block, so that h
+ *   need not be kept.  With the conv descriptor of the layer (n = rows, 1x1, c channels, 2 f filters),
+ *   tbn_conv2d_bwd_data of dgu gives dx and tbn_conv2d_bwd_weight of x and dgu gives dW.
+ * NaN and infinities in x reach their own row alone.
+ * ws: tbn_glu_workspace_size bytes (may be NULL when that is 0; it is for c % 8 == 0, and a kept gu needs none): x with rows
+ * padded to a multiple of 8.
+ * An output or ws may not overlap an input or another output: TBN_ERR_SHAPE.
+ * Limits: rows <= 2^30, c <= 2^20, f <= 2^24, the codes below 2 GiB, rows (c + 7) and rows f <= 2^34 (TBN_ERR_SHAPE).
+ */
+typedef enum tbn_act { TBN_ACT_SILU = 0, TBN_ACT_GELU = 1, TBN_ACT_RELU = 2 } tbn_act;
+
+typedef struct tbn_glu_desc {
+    int64_t rows;
+    int32_t c, f;
+    tbn_act act;
+} tbn_glu_desc;
+
+tbn_status tbn_glu_workspace_size(const tbn_glu_desc* desc, size_t* bytes);
+tbn_status tbn_glu_fwd(const tbn_glu_desc* desc, const void* x, const uint32_t* codes, const float* alpha, void* h, tbn_dtype ht,
+                       void* gu, void* ws, size_t ws_bytes, hipStream_t stream);
+tbn_status tbn_glu_bwd(const tbn_glu_desc* desc, const void* dh, const void* gu, const void* x, const uint32_t* codes,
+                       const float* alpha, void* dgu, void* h, tbn_dtype ht, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Muon: a step on real weights that are matrices, along their momentum made orthogonal.  In place, for every matrix:
+ *   m = momentum m + g;   u = g + momentum m (nesterov) or m;   X = u / (|u| + eps), |u| the root of the sum of squares;
+ *   `steps` times:  A = X X^T,  X = a X + (b A + c A A) X,  (a, b, c) = (3.4445, -4.7750, 2.0315)
+ *   (of X^T where there are more rows than columns);
+ *   w = w - lr weight_decay w - lr scale X.
+ * Five steps bring every singular value of the update that is not tiny to between 0.7 and 1.2.  Sums are fp32, factors are held
+ * in 22 bits, |u| is summed in 64 bits.  A gradient with an infinity or NaN makes the whole matrix NaN, and its own values of m.
+ *   tensors  `n` of them in host memory (read during the call only): w, m [rows][cols] fp32 (for a convolution: K filters of
+ *            R*S*C values), g [rows][cols] of type gt, the weight decay, and the scale (customarily
+ *            sqrt(max(1, rows / cols))).
+ *   hyper    lr, momentum in [0, 1), eps in [1e-30, 1], steps 1 to 32; lr_dev (optional) replaces lr by a value in device memory,
+ *            read when the kernels run.
+ *   ws       tbn_muon_workspace_size bytes for the same list (its rows and cols alone are read).
+ * w, m and g need no alignment beyond their elements'.  No two of the written arrays may overlap, nor may any g or ws overlap
+ * one of them: TBN_ERR_SHAPE.  Deterministic.  Many matrices in one call share its launches.
+ * Limits: sides up to 2^20, rows cols < 2^31.
+ */
+typedef struct tbn_muon_tensor {
+    float* w;
+    float* m;
+    const void* g;
+    int32_t rows, cols;
+    float weight_decay, scale;
+} tbn_muon_tensor;
+
+typedef struct tbn_muon_hyper {
+    double lr, momentum, eps;
+    int32_t steps, nesterov;
+    const float* lr_dev;
+} tbn_muon_hyper;
+
+tbn_status tbn_muon_workspace_size(const tbn_muon_tensor* tensors, int32_t n, size_t* bytes);
+tbn_status tbn_muon_step(const tbn_muon_tensor* tensors, int32_t n, tbn_dtype gt, const tbn_muon_hyper* hyper, void* ws,
+                         size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Layers that stay out of two bits (the first and the last of a network), served in 8-bit integers with a scale for each row
+ * of both operands, each token and each channel.
+ *
+ * tbn_quantize_rows_i8: rows of c values to 8 bits:  scale = t fp32(1/127), t the row's largest finite magnitude;
+ *   q = clamp(round-half-even(x fp32(127 / t)), -127, 127), products in fp32; infinities become +-127, a NaN 0.  A row whose t
+ *   is below 2^-100 has scale 0 and zeros.  x [rows][c] dtype xt; q [rows][round_up(c, 16)], zeros behind the c values;
+ *   scale [rows] fp32.  For activations (rows are tokens) and for weights (rows are channels).
+ *
+ * tbn_matmul_i8:  y[m][n] = act(scale_m wscale_n sum over k of q[m][k] w[n][k] + bias_n + residual[m][n]), the sum exact in
+ *   int32, the rest in fp32.
+ *   q [rows][c] int8, w [n][c] int8 (any values, c % 16 == 0), x_scale [rows], w_scale [n] fp32;  `ep` as for the two-bit
+ *   layers (optional; its scale multiplies w_scale): bias [n], residual [rows][n] of y's type, relu (NaN stays).  y [rows][n], dtype yt;
+ *   the residual may be y itself.
+ * An output may not overlap an input (but for y and the residual) or another output: TBN_ERR_SHAPE.
+ * Limits: c <= 131056 (int32 sums) for the product, 2^24 for the rows, n <= 2^24, rows <= 2^30, rows c, rows n and n c <= 2^34
+ * (TBN_ERR_SHAPE).
+ */
+tbn_status tbn_quantize_rows_i8(const void* x, tbn_dtype xt, int64_t rows, int32_t c, int8_t* q, float* scale, hipStream_t stream);
+tbn_status tbn_matmul_i8(int64_t rows, int32_t n, int32_t c, const int8_t* q, const float* x_scale, const int8_t* w,
+                         const float* w_scale, const tbn_epilogue* ep, void* y, tbn_dtype yt, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,6 +21,9 @@ Calls (same names as the C ABI, without the ``tbn_`` prefix):
   sgd_step_quantize(w, v, g, lr, ...)  the update fused with the next quantisation
   layernorm_fwd / layernorm_bwd, adamw_step, adapter_fwd / adapter_bwd: what is trained and served beside
                                    frozen two-bit filters
+  glu_fwd / glu_bwd                a gated block of two-bit filters: projections, activation and product in one pass
+  muon_step                        real weights moved along their orthogonalised momentum
+  quantize_rows_i8, matmul_i8      layers that stay out of two bits, in 8-bit integers with a scale a row
 """
 from __future__ import annotations
 
@@ -126,6 +129,13 @@ def load():
         "tbn_adapter_fwd": ([vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, i32, vp, vp, ctypes.c_size_t, vp], i32),
         "tbn_adapter_bwd": ([vp, vp, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, ctypes.c_size_t, vp],
                             i32),
+        "tbn_glu_workspace_size": ([vp, vp], i32),
+        "tbn_glu_fwd": ([vp, vp, vp, vp, vp, i32, vp, vp, ctypes.c_size_t, vp], i32),
+        "tbn_glu_bwd": ([vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, ctypes.c_size_t, vp], i32),
+        "tbn_muon_workspace_size": ([vp, i32, vp], i32),
+        "tbn_muon_step": ([vp, i32, i32, vp, vp, ctypes.c_size_t, vp], i32),
+        "tbn_quantize_rows_i8": ([vp, i32, i64, i32, vp, vp, vp], i32),
+        "tbn_matmul_i8": ([i64, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp], i32),
         "tbn_conv2d_fwd_noalloc": ([vp, vp, i32, vp, vp, vp, vp, i32, vp], i32),
         "tbn_tuning_set": ([i32, i32], i32),
         "tbn_tuning_get": ([i32], i32),
@@ -179,6 +189,8 @@ def exported_symbols():
                    "tbn_batchnorm_train_fwd", "tbn_batchnorm_train_bwd", "tbn_relu_bwd", "tbn_softmax_xent",
                    "tbn_layernorm_fwd", "tbn_layernorm_workspace_size", "tbn_layernorm_bwd", "tbn_adamw_step",
                    "tbn_adapter_workspace_size", "tbn_adapter_fwd", "tbn_adapter_bwd",
+                   "tbn_glu_workspace_size", "tbn_glu_fwd", "tbn_glu_bwd", "tbn_muon_workspace_size", "tbn_muon_step",
+                   "tbn_quantize_rows_i8", "tbn_matmul_i8",
                    "tbn_tuning_set", "tbn_tuning_get", "tbn_conv2d_fwd_noalloc"])
 
 
@@ -1017,3 +1029,222 @@ def adapter_bwd(x, dy, index, a, b, t, scale=None, residual=None, out_dtype=None
              _dtype_code(a.dtype), ps, pt, pr, _beside(dx, "dx", x, _FLOATS), xt, _beside(da, "da", x, _F32),
              _beside(db, "db", x, _F32), _beside(ws, "ws", x, None), ws.numel() * ws.element_size())
     return dx, da, db
+
+
+# --------------------------------------------------------------------------------------
+# Feed-forward blocks: the gated block of two-bit filters, Muon on the real weights, and products in 8-bit integers for
+# layers that stay out of two bits.  These calls run on the device of their first tensor, on its current stream.
+# --------------------------------------------------------------------------------------
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
+
+
+class GluDesc(ctypes.Structure):
+    """A gated block: `rows` rows of c features, f gates and f further filters."""
+
+    _fields_ = [("rows", ctypes.c_int64), ("c", ctypes.c_int32), ("f", ctypes.c_int32), ("act", ctypes.c_int32)]
+
+
+def glu_workspace_size(desc: GluDesc) -> int:
+    b = ctypes.c_size_t()
+    _call("tbn_glu_workspace_size", ctypes.byref(desc), ctypes.byref(b))
+    return b.value
+
+
+def _activation(act):
+    if act not in ACTIVATIONS:
+        raise ValueError("act is one of %s: got %r" % (", ".join(ACTIVATIONS), act))
+    return ACTIVATIONS[act]
+
+
+def _glu_filters(x, codes, alpha):
+    """(rows, c, f) of a block's input and filters."""
+    rows, c = _rows_of(x)
+    if alpha.numel() < 2 or alpha.numel() % 2:
+        raise ValueError("alpha has %d elements, expected the gates' and as many others" % alpha.numel())
+    _numel(codes, packed_words(alpha.numel(), c), "codes")
+    return rows, c, alpha.numel() // 2
+
+
+def _glu_ws(d, ws, device):
+    need = glu_workspace_size(d)
+    if ws is None and need:
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+    return ws, 0 if ws is None else ws.numel() * ws.element_size()
+
+
+def glu_fwd(x, codes, alpha, act="silu", want_gu=False, out_dtype=torch.bfloat16, h=None, ws=None):
+    """A gated block of two-bit filters: x [..][C] bf16, `codes` and `alpha` of 2 F filters of C elements (quantize of a
+    [2 F][C] matrix: the gates first).  g and u the two projections, h = act(g) u; act "silu", "gelu" or "relu".  Returns
+    (h, gu): h [..][F] of `out_dtype`, and with `want_gu` the projections [..][2 F] bf16 for glu_bwd (else None)."""
+    out = (_native or _load_native()).glu_fwd(x, codes, alpha, act, want_gu, out_dtype, h, ws)
+    if out is not NotImplemented:
+        return out
+    rows, c, f = _glu_filters(x, codes, alpha)
+    d = GluDesc(rows, c, f, _activation(act))
+    px, pc, pa = _dev(x, "x", (torch.bfloat16,)), _beside(codes, "codes", x, (torch.int32,)), _beside(alpha, "alpha", x, _F32)
+    if h is None:
+        _dtype_code(out_dtype)
+        h = torch.empty(tuple(x.shape[:-1]) + (f,), dtype=out_dtype, device=x.device)
+    _numel(h, rows * f, "h")
+    gu = torch.empty(tuple(x.shape[:-1]) + (2 * f,), dtype=torch.bfloat16, device=x.device) if want_gu else None
+    ws, ws_bytes = _glu_ws(d, ws, x.device)
+    _call_on(x, "tbn_glu_fwd", ctypes.byref(d), px, pc, pa, _beside(h, "h", x, _FLOATS), _dtype_code(h.dtype),
+             _beside(gu, "gu", x, None), _beside(ws, "ws", x, None), ws_bytes)
+    return h, gu
+
+
+def glu_bwd(dh, gu=None, x=None, codes=None, alpha=None, act="silu", want_h=False, out_dtype=torch.bfloat16, dgu=None, ws=None):
+    """Backward of glu_fwd from dh [..][F] bf16 to the projections: returns (dgu, h), dgu [..][2 F] bf16 and, with `want_h`, the
+    block's output again (else None).  From the projections `gu` that glu_fwd gave, or, without them, from its x, codes and
+    alpha, which computes them again.  The 2 F filters are those of one layer: conv2d_bwd_data of dgu gives dx,
+    conv2d_bwd_weight of x and dgu gives dW (straight-through)."""
+    out = (_native or _load_native()).glu_bwd(dh, gu, x, codes, alpha, act, want_h, out_dtype, dgu, ws)
+    if out is not NotImplemented:
+        return out
+    rows, f = _rows_of(dh)
+    c = 8
+    if gu is not None:
+        _numel(gu, 2 * dh.numel(), "gu")
+        x = codes = alpha = None
+    else:
+        if x is None or codes is None or alpha is None:
+            raise ValueError("glu_bwd needs gu, or x, codes and alpha")
+        _numel(alpha, 2 * f, "alpha")
+        x_rows, c, _ = _glu_filters(x, codes, alpha)
+        if x_rows != rows:
+            raise ValueError("x has %d rows, expected %d" % (x_rows, rows))
+    d = GluDesc(rows, c, f, _activation(act))
+    pd, pg = _dev(dh, "dh", (torch.bfloat16,)), _beside(gu, "gu", dh, (torch.bfloat16,))
+    px, pc, pa = (_beside(x, "x", dh, (torch.bfloat16,)), _beside(codes, "codes", dh, (torch.int32,)), _beside(alpha, "alpha", dh, _F32))
+    if dgu is None:
+        dgu = torch.empty(tuple(dh.shape[:-1]) + (2 * f,), dtype=torch.bfloat16, device=dh.device)
+    _numel(dgu, rows * 2 * f, "dgu")
+    _dtype_code(out_dtype)
+    h = torch.empty(dh.shape, dtype=out_dtype, device=dh.device) if want_h else None
+    ws, ws_bytes = _glu_ws(d, ws, dh.device)
+    _call_on(dh, "tbn_glu_bwd", ctypes.byref(d), pd, pg, px, pc, pa, _beside(dgu, "dgu", dh, (torch.bfloat16,)),
+             _beside(h, "h", dh, _FLOATS), _dtype_code(out_dtype), _beside(ws, "ws", dh, None), ws_bytes)
+    return dgu, h
+
+
+class MuonTensor(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("w", "m", "g")] + [("rows", ctypes.c_int32), ("cols", ctypes.c_int32),
+                                                                  ("weight_decay", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class MuonHyper(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_double) for f in ("lr", "momentum", "eps")] + [
+        ("steps", ctypes.c_int32), ("nesterov", ctypes.c_int32), ("lr_dev", ctypes.c_void_p)]
+
+
+def _muon_table(w):
+    table = (MuonTensor * len(w))()
+    for i, t in enumerate(w):
+        if t.dim() < 2 or t.numel() < 1:
+            raise ValueError("w[%d] is no matrix: %s" % (i, tuple(t.shape)))
+        rows, cols = t.shape[0], t.numel() // t.shape[0]
+        if rows > 1 << 20 or cols > 1 << 20:
+            raise ValueError("w[%d] has a side over 2^20" % i)
+        table[i].rows, table[i].cols = rows, cols
+    return table
+
+
+def muon_workspace_size(w) -> int:
+    """Bytes of workspace of muon_step for a list of matrices (their shapes alone are read)."""
+    b = ctypes.c_size_t()
+    _call("tbn_muon_workspace_size", _muon_table(w), len(w), ctypes.byref(b))
+    return b.value
+
+
+def muon_step(w, m, g, lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.0, scale=None, eps=1e-7, steps=5, ws=None):
+    """One step of Muon over lists of matrices, in place: m = momentum m + g, the update g + momentum m (without `nesterov` m) made
+    orthogonal by `steps` Newton-Schulz products, w = w - lr weight_decay w - lr scale times it.  w and m fp32, g all fp32
+    or all bf16; a tensor of more than two axes is a matrix of its first by all others (a convolution's filters).  `scale`: one
+    number a matrix (default sqrt(max(1, rows / cols))).  `lr` may be a one-element fp32 GPU tensor, read when the kernels run.
+    `weight_decay`: a number or one for each matrix.  Returns (w, m)."""
+    out = (_native or _load_native()).muon_step(w, m, g, lr, momentum, nesterov, weight_decay, scale, eps, steps, ws)
+    if out is not NotImplemented:
+        return out
+    n = len(w)
+    if n == 0:
+        raise ValueError("w has no tensors")
+    decays = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(d) for d in weight_decay]
+    table = _muon_table(w)
+    scales = [max(1.0, t.rows / t.cols) ** 0.5 for t in table] if scale is None else [float(s) for s in scale]
+    for name, l in (("m", m), ("g", g), ("weight_decay", decays), ("scale", scales)):
+        if len(l) != n:
+            raise ValueError("%s has %d entries, expected %d" % (name, len(l), n))
+    for i in range(n):
+        for name, t in (("m", m[i]), ("g", g[i])):
+            _numel(t, w[i].numel(), "%s[%d]" % (name, i))
+    first = w[0]
+    gt = _dtype_code(g[0].dtype)
+    for i in range(n):
+        table[i].w, table[i].m, table[i].g = (_beside(t, "%s[%d]" % (name, i), first, types) for name, t, types in (
+            ("w", w[i], _F32), ("m", m[i], _F32), ("g", g[i], (g[0].dtype,))))
+        table[i].weight_decay, table[i].scale = decays[i], scales[i]
+    h = MuonHyper(0.0, float(momentum), float(eps), int(steps), 1 if nesterov else 0, None)
+    if isinstance(lr, torch.Tensor):
+        _numel(lr, 1, "lr")
+        h.lr_dev = _beside(lr, "lr", first, _F32)
+    else:
+        h.lr = float(lr)
+    if ws is None:
+        ws = torch.empty(muon_workspace_size(w), dtype=torch.uint8, device=first.device)
+    _call_on(first, "tbn_muon_step", table, n, gt, ctypes.byref(h), _beside(ws, "ws", first, None), ws.numel() * ws.element_size())
+    return w, m
+
+
+def quantize_rows_i8(x, q=None, scale=None):
+    """Rows of x [..][C] (bf16 or fp32) in 8-bit integers with a scale each: scale = largest / 127, q the nearest integer of
+    x / scale.  Returns (q [rows][C rounded up to 16] int8 with zeros behind the C values, scale [rows] fp32).  For activations,
+    a scale a token, and for weights [N][C], a scale a channel."""
+    out = (_native or _load_native()).quantize_rows_i8(x, q, scale)
+    if out is not NotImplemented:
+        return out
+    rows, c = _rows_of(x)
+    pitch = -(-c // 16) * 16
+    px = _dev(x, "x", _FLOATS)
+    if q is None:
+        q = torch.empty((rows, pitch), dtype=torch.int8, device=x.device)
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _numel(q, rows * pitch, "q")
+    _numel(scale, rows, "scale")
+    _call_on(x, "tbn_quantize_rows_i8", px, _dtype_code(x.dtype), rows, c, _beside(q, "q", x, (torch.int8,)),
+             _beside(scale, "scale", x, _F32))
+    return q, scale
+
+
+def matmul_i8(xq, x_scale, wq, w_scale, scale=None, bias=None, residual=None, relu=False, out_dtype=torch.bfloat16, y=None):
+    """y = act(x_scale w_scale (xq wq^T) + bias + residual): xq [rows][C] and wq [N][C] int8 as quantize_rows_i8 gives them, the
+    sums exact.  x_scale [rows], w_scale [N], `scale` (a factor of w_scale) and `bias` [N] fp32; residual of y's type, y itself
+    at most.  y [rows][N] of `out_dtype`."""
+    out = (_native or _load_native()).matmul_i8(xq, x_scale, wq, w_scale, scale, bias, residual, relu, out_dtype, y)
+    if out is not NotImplemented:
+        return out
+    rows, c = _rows_of(xq)
+    n, wc = _rows_of(wq)
+    if wc != c:
+        raise ValueError("wq has rows of %d values, expected %d" % (wc, c))
+    _numel(x_scale, rows, "x_scale")
+    _numel(w_scale, n, "w_scale")
+    _at_least(scale, n, "scale")
+    _at_least(bias, n, "bias")
+    i8 = (torch.int8,)
+    pq, pw = _dev(xq, "xq", i8), _beside(wq, "wq", xq, i8)
+    pxs, pws = _beside(x_scale, "x_scale", xq, _F32), _beside(w_scale, "w_scale", xq, _F32)
+    if y is not None:
+        _numel(y, rows * n, "y")
+        out_dtype = y.dtype
+    yt = _dtype_code(out_dtype)
+    if residual is not None:
+        _numel(residual, rows * n, "residual")
+        if residual.dtype != out_dtype:
+            raise TypeError("residual must have y's dtype")
+    ep = Epilogue(_beside(scale, "scale", xq, _F32), _beside(bias, "bias", xq, _F32), _beside(residual, "residual", xq, _FLOATS),
+                  1 if relu else 0)
+    if y is None:
+        y = torch.empty((rows, n), dtype=out_dtype, device=xq.device)
+    _call_on(xq, "tbn_matmul_i8", rows, n, c, pq, pxs, pw, pws, ctypes.byref(ep), _beside(y, "y", xq, _FLOATS), yt)
+    return y

@@ -462,4 +462,84 @@ hipError_t launch_adapter_outer(const AdapterOuter& o, int32_t S, int32_t splits
 hipError_t launch_adapter_outer_sum(const float* part, int32_t splits, int64_t na, int64_t nb, float* da, float* db,
                                     hipStream_t s);
 
+// Products in 8-bit integers with a scale for each row of both operands.
+struct RowsI8Args {
+    const int8_t* x;  // [rows][c], c % 16 == 0
+    const int8_t* w;  // [n][c]
+    const float* x_scale;
+    const float* w_scale;
+    const float* scale;    // a factor of w_scale, or null
+    const float* bias;     // or null
+    const void* residual;  // of y's type, or null
+    void* y;               // [rows][n]
+    int64_t rows;
+    int32_t n, c;
+    int32_t relu, y_f32;
+};
+hipError_t launch_rows_i8(const void* x, int x_f32, int64_t rows, int32_t c, int8_t* q, float* scale, hipStream_t s);
+hipError_t launch_matmul_i8(const RowsI8Args& a, hipStream_t s);
+
+// Muon's step: matrices of the caller, hyperparameters, and what the kernels take.
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+constexpr int kMuonJobs = 24;  // matrices of a launch: their tables are kernel arguments (4 KiB at most)
+struct MuonHyper {
+    float lr, momentum, eps;
+    const float* lr_dev;
+    int32_t steps, nesterov, g_f32;
+};
+struct MuonStartJob {
+    float* m;
+    const void* g;
+    uint8_t* direct;  // X (or X^T) in the layout of m, and its transpose
+    uint8_t* turned;
+    double* norm;     // partial sums of squares
+    int32_t rows, cols;
+    uint32_t pitch_d, pitch_t;
+    uint32_t first, blocks, parts;
+};
+struct MuonStart {
+    MuonStartJob job[kMuonJobs];
+    int32_t n, nesterov;
+    float momentum, eps;
+};
+struct MuonJob {
+    const uint8_t* a;    // rows of M and of N, `pitch` bytes each
+    const uint8_t* b;
+    const uint8_t* aux;  // v = p (a b^T) + q aux, rows of pitch_o bytes
+    uint8_t* direct;     // v by rows, or null
+    uint8_t* turned;     // v by columns, or null
+    float* w;            // [M][N] moved along v, or null
+    f32x4_t* part;       // the sums of a split reduction
+    uint32_t pitch, pitch_o, pitch_t;
+    int32_t M, N;
+    uint32_t first, splits;
+    int32_t symmetric;
+    float p, q, weight_decay, scale;
+};
+struct MuonProducts {
+    MuonJob job[kMuonJobs];
+    const float* lr_dev;
+    float lr;
+    int32_t n;
+};
+static_assert(sizeof(MuonProducts) <= 4096 && sizeof(MuonStart) <= 4096, "kernel arguments");
+int muon_group(const tbn_muon_tensor* t, int n);
+int64_t muon_group_bytes(const tbn_muon_tensor* t, int n);
+hipError_t launch_muon_group(const tbn_muon_tensor* t, int n, const MuonHyper& h, uint8_t* ws, hipStream_t s);
+
+// The gated block of two-bit filters.
+struct GluArgs {
+    const uint16_t* x;      // [rows][c] bf16, c % 8 == 0
+    const uint32_t* codes;  // of 2 f filters
+    const float* alpha;     // [2 f]
+    const uint16_t* dh;     // [rows][f]: the backward pass; null: the forward pass
+    void* h;                // [rows][f], or null
+    uint16_t* gu;           // [rows][2 f]: the projections (forward) or their gradients, or null
+    int64_t rows;
+    int32_t c, f;
+    int32_t h_f32;
+};
+// `gu`: kept projections, for the backward pass without products
+hipError_t launch_glu(const GluArgs& a, const uint16_t* gu, int act, hipStream_t s);
+
 }  // namespace tbn

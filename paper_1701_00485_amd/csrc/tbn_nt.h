@@ -1,0 +1,178 @@
+// tbn_nt.h -- the inner loop that products of two row-major operands share: C[m][n] = sum over k of A[m][k] B[n][k],
+// both operands' rows contiguous along k, for 8-bit integers and for 32-bit values held as two 16-bit halves.
+//
+//   * A stage is 128 bytes of every row of the tile, whatever the type: 128 8-bit values, or 32 values as 32 leading
+//     and 32 trailing halves.  It goes from memory into LDS by buffer loads in LDS-DMA mode, 16-byte segments
+//     XOR-swizzled by (row / 2) % 8 on the way, so that the operand reads meet no bank twice.
+//   * Rows past the operand's end lie outside its buffer resource and arrive as zeros; so do segments past the end of A's
+//     row, and then it does not matter what B holds there.
+//   * Of a block's waves each owns (BM / WAVES_M) x (BN / WAVES_N) outputs.  The second operand goes first into the matrix
+//     instruction, so that lane l of 32x32 tile (i, t) holds row 32 i + l % 32 and, for each v / 4, the four consecutive
+//     columns 32 t + 8 (v / 4) + 4 (l / 32) + 0..3.
+//   * Operands of step u + 1 are read from LDS while the matrix instructions of step u run; the copies of the next stage
+//     are spread over the steps.
+#pragma once
+
+#include "tbn_device.h"
+#include "tbn_dma.h"
+
+namespace tbn {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// 8-bit integers: four steps of 32 a stage, exact 32-bit sums.
+struct NtI8 {
+    typedef i32x16 Acc;
+    static constexpr int STEPS = 4, PARTS = 1;
+    static __device__ __forceinline__ int seg(int u, int, int half) { return 2 * u + half; }
+    template <int TM, int TN>
+    static __device__ __forceinline__ void step(const u32x4 (&a)[PARTS][TM], const u32x4 (&b)[PARTS][TN], Acc (&acc)[TM][TN]) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int t = 0; t < TN; ++t)
+                acc[i][t] = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, b[0][t]),
+                                                                  __builtin_bit_cast(i32x4, a[0][i]), acc[i][t], 0, 0, 0);
+    }
+};
+
+// 32-bit values x = hi + lo in two fp16 halves (22 bits of x): two steps of 16 a stage, three products each; lo lo, 2^-22
+// of the product, is left out.
+struct NtF16x2 {
+    typedef f32x16 Acc;
+    static constexpr int STEPS = 2, PARTS = 2;
+    static __device__ __forceinline__ int seg(int u, int part, int half) { return 4 * part + 2 * u + half; }
+    static __device__ __forceinline__ f32x16 mul(u32x4 b, u32x4 a, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
+    }
+    template <int TM, int TN>
+    static __device__ __forceinline__ void step(const u32x4 (&a)[PARTS][TM], const u32x4 (&b)[PARTS][TN], Acc (&acc)[TM][TN]) {
+#pragma unroll
+        for (int p = 0; p < 3; ++p)  // lo hi, hi lo, hi hi
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int t = 0; t < TN; ++t) acc[i][t] = mul(b[p == 0][t], a[p == 1][i], acc[i][t]);
+    }
+};
+
+// The rows of an operand that a block's waves copy: row 8 (wave + WAVES j) + lane / 8 of the tile is this lane's of copy j.
+template <int ROWS, int WAVES>
+struct NtRows {
+    static constexpr int COPIES = ROWS / 8 / WAVES;
+    static_assert(ROWS % (8 * WAVES) == 0 && WAVES % 2 == 0, "whole copies");
+    v4i rsrc;
+    uint32_t off[COPIES];
+    // `row0` < rows; ROWS * pitch < 2^31 and pitch % 16 == 0 (checked by the host)
+    __device__ __forceinline__ void init(const void* p, int64_t row0, int64_t rows, uint32_t pitch, int wave, int lane, int seg) {
+        const int64_t left = rows - row0 < ROWS ? rows - row0 : ROWS;
+        rsrc = make_rsrc(reinterpret_cast<const uint8_t*>(p) + row0 * pitch, (uint32_t)(left * pitch));
+#pragma unroll
+        for (int j = 0; j < COPIES; ++j) off[j] = (uint32_t)(8 * (wave + WAVES * j) + (lane >> 3)) * pitch + 16u * seg;
+    }
+    // copy j of the stage at byte `at` of the rows (bit 31 set in lanes whose segment is past the row's end)
+    __device__ __forceinline__ void issue(int j, uint32_t lds, uint32_t at, int wave) const {
+        dma_b128(rsrc, lds + (uint32_t)(8 * (wave + WAVES * j)) * 128u, off[j] + at);
+    }
+};
+
+template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, class Op>
+struct NtLoop {
+    static constexpr int WAVES = WAVES_M * WAVES_N;
+    static constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 32, TN = WN / 32;
+    static constexpr int STAGE = (BM + BN) * 128, BYTES = STAGES * STAGE;
+    typedef typename Op::Acc Acc;
+    typedef NtRows<BM, WAVES> RowsA;
+    typedef NtRows<BN, WAVES> RowsB;
+    static constexpr int COPIES = RowsA::COPIES + RowsB::COPIES;
+
+    // Logical 16-byte segment that a lane copies of its row.
+    static __device__ __forceinline__ int copy_seg(int wave, int lane) { return (lane & 7) ^ ((4 * (wave & 1)) | ((lane >> 4) & 3)); }
+
+    // Adds the products of stages s0 .. s1 - 1 to acc.  `row_bytes`: of A's rows.  Every wave of the block calls it; it ends
+    // behind a barrier, after which the LDS is free.
+    static __device__ __forceinline__ void run(const RowsA& ra, const RowsB& rb, uint8_t* smem, int s0, int s1, uint32_t row_bytes, int wave,
+                                               int lane, Acc (&acc)[TM][TN]) {
+        const int wm = wave / WAVES_N, wn = wave % WAVES_N;
+        const int half = lane >> 5, l32 = lane & 31;
+        const int sw = (l32 >> 1) & 7;
+        const uint32_t base = lds_addr(smem);
+        const uint32_t my = 16u * copy_seg(wave, lane);
+        const int n = s1 - s0;
+        int islot = 0;
+        // copies j0 .. j1 - 1 of stage s
+        auto issue = [&](int s, int j0, int j1) {
+            const uint32_t lds = base + (uint32_t)(islot * STAGE);
+            const uint32_t kb = (uint32_t)(s0 + s) * 128u;
+            const uint32_t at_a = kb + my < row_bytes ? kb : kb | 0x80000000u;
+#pragma unroll
+            for (int j = 0; j < COPIES; ++j) {
+                if (j < j0 || j >= j1) continue;
+                if (j < RowsA::COPIES)
+                    ra.issue(j, lds, at_a, wave);
+                else
+                    rb.issue(j - RowsA::COPIES, lds + BM * 128, kb, wave);
+            }
+            if (j1 == COPIES) islot = islot + 1 == STAGES ? 0 : islot + 1;
+        };
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s)
+            if (s < n) issue(s, 0, COPIES);
+        int cslot = 0;
+        const int arow = (wm * WM + l32) * 128, brow = (wn * WN + l32) * 128 + BM * 128;
+        for (int s = 0; s < n; ++s) {
+            if (s + STAGES - 2 < n)
+                wait_vmcnt((STAGES - 2) * COPIES);
+            else
+                wait_vmcnt(0);
+            __syncthreads();
+            const uint8_t* st = smem + cslot * STAGE;
+            cslot = cslot + 1 == STAGES ? 0 : cslot + 1;
+            u32x4 a[2][Op::PARTS][TM], b[2][Op::PARTS][TN];
+            auto read = [&](int u, int k) {
+#pragma unroll
+                for (int p = 0; p < Op::PARTS; ++p) {
+                    const int so = 16 * (Op::seg(u, p, half) ^ sw);
+#pragma unroll
+                    for (int t = 0; t < TN; ++t) b[k][p][t] = *reinterpret_cast<const u32x4*>(st + brow + 32 * 128 * t + so);
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) a[k][p][i] = *reinterpret_cast<const u32x4*>(st + arow + 32 * 128 * i + so);
+                }
+            };
+            read(0, 0);
+#pragma unroll
+            for (int u = 0; u < Op::STEPS; ++u) {
+                if (s + STAGES - 1 < n) issue(s + STAGES - 1, u * COPIES / Op::STEPS, (u + 1) * COPIES / Op::STEPS);
+                if (u + 1 < Op::STEPS) read(u + 1, (u + 1) & 1);
+                Op::step(a[u & 1], b[u & 1], acc);
+                if (u + 1 < Op::STEPS) {
+                    constexpr int READS = Op::PARTS * (TM + TN), MUL = TM * TN * (Op::PARTS == 1 ? 1 : 3);
+#pragma unroll
+                    for (int k = 0; k < (READS < MUL ? READS : MUL); ++k) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x100, (READS + MUL - 1) / MUL, 0);
+                    }
+#pragma unroll
+                    for (int k = READS; k < MUL; ++k) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        __syncthreads();
+    }
+};
+
+// Tile (m, n) of the work index w: bands of 8 tile rows, so that the blocks that an XCD runs side by side share rows of
+// both operands in its L2.
+__device__ __forceinline__ void nt_tile(uint32_t w, uint32_t tiles_m, uint32_t tiles_n, uint32_t* m, uint32_t* n) {
+    constexpr uint32_t BAND = 8;
+    const uint32_t band = w / (BAND * tiles_n), first = band * BAND;
+    const uint32_t rows = tiles_m - first < BAND ? tiles_m - first : BAND;
+    const uint32_t in = w - first * tiles_n;
+    *n = in / rows;
+    *m = first + (in - *n * rows);
+}
+
+}  // namespace tbn

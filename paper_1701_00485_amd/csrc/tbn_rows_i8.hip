@@ -1,0 +1,340 @@
+// tbn_rows_i8.hip -- products in 8-bit integers with a scale for each row of both operands (each token, each channel):
+// the rows made 8-bit, and y[m][n] = act(scale_m scale_n sum over k of q[m][k] w[n][k] + bias_n + residual), the sum exact.
+#include "tbn_kernels.h"
+#include "tbn_nt.h"
+
+namespace tbn {
+
+namespace {
+
+// ---- rows to 8 bits ----------------------------------------------------------------------
+// scale = t fp32(1/127) with t the row's largest finite magnitude, q = x (127 / t) rounded to the nearest, ties to even, and
+// held within +-127; NaN gives 0.  A row whose t is below 2^-100 has scale 0 and zeros (127 / t would leave fp32's range).
+// One pass over x where a thread can hold its part of the row (VECS pieces of 8 values), else two, the second from
+// the caches.
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+
+template <bool F32>
+__device__ __forceinline__ void load8(const void* x, int64_t at, int n, bool wide, float (&v)[8]) {
+    if (n >= 8 && wide) {
+        if constexpr (F32) {
+            const f32x4* p = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(x) + at);
+            const f32x4 a = p[0], b = p[1];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+        } else {
+            const u32x4 r = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(x) + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[2 * e] = bf16_bits_to_f32(r[e] & 0xFFFFu), v[2 * e + 1] = __uint_as_float(r[e] & 0xFFFF0000u);
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        v[e] = 0.0f;
+        if (e < n) v[e] = F32 ? reinterpret_cast<const float*>(x)[at + e] : bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(x)[at + e]);
+    }
+}
+
+__device__ __forceinline__ float top8(const float (&v)[8], float t) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float m = fabsf(v[e]);
+        t = m <= 3.402823466e38f ? fmaxf(t, m) : t;  // neither infinities nor NaN
+    }
+    return t;
+}
+
+__device__ __forceinline__ u32x2_t codes8(const float (&v)[8], float inv) {
+    u32x2_t r = {0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float q = rintf(v[e] * inv);
+        q = v[e] == v[e] && inv > 0.0f ? fminf(fmaxf(q, -127.0f), 127.0f) : 0.0f;
+        r[e / 4] |= ((uint32_t)(int)q & 0xFFu) << (8 * (e % 4));
+    }
+    return r;
+}
+
+// THREADS of a row, 256 / THREADS rows a block.
+template <bool F32, int THREADS, int VECS>
+__global__ __launch_bounds__(256) void rows_i8_kernel(const void* __restrict__ x, int64_t rows, int32_t c, int32_t pitch, bool wide,
+                                                      int8_t* __restrict__ q, float* __restrict__ scale) {
+    __shared__ float tops[4];
+    const int tid = threadIdx.x % THREADS;
+    const int64_t row = (int64_t)blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS;
+    if (THREADS < 256 && row >= rows) return;  // (a wave a row: no barrier follows)
+    const int64_t x0 = row * c, q0 = row * pitch;
+    const int vecs = pitch / 8;
+    float v[VECS ? VECS : 1][8];
+    float t = 0.0f;
+    if constexpr (VECS > 0) {
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) {
+            const int e = (tid + THREADS * j) * 8;
+            load8<F32>(x, x0 + e, c - e, wide, v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) t = top8(v[j], t);
+    } else {
+        for (int i = tid; i < vecs; i += THREADS) {
+            load8<F32>(x, x0 + 8 * i, c - 8 * i, wide, v[0]);
+            t = top8(v[0], t);
+        }
+    }
+#pragma unroll
+    for (int d = 32; d; d /= 2) t = fmaxf(t, __shfl_xor(t, d, 64));
+    if constexpr (THREADS == 256) {
+        if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = t;
+        __syncthreads();
+        t = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    }
+    const float inv = t >= 0x1p-100f ? 127.0f / t : 0.0f;
+    if (tid == 0) scale[row] = inv > 0.0f ? t * (1.0f / 127.0f) : 0.0f;
+    if constexpr (VECS > 0) {
+#pragma unroll
+        for (int j = 0; j < VECS; ++j)
+            if (tid + THREADS * j < vecs) *reinterpret_cast<u32x2_t*>(q + q0 + (tid + THREADS * j) * 8) = codes8(v[j], inv);
+    } else {
+        for (int i = tid; i < vecs; i += THREADS) {
+            load8<F32>(x, x0 + 8 * i, c - 8 * i, wide, v[0]);
+            *reinterpret_cast<u32x2_t*>(q + q0 + 8 * i) = codes8(v[0], inv);
+        }
+    }
+}
+
+// ---- what follows the sums ---------------------------------------------------------------
+// y of 8 consecutive channels n0 .. n0 + 7 of row m from their sums; `whole`: they all exist and lie 16-byte aligned.
+__device__ __forceinline__ void finish8(const RowsI8Args& a, int64_t m, int32_t n0, const float (&s)[8], bool whole) {
+    const float sx = a.x_scale[m];
+    const int64_t o = m * a.n + n0;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int32_t n = whole || n0 + e < a.n ? n0 + e : a.n - 1;
+        v[e] = s[e] * (sx * (a.scale ? a.w_scale[n] * a.scale[n] : a.w_scale[n])) + (a.bias ? a.bias[n] : 0.0f);
+    }
+    if (a.residual) {
+        if (whole && !a.y_f32) {
+            const u32x4 r = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.residual) + o);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[2 * e] += bf16_bits_to_f32(r[e] & 0xFFFFu), v[2 * e + 1] += __uint_as_float(r[e] & 0xFFFF0000u);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (n0 + e < a.n)
+                    v[e] += a.y_f32 ? reinterpret_cast<const float*>(a.residual)[o + e]
+                                    : bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(a.residual)[o + e]);
+        }
+    }
+    if (a.relu) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = v[e] > 0.0f || v[e] != v[e] ? v[e] : 0.0f;
+    }
+    if (whole && a.y_f32) {
+        f32x4* p = reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.y) + o);
+        p[0] = f32x4{v[0], v[1], v[2], v[3]};
+        p[1] = f32x4{v[4], v[5], v[6], v[7]};
+    } else if (whole) {
+        *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(a.y) + o) =
+            u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (n0 + e >= a.n) break;
+            if (a.y_f32)
+                reinterpret_cast<float*>(a.y)[o + e] = v[e];
+            else
+                reinterpret_cast<uint16_t*>(a.y)[o + e] = (uint16_t)f32_to_bf16_bits(v[e]);
+        }
+    }
+}
+
+// ---- many rows ---------------------------------------------------------------------------
+template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BM * BN >= 65536 ? 1 : 2) void matmul_i8_kernel(const RowsI8Args a) {
+    typedef NtLoop<BM, BN, WAVES_M, WAVES_N, STAGES, NtI8> Loop;
+    constexpr int PITCH = Loop::WN + 4;  // of a staged row, in floats
+    static_assert(Loop::BYTES >= Loop::WAVES * 32 * PITCH * 4, "staging fits in the ring");
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[Loop::BYTES];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t tiles_n = (uint32_t)((a.n + BN - 1) / BN), tiles_m = (uint32_t)((a.rows + BM - 1) / BM);
+    uint32_t tm, tn;
+    nt_tile((uint32_t)xcd_remap(blockIdx.x, gridDim.x), tiles_m, tiles_n, &tm, &tn);
+    const int64_t m0 = (int64_t)tm * BM;
+    const int32_t n0 = (int32_t)(tn * BN);
+
+    typename Loop::RowsA ra;
+    typename Loop::RowsB rb;
+    ra.init(a.x, m0, a.rows, (uint32_t)a.c, wave, lane, Loop::copy_seg(wave, lane));
+    rb.init(a.w, n0, a.n, (uint32_t)a.c, wave, lane, Loop::copy_seg(wave, lane));
+    i32x16 acc[Loop::TM][Loop::TN];
+#pragma unroll
+    for (int i = 0; i < Loop::TM; ++i)
+#pragma unroll
+        for (int t = 0; t < Loop::TN; ++t)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][t][v] = 0;
+    Loop::run(ra, rb, smem, 0, (a.c + 127) / 128, (uint32_t)a.c, wave, lane, acc);
+
+    // a wave turns each 32 rows of its tile in LDS and writes them with 16-byte stores
+    float* stage = reinterpret_cast<float*>(smem) + wave * 32 * PITCH;
+    const int wm = wave / WAVES_N, wn = wave % WAVES_N, half = lane >> 5, l32 = lane & 31;
+    constexpr int CG = Loop::WN / 8, RPP = 64 / CG;
+    const bool even = a.n % 8 == 0;  // y and the residual begin 16-byte aligned
+#pragma unroll
+    for (int i = 0; i < Loop::TM; ++i) {
+#pragma unroll
+        for (int t = 0; t < Loop::TN; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4*>(stage + l32 * PITCH + 32 * t + 8 * g + 4 * half) =
+                    f32x4{(float)acc[i][t][4 * g], (float)acc[i][t][4 * g + 1], (float)acc[i][t][4 * g + 2], (float)acc[i][t][4 * g + 3]};
+        __builtin_amdgcn_wave_barrier();
+        const int col = n0 + wn * Loop::WN + 8 * (lane % CG);
+#pragma unroll
+        for (int p = 0; p < 32 / RPP; ++p) {
+            const int r = p * RPP + lane / CG;
+            const int64_t m = m0 + wm * Loop::WM + 32 * i + r;
+            const f32x4* s = reinterpret_cast<const f32x4*>(stage + r * PITCH + 8 * (lane % CG));
+            const f32x4 lo = s[0], hi = s[1];
+            const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if (m < a.rows && col < a.n) finish8(a, m, col, v, even);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// ---- up to 16 rows -----------------------------------------------------------------------
+// The weights are read once and bound it.  A block owns 16 NG channels; each of its WAVES waves takes a range of the values,
+// 128 bytes of every channel a step: lane (f = l % 16, q = l / 16) reads bytes 32 q .. 32 q + 31 of channel f's as two
+// 16-byte pieces, a matrix instruction each, and of row f of x the same bytes (the order of the values in a sum of
+// integers is free).  The waves' sums meet in LDS.
+template <int NG, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void matvec_i8_kernel(const RowsI8Args a) {
+    __shared__ i32x4 sums[WAVES][NG][64];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int f = lane & 15, q = lane >> 4;
+    const int32_t n0 = (int32_t)blockIdx.x * 16 * NG;
+    const int steps = (a.c + 127) / 128;
+    const int s0 = (int)((int64_t)steps * wave / WAVES), s1 = (int)((int64_t)steps * (wave + 1) / WAVES);
+    const int8_t* wp[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) wp[g] = a.w + (int64_t)min(n0 + 16 * g + f, a.n - 1) * a.c;
+    const bool have = f < a.rows;
+    const int8_t* xp = a.x + (int64_t)(have ? f : 0) * a.c;
+    i32x4 acc[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) acc[g] = i32x4{0, 0, 0, 0};
+    constexpr int DEPTH = 2;
+    i32x4 wv[DEPTH][NG][2], xv[DEPTH][2];
+    auto load = [&](int d, int s) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int k = s * 128 + 32 * q + 16 * u;
+            const bool in = k < a.c;
+            const int kk = in ? k : 0;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) wv[d][g][u] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(wp[g] + kk));
+            xv[d][u] = i32x4{0, 0, 0, 0};
+            if (have && in) xv[d][u] = *reinterpret_cast<const i32x4*>(xp + kk);
+        }
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        if (s0 + d < s1) load(d, s0 + d);
+    for (int s = s0; s < s1; s += DEPTH) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            if (s + d >= s1) break;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int g = 0; g < NG; ++g) acc[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[d][g][u], xv[d][u], acc[g], 0, 0, 0);
+            if (s + d + DEPTH < s1) load(d, s + d + DEPTH);
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < NG; ++g) sums[wave][g][lane] = acc[g];
+    __syncthreads();
+    // lane (f, q) holds row f, channels 4 q .. 4 q + 3 of its 16
+    for (int g = wave; g < NG; g += WAVES) {
+        i32x4 t = sums[0][g][lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) t += sums[w][g][lane];
+        if (!have) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int32_t n = n0 + 16 * g + 4 * q + e;
+            if (n >= a.n) break;
+            const int64_t o = (int64_t)f * a.n + n;
+            const float sw = a.scale ? a.w_scale[n] * a.scale[n] : a.w_scale[n];
+            float v = (float)t[e] * (a.x_scale[f] * sw) + (a.bias ? a.bias[n] : 0.0f);
+            if (a.residual)
+                v += a.y_f32 ? reinterpret_cast<const float*>(a.residual)[o] : bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(a.residual)[o]);
+            if (a.relu) v = v > 0.0f || v != v ? v : 0.0f;
+            if (a.y_f32)
+                reinterpret_cast<float*>(a.y)[o] = v;
+            else
+                reinterpret_cast<uint16_t*>(a.y)[o] = (uint16_t)f32_to_bf16_bits(v);
+        }
+    }
+}
+
+template <int BM, int BN, int WM, int WN, int STAGES>
+hipError_t launch_tiles(const RowsI8Args& a, hipStream_t s) {
+    const int64_t blocks = (a.rows + BM - 1) / BM * ((a.n + BN - 1) / BN);
+    hipLaunchKernelGGL((matmul_i8_kernel<BM, BN, WM, WN, STAGES>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rows_i8(const void* x, int x_f32, int64_t rows, int32_t c, int8_t* q, float* scale, hipStream_t s) {
+    const int32_t pitch = (c + 15) / 16 * 16;
+    const bool wide = c % (x_f32 ? 4 : 8) == 0;
+#define TBN_ROWS(f32, threads, vecs)                                                                                           \
+    hipLaunchKernelGGL((rows_i8_kernel<f32, threads, vecs>), dim3((unsigned)((rows + 256 / threads - 1) / (256 / threads))), dim3(256), \
+                       0, s, x, rows, c, pitch, wide, q, scale)
+#define TBN_ROWS_BY_SIZE(f32)            \
+    if (c <= 64 * 8 * 2)                 \
+        TBN_ROWS(f32, 64, 2);            \
+    else if (c <= 256 * 8 * 2)           \
+        TBN_ROWS(f32, 256, 2);           \
+    else if (c <= 256 * 8 * 4)           \
+        TBN_ROWS(f32, 256, 4);           \
+    else                                 \
+        TBN_ROWS(f32, 256, 0)
+    if (x_f32) {
+        TBN_ROWS_BY_SIZE(true);
+    } else {
+        TBN_ROWS_BY_SIZE(false);
+    }
+#undef TBN_ROWS_BY_SIZE
+#undef TBN_ROWS
+    return hipGetLastError();
+}
+
+hipError_t launch_matmul_i8(const RowsI8Args& a, hipStream_t s) {
+    if (a.rows <= 16) {
+        const int64_t groups = (a.n + 15) / 16;
+#define TBN_VEC(ng) hipLaunchKernelGGL((matvec_i8_kernel<ng, 8>), dim3((unsigned)((groups + ng - 1) / ng)), dim3(512), 0, s, a)
+        if (groups >= 4 * 256)
+            TBN_VEC(4);
+        else if (groups >= 2 * 256)
+            TBN_VEC(2);
+        else
+            TBN_VEC(1);
+#undef TBN_VEC
+        return hipGetLastError();
+    }
+    const int64_t big = (a.rows + 255) / 256 * ((a.n + 255) / 256);
+    if (big >= 192) return launch_tiles<256, 256, 2, 2, 2>(a, s);
+    const int64_t mid = (a.rows + 127) / 128 * ((a.n + 127) / 128);
+    if (mid >= 192) return launch_tiles<128, 128, 2, 2, 2>(a, s);
+    return launch_tiles<64, 64, 2, 2, 4>(a, s);
+}
+
+}  // namespace tbn

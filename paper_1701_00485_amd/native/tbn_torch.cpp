@@ -21,6 +21,8 @@
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 
+#include <algorithm>
+#include <cmath>
 #include <vector>
 
 #include "tbn.h"
@@ -973,6 +975,196 @@ PyObject* adapter_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- feed-forward blocks -----------------------------------------------------------------
+bool activation(PyObject* o, tbn_act* out) {
+    if (!PyUnicode_CheckExact(o)) return false;
+    if (PyUnicode_CompareWithASCIIString(o, "silu") == 0) return *out = TBN_ACT_SILU, true;
+    if (PyUnicode_CompareWithASCIIString(o, "gelu") == 0) return *out = TBN_ACT_GELU, true;
+    if (PyUnicode_CompareWithASCIIString(o, "relu") == 0) return *out = TBN_ACT_RELU, true;
+    return false;
+}
+
+std::vector<int64_t> with_last(const at::Tensor& t, int64_t last) {
+    std::vector<int64_t> s(t.sizes().begin(), t.sizes().end());
+    s.back() = last;
+    return s;
+}
+
+// (x, codes, alpha, act, want_gu, out_dtype, h, ws)
+PyObject* glu_fwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    TBN_ARGS(8);
+    const at::Tensor* x = dense(v[0], at::kBFloat16);
+    tbn_glu_desc d = {};
+    bool want;
+    at::ScalarType ht;
+    Out h, gu;
+    Ws ws;
+    size_t need = 0;
+    if (!x || !rows_of(*x, &d.rows, &d.c)) return declined();
+    const at::Tensor *codes = beside(v[1], *x, at::kInt), *alpha = beside(v[2], *x, at::kFloat);
+    if (!codes || !alpha || alpha->numel() < 2 || alpha->numel() % 2 || alpha->numel() > INT32_MAX ||
+        codes->numel() != tbn_packed_words(alpha->numel(), d.c) || !activation(v[3], &d.act) || !truth(v[4], &want) ||
+        !out_type(v[6], v[5], &ht) || !ws.take(v[7]) || !near(ws, *x))
+        return declined();
+    d.f = (int32_t)(alpha->numel() / 2);
+    if (!h.take(v[6], ht, d.rows * d.f) || !near(h, *x) || tbn_glu_workspace_size(&d, &need) != TBN_OK) return declined();
+    OnDevice on(*x);
+    h.make(with_last(*x, d.f), ht, *x);
+    if (want) gu.make(with_last(*x, 2 * (int64_t)d.f), at::kBFloat16, *x);
+    ws.make(need, *x);
+    void *xp = x->data_ptr(), *hp = h.t.data_ptr(), *gp = want ? gu.t.data_ptr() : nullptr;
+    if (!call("tbn_glu_fwd", [&] {
+            return tbn_glu_fwd(&d, xp, u32(*codes), f32(*alpha), hp, code(ht), gp, ws.ptr(), ws.bytes(), on.stream);
+        }))
+        return nullptr;
+    return pack({h.object(), want ? gu.object() : none()});
+    END_HANDLE_TH_ERRORS
+}
+
+// (dh, gu, x, codes, alpha, act, want_h, out_dtype, dgu, ws)
+PyObject* glu_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    TBN_ARGS(10);
+    const at::Tensor *dh = dense(v[0], at::kBFloat16), *gu = nullptr, *x = nullptr, *codes = nullptr, *alpha = nullptr;
+    tbn_glu_desc d = {};
+    bool want;
+    at::ScalarType ht;
+    Out dgu, h;
+    Ws ws;
+    size_t need = 0;
+    if (!dh || !rows_of(*dh, &d.rows, &d.f)) return declined();
+    d.c = 8;
+    if (v[1] != Py_None) {
+        gu = beside(v[1], *dh, at::kBFloat16);
+        if (!gu || gu->numel() != 2 * dh->numel()) return declined();
+    } else {
+        int64_t rows;
+        x = beside(v[2], *dh, at::kBFloat16), codes = beside(v[3], *dh, at::kInt), alpha = beside(v[4], *dh, at::kFloat);
+        if (!x || !codes || !alpha || !rows_of(*x, &rows, &d.c) || rows != d.rows || alpha->numel() != 2 * (int64_t)d.f ||
+            codes->numel() != tbn_packed_words(alpha->numel(), d.c))
+            return declined();
+    }
+    if (!activation(v[5], &d.act) || !truth(v[6], &want) || !float_type(v[7], &ht) ||
+        !dgu.take(v[8], at::kBFloat16, 2 * dh->numel()) || !near(dgu, *dh) || !ws.take(v[9]) || !near(ws, *dh) ||
+        tbn_glu_workspace_size(&d, &need) != TBN_OK)
+        return declined();
+    OnDevice on(*dh);
+    dgu.make(with_last(*dh, 2 * (int64_t)d.f), at::kBFloat16, *dh);
+    if (want) h.make(dh->sizes(), ht, *dh);
+    ws.make(need, *dh);
+    void *dhp = dh->data_ptr(), *gp = gu ? gu->data_ptr() : nullptr, *xp = x ? x->data_ptr() : nullptr;
+    void *dp = dgu.t.data_ptr(), *hp = want ? h.t.data_ptr() : nullptr;
+    if (!call("tbn_glu_bwd", [&] {
+            return tbn_glu_bwd(&d, dhp, gp, xp, codes ? u32(*codes) : nullptr, alpha ? f32(*alpha) : nullptr, dp, hp, code(ht),
+                               ws.ptr(), ws.bytes(), on.stream);
+        }))
+        return nullptr;
+    return pack({dgu.object(), want ? h.object() : none()});
+    END_HANDLE_TH_ERRORS
+}
+
+// (w, m, g, lr, momentum, nesterov, weight_decay, scale, eps, steps, ws)
+PyObject* muon_step(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    TBN_ARGS(11);
+    if (!PyList_CheckExact(v[0]) || PyList_GET_SIZE(v[0]) < 1 || PyList_GET_SIZE(v[0]) > (1 << 20)) return declined();
+    const Py_ssize_t count = PyList_GET_SIZE(v[0]);
+    PyObject **w, **m, **g, **decay = nullptr, **scale = nullptr;
+    double wd = 0.0;
+    tbn_muon_hyper h = {};
+    bool nesterov, plain;
+    Ws ws;
+    size_t need = 0;
+    if (!list_of(v[0], count, &w) || !list_of(v[1], count, &m) || !list_of(v[2], count, &g) || !real(v[4], &h.momentum) ||
+        !truth(v[5], &nesterov) || (!real(v[6], &wd) && !list_of(v[6], count, &decay)) ||
+        (v[7] != Py_None && !list_of(v[7], count, &scale)) || !real(v[8], &h.eps) || !integer(v[9], &h.steps) || !ws.take(v[10]))
+        return declined();
+    h.nesterov = nesterov ? 1 : 0;
+    const at::Tensor *first = dense(w[0]), *g0 = dense(g[0]);
+    tbn_dtype gt;
+    if (!first || !g0 || !float_type(*g0, &gt) || !near(ws, *first) ||
+        !number_or_device(v[3], *first, at::kFloat, &h.lr_dev, &plain) || (plain && !real(v[3], &h.lr)))
+        return declined();
+    std::vector<tbn_muon_tensor> table((size_t)count);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        const at::Tensor *wt = beside(w[i], *first, at::kFloat), *mt = beside(m[i], *first, at::kFloat);
+        const at::Tensor* gg = beside(g[i], *first, g0->scalar_type());
+        if (!wt || !mt || !gg || wt->dim() < 2 || wt->numel() < 1 || mt->numel() != wt->numel() || gg->numel() != wt->numel())
+            return declined();
+        const int64_t rows = wt->size(0), cols = wt->numel() / rows;
+        if (rows > (1 << 20) || cols > (1 << 20)) return declined();
+        double d = wd, s = std::sqrt(std::max(1.0, (double)rows / (double)cols));
+        if ((decay && !real(decay[i], &d)) || (scale && !real(scale[i], &s))) return declined();
+        table[(size_t)i] = {f32(*wt), f32(*mt), gg->data_ptr(), (int32_t)rows, (int32_t)cols, (float)d, (float)s};
+    }
+    if (tbn_muon_workspace_size(table.data(), (int32_t)count, &need) != TBN_OK) return declined();
+    OnDevice on(*first);
+    ws.make(need, *first);
+    if (!call("tbn_muon_step", [&] {
+            return tbn_muon_step(table.data(), (int32_t)count, gt, &h, ws.ptr(), ws.bytes(), on.stream);
+        }))
+        return nullptr;
+    Py_INCREF(v[0]);
+    Py_INCREF(v[1]);
+    return pack({v[0], v[1]});
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, q, scale)
+PyObject* quantize_rows_i8(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    TBN_ARGS(3);
+    const at::Tensor* x = dense(v[0]);
+    tbn_dtype xt;
+    int64_t rows;
+    int32_t c;
+    Out q, scale;
+    if (!x || !float_type(*x, &xt) || !rows_of(*x, &rows, &c) || c > (1 << 24)) return declined();
+    const int64_t pitch = ((int64_t)c + 15) / 16 * 16;
+    if (!q.take(v[1], at::kChar, rows * pitch) || !near(q, *x) || !scale.take(v[2], at::kFloat, rows) || !near(scale, *x)) return declined();
+    OnDevice on(*x);
+    q.make({rows, pitch}, at::kChar, *x);
+    scale.make({rows}, at::kFloat, *x);
+    void *xp = x->data_ptr(), *qp = q.t.data_ptr();
+    if (!call("tbn_quantize_rows_i8",
+              [&] { return tbn_quantize_rows_i8(xp, xt, rows, c, reinterpret_cast<int8_t*>(qp), f32(scale.t), on.stream); }))
+        return nullptr;
+    return pack({q.object(), scale.object()});
+    END_HANDLE_TH_ERRORS
+}
+
+// (xq, x_scale, wq, w_scale, scale, bias, residual, relu, out_dtype, y)
+PyObject* matmul_i8(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    TBN_ARGS(10);
+    const at::Tensor* x = dense(v[0], at::kChar);
+    int64_t rows, channels;
+    int32_t c, wc;
+    bool relu;
+    at::ScalarType yt;
+    Opt scale, bias, residual;
+    Out y;
+    if (!x || !rows_of(*x, &rows, &c)) return declined();
+    const at::Tensor *xs = beside(v[1], *x, at::kFloat), *w = beside(v[2], *x, at::kChar), *s = beside(v[3], *x, at::kFloat);
+    if (!xs || !w || !s || !rows_of(*w, &channels, &wc) || wc != c || channels > (1 << 24) || xs->numel() != rows ||
+        s->numel() != channels || !scale.take(v[4], *x, at::kFloat, channels) || !bias.take(v[5], *x, at::kFloat, channels) ||
+        !truth(v[7], &relu) || !out_type(v[9], v[8], &yt) || !residual.take(v[6], *x, yt, rows * channels) ||
+        (residual.t && residual.t->numel() != rows * channels) || !y.take(v[9], yt, rows * channels) || !near(y, *x))
+        return declined();
+    OnDevice on(*x);
+    y.make({rows, channels}, yt, *x);
+    void *xp = x->data_ptr(), *wp = w->data_ptr(), *yp = y.t.data_ptr();
+    const tbn_epilogue ep = {scale.ptr<float>(), bias.ptr<float>(), residual.ptr(), relu ? 1 : 0};
+    if (!call("tbn_matmul_i8", [&] {
+            return tbn_matmul_i8(rows, (int32_t)channels, c, reinterpret_cast<int8_t*>(xp), f32(*xs), reinterpret_cast<int8_t*>(wp),
+                                 f32(*s), &ep, yp, code(yt), on.stream);
+        }))
+        return nullptr;
+    return y.object();
+    END_HANDLE_TH_ERRORS
+}
+
 // (ConvDesc, TbnError): the Python types that the calls above know
 PyObject* bind_types(PyObject*, PyObject* const* v, Py_ssize_t n) {
     TBN_ARGS(2);
@@ -990,7 +1182,9 @@ PyMethodDef methods[] = {
     TBN_FN(sgd_step_quantize), TBN_FN(quantize_act_i8),    TBN_FN(quantize_act_fp8),    TBN_FN(maxpool2d_fwd),
     TBN_FN(maxpool2d_bwd),    TBN_FN(avgpool_global),      TBN_FN(batchnorm_train_fwd), TBN_FN(batchnorm_train_bwd),
     TBN_FN(relu_bwd),         TBN_FN(softmax_xent),        TBN_FN(layernorm_fwd),       TBN_FN(layernorm_bwd),
-    TBN_FN(adamw_step),       TBN_FN(adapter_fwd),         TBN_FN(adapter_bwd),         TBN_FN(bind_types),
+    TBN_FN(adamw_step),       TBN_FN(adapter_fwd),         TBN_FN(adapter_bwd),         TBN_FN(glu_fwd),
+    TBN_FN(glu_bwd),          TBN_FN(muon_step),           TBN_FN(quantize_rows_i8),    TBN_FN(matmul_i8),
+    TBN_FN(bind_types),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tbn_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
