@@ -479,50 +479,14 @@ struct RowsI8Args {
 hipError_t launch_rows_i8(const void* x, int x_f32, int64_t rows, int32_t c, int8_t* q, float* scale, hipStream_t s);
 hipError_t launch_matmul_i8(const RowsI8Args& a, hipStream_t s);
 
-// Muon's step: matrices of the caller, hyperparameters, and what the kernels take.
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-constexpr int kMuonJobs = 24;  // matrices of a launch: their tables are kernel arguments (4 KiB at most)
+// Muon's step.
+constexpr int kMuonMatrices = 64;  // that share launches
+constexpr int kMuonSteps = 32;     // at most
 struct MuonHyper {
     float lr, momentum, eps;
     const float* lr_dev;
     int32_t steps, nesterov, g_f32;
 };
-struct MuonStartJob {
-    float* m;
-    const void* g;
-    uint8_t* direct;  // X (or X^T) in the layout of m, and its transpose
-    uint8_t* turned;
-    double* norm;     // partial sums of squares
-    int32_t rows, cols;
-    uint32_t pitch_d, pitch_t;
-    uint32_t first, blocks, parts;
-};
-struct MuonStart {
-    MuonStartJob job[kMuonJobs];
-    int32_t n, nesterov;
-    float momentum, eps;
-};
-struct MuonJob {
-    const uint8_t* a;    // rows of M and of N, `pitch` bytes each
-    const uint8_t* b;
-    const uint8_t* aux;  // v = p (a b^T) + q aux, rows of pitch_o bytes
-    uint8_t* direct;     // v by rows, or null
-    uint8_t* turned;     // v by columns, or null
-    float* w;            // [M][N] moved along v, or null
-    f32x4_t* part;       // the sums of a split reduction
-    uint32_t pitch, pitch_o, pitch_t;
-    int32_t M, N;
-    uint32_t first, splits;
-    int32_t symmetric;
-    float p, q, weight_decay, scale;
-};
-struct MuonProducts {
-    MuonJob job[kMuonJobs];
-    const float* lr_dev;
-    float lr;
-    int32_t n;
-};
-static_assert(sizeof(MuonProducts) <= 4096 && sizeof(MuonStart) <= 4096, "kernel arguments");
 int muon_group(const tbn_muon_tensor* t, int n);
 int64_t muon_group_bytes(const tbn_muon_tensor* t, int n);
 hipError_t launch_muon_group(const tbn_muon_tensor* t, int n, const MuonHyper& h, uint8_t* ws, hipStream_t s);

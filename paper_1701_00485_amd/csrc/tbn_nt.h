@@ -78,7 +78,7 @@ struct NtRows {
     }
 };
 
-template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, class Op>
+template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, class Op, bool EARLY = false>
 struct NtLoop {
     static constexpr int WAVES = WAVES_M * WAVES_N;
     static constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 32, TN = WN / 32;
@@ -144,7 +144,8 @@ struct NtLoop {
             read(0, 0);
 #pragma unroll
             for (int u = 0; u < Op::STEPS; ++u) {
-                if (s + STAGES - 1 < n) issue(s + STAGES - 1, u * COPIES / Op::STEPS, (u + 1) * COPIES / Op::STEPS);
+                if (EARLY && u == 0 && s + STAGES - 1 < n) issue(s + STAGES - 1, 0, COPIES);
+                if (!EARLY && s + STAGES - 1 < n) issue(s + STAGES - 1, u * COPIES / Op::STEPS, (u + 1) * COPIES / Op::STEPS);
                 if (u + 1 < Op::STEPS) read(u + 1, (u + 1) & 1);
                 Op::step(a[u & 1], b[u & 1], acc);
                 if (u + 1 < Op::STEPS) {

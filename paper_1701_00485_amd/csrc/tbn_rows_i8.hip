@@ -104,16 +104,14 @@ __global__ __launch_bounds__(256) void rows_i8_kernel(const void* __restrict__ x
 }
 
 // ---- what follows the sums ---------------------------------------------------------------
-// y of 8 consecutive channels n0 .. n0 + 7 of row m from their sums; `whole`: they all exist and lie 16-byte aligned.
-__device__ __forceinline__ void finish8(const RowsI8Args& a, int64_t m, int32_t n0, const float (&s)[8], bool whole) {
-    const float sx = a.x_scale[m];
+// y of 8 consecutive channels n0 .. n0 + 7 of row m from their sums, the row's and the channels' scales and biases; `whole`: they all
+// exist and lie 16-byte aligned.
+__device__ __forceinline__ void finish8(const RowsI8Args& a, int64_t m, int32_t n0, const float (&s)[8], float sx, const float (&sw)[8],
+                                        const float (&bias)[8], bool whole) {
     const int64_t o = m * a.n + n0;
     float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int32_t n = whole || n0 + e < a.n ? n0 + e : a.n - 1;
-        v[e] = s[e] * (sx * (a.scale ? a.w_scale[n] * a.scale[n] : a.w_scale[n])) + (a.bias ? a.bias[n] : 0.0f);
-    }
+    for (int e = 0; e < 8; ++e) v[e] = s[e] * (sx * sw[e]) + bias[e];
     if (a.residual) {
         if (whole && !a.y_f32) {
             const u32x4 r = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.residual) + o);
@@ -152,10 +150,10 @@ __device__ __forceinline__ void finish8(const RowsI8Args& a, int64_t m, int32_t 
 
 // ---- many rows ---------------------------------------------------------------------------
 template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
-__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BM * BN >= 65536 ? 1 : 2) void matmul_i8_kernel(const RowsI8Args a) {
-    typedef NtLoop<BM, BN, WAVES_M, WAVES_N, STAGES, NtI8> Loop;
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BM * BN >= 65536 ? 1 : BM * BN >= 16384 ? 2 : 3) void matmul_i8_kernel(const RowsI8Args a) {
+    typedef NtLoop<BM, BN, WAVES_M, WAVES_N, STAGES, NtI8, true> Loop;
     constexpr int PITCH = Loop::WN + 4;  // of a staged row, in floats
-    static_assert(Loop::BYTES >= Loop::WAVES * 32 * PITCH * 4, "staging fits in the ring");
+    static_assert(Loop::BYTES >= Loop::WAVES * 32 * PITCH * 4 + (BM + 2 * BN) * 4, "staging fits in the ring");
     __shared__ __attribute__((aligned(1024))) uint8_t smem[Loop::BYTES];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -178,11 +176,29 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BM * BN >= 65536 ? 1 : 2) v
             for (int v = 0; v < 16; ++v) acc[i][t][v] = 0;
     Loop::run(ra, rb, smem, 0, (a.c + 127) / 128, (uint32_t)a.c, wave, lane, acc);
 
+    // the tile's scales and biases, behind the waves' staging
+    float* const row_scale = reinterpret_cast<float*>(smem) + Loop::WAVES * 32 * PITCH;
+    float* const col_scale = row_scale + BM;
+    float* const col_bias = col_scale + BN;
+    for (int i = threadIdx.x; i < BM + BN; i += 64 * Loop::WAVES) {
+        if (i < BM) {
+            row_scale[i] = m0 + i < a.rows ? a.x_scale[m0 + i] : 0.0f;
+        } else {
+            const int32_t n = n0 + (i - BM);
+            const bool in = n < a.n;
+            row_scale[i] = in ? (a.scale ? a.w_scale[n] * a.scale[n] : a.w_scale[n]) : 0.0f;
+            row_scale[i + BN] = in && a.bias ? a.bias[n] : 0.0f;
+        }
+    }
+    __syncthreads();
     // a wave turns each 32 rows of its tile in LDS and writes them with 16-byte stores
     float* stage = reinterpret_cast<float*>(smem) + wave * 32 * PITCH;
     const int wm = wave / WAVES_N, wn = wave % WAVES_N, half = lane >> 5, l32 = lane & 31;
     constexpr int CG = Loop::WN / 8, RPP = 64 / CG;
     const bool even = a.n % 8 == 0;  // y and the residual begin 16-byte aligned
+    float sw[8], bias[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sw[e] = col_scale[wn * Loop::WN + 8 * (lane % CG) + e], bias[e] = col_bias[wn * Loop::WN + 8 * (lane % CG) + e];
 #pragma unroll
     for (int i = 0; i < Loop::TM; ++i) {
 #pragma unroll
@@ -200,7 +216,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BM * BN >= 65536 ? 1 : 2) v
             const f32x4* s = reinterpret_cast<const f32x4*>(stage + r * PITCH + 8 * (lane % CG));
             const f32x4 lo = s[0], hi = s[1];
             const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            if (m < a.rows && col < a.n) finish8(a, m, col, v, even);
+            if (m < a.rows && col < a.n) finish8(a, m, col, v, row_scale[wm * Loop::WM + 32 * i + r], sw, bias, even);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -331,10 +347,10 @@ hipError_t launch_matmul_i8(const RowsI8Args& a, hipStream_t s) {
         return hipGetLastError();
     }
     const int64_t big = (a.rows + 255) / 256 * ((a.n + 255) / 256);
-    if (big >= 192) return launch_tiles<256, 256, 2, 2, 2>(a, s);
+    if (big >= 192) return launch_tiles<256, 256, 2, 4, 2>(a, s);
     const int64_t mid = (a.rows + 127) / 128 * ((a.n + 127) / 128);
     if (mid >= 192) return launch_tiles<128, 128, 2, 2, 2>(a, s);
-    return launch_tiles<64, 64, 2, 2, 4>(a, s);
+    return launch_tiles<64, 64, 2, 2, 3>(a, s);
 }
 
 }  // namespace tbn
