@@ -64,37 +64,31 @@ __device__ __forceinline__ void get8(const uint8_t* p, float (&v)[8]) {
 __device__ __forceinline__ int64_t place(int64_t c) { return c / 32 * 128 + c % 32 * 2; }
 
 // ---- tables ------------------------------------------------------------------------------
-// A launch's table: the first blocks (tiles) of its jobs, the first divided stages, and the jobs.
-static_assert(kMuonMatrices <= 64, "a lane finds a job");
+static_assert(kMuonMatrices <= 64, "a lane finds a matrix");
 
-template <typename T>
-struct Table {
-    const uint32_t* first[2];  // round_up(n, 8) each, the largest value behind the last
-    const T* job;
-    int32_t n;
-    // The job that `at` falls into.
-    __device__ __forceinline__ const T& find(int which, uint32_t at) const {
-        const int lane = threadIdx.x & 63;
-        const uint32_t f = lane < n ? first[which][lane] : 0xFFFFFFFFu;
-        return job[__popcll(__ballot(f <= at)) - 1];
-    }
-};
-
-struct StartJob {
-    float* m;
+// A matrix: m <= n, transposed if `tall`; its arrays in the workspace.
+struct Matrix {
+    float* w;
+    float* mom;
     const void* g;
-    uint8_t* direct;  // X (or X^T) in the layout of m, and its transpose
-    uint8_t* turned;
-    double* norm;     // partial sums of squares
-    int32_t rows, cols;
-    uint32_t pitch_d, pitch_t;
-    uint32_t first, first_tile, parts, unused;
+    uint8_t *x[2], *xt[2], *a, *t, *p[3];
+    double* norm;          // partial sums of squares, `parts` of them
+    int32_t m, n;
+    uint32_t mp, np;       // bytes of a row of m (n) values
+    uint32_t parts, tall;
+    float weight_decay, scale;
 };
-struct Start {
-    Table<StartJob> table;
-    int32_t nesterov;
-    float momentum, eps;
+
+// What the launches are: A = X X^T; P of A; P A; P A P; the product of both P; P X.
+enum Kind { GRAM, POLY, TIMES, BOTH, PAIR, APPLY };
+struct Step {
+    int32_t kind;
+    int32_t second;  // of a chain's two steps
+    int32_t two;     // APPLY: by the product of two P
+    int32_t now;     // which X
+    int32_t last;    // APPLY: into w
 };
+
 // v = p (a b^T) + q aux + diag on the diagonal
 struct Job {
     const uint8_t* a;    // rows of M and of N, `pitch` bytes each
@@ -102,16 +96,67 @@ struct Job {
     const uint8_t* aux;  // rows of pitch_o bytes, or null
     uint8_t* direct;     // v by rows, or null
     uint8_t* turned;     // v by columns, or null
-    float* w;            // [M][N] moved along v, or null
     uint32_t pitch, pitch_o, pitch_t;
     int32_t M, N;
-    uint32_t first, first_tile;  // divided stages, and tiles, of the jobs before it
-    int32_t symmetric;
-    float p, q, diag, weight_decay, scale;
-    uint32_t unused;
+    bool symmetric, to_w;
+    float p, q, diag;
+};
+
+// Scales of the halves: X 2^12, A 2^14, P and P A 2^13, a product of two P 2^12.  `x`: a Matrix, here or in constant memory.
+template <typename X>
+__host__ __device__ __forceinline__ Job job_of(X x, const Step& s) {
+    const int kind = s.kind;
+    const bool apply = kind == APPLY, poly = kind == POLY, gram = kind == GRAM;
+    const bool turn = apply && s.last && x->tall;  // along the rows of w
+    const uint8_t* const p = s.second ? x->p[1] : x->p[0];
+    const uint8_t *const by = s.two ? x->p[2] : x->p[0], *const xt = s.now ? x->xt[1] : x->xt[0];
+    uint8_t* const to = gram || kind == BOTH ? x->a : kind == TIMES ? x->t : kind == PAIR ? x->p[2] : s.second ? x->p[1] : x->p[0];
+    Job j;
+    j.a = gram ? (s.now ? x->x[1] : x->x[0]) : poly ? x->a : !apply ? p : turn ? xt : by;
+    j.b = gram ? (s.now ? x->x[1] : x->x[0]) : poly || kind == TIMES ? x->a : kind == BOTH ? x->t : kind == PAIR ? x->p[0] : turn ? by : xt;
+    j.aux = poly ? x->a : nullptr;
+    j.direct = !apply ? to : s.last ? nullptr : s.now ? x->x[0] : x->x[1];
+    j.turned = !apply ? to : s.last ? nullptr : s.now ? x->xt[0] : x->xt[1];
+    j.pitch = gram ? x->np : x->mp;
+    j.pitch_o = apply ? x->np : x->mp;
+    j.pitch_t = x->mp;
+    j.M = turn ? x->n : x->m;
+    j.N = apply && !turn ? x->n : x->m;
+    j.symmetric = !apply;
+    j.to_w = apply && s.last;
+    j.p = gram ? 0x1p-10f : poly ? kC * 0x1p-15f : kind == BOTH ? 0x1p-12f : apply ? (s.two ? 0x1p-12f : 0x1p-13f) : 0x1p-14f;
+    j.q = poly ? kB * 0x1p-1f : 0.0f;
+    j.diag = poly ? kA * 0x1p13f : 0.0f;
+    return j;
+}
+
+// The matrices, and for every launch the first blocks (tiles) of each and its first divided stages.
+struct Table {
+    const uint32_t* first;    // round_up(n, 8) words
+    const uint32_t* divided;  // ... behind them
+    const Matrix* matrix;
+    int32_t n;
+};
+// What no kernel that reads it writes: scalar loads.
+template <typename T>
+__device__ __forceinline__ const __attribute__((address_space(4))) T* constant(const T* p) {
+    return (const __attribute__((address_space(4))) T*)(uintptr_t)p;
+}
+// The matrix that `at` falls to.
+__device__ __forceinline__ int find(const uint32_t* first, int n, uint32_t at) {
+    const int lane = threadIdx.x & 63;
+    const uint32_t f = lane < n ? first[lane] : 0xFFFFFFFFu;
+    return __popcll(__ballot(f <= at)) - 1;
+}
+
+struct Start {
+    Table table;
+    int32_t nesterov;
+    float momentum, eps;
 };
 struct Products {
-    Table<Job> table;
+    Table table;
+    Step step;
     const float* lr_dev;
     f32x4* part;      // two sums of a tile for every block that divides stages
     float lr;
@@ -150,16 +195,17 @@ __device__ __forceinline__ f32x4 grad4(const void* g, int64_t i) {
         return reinterpret_cast<const f32x4*>(g)[i];
     }
 }
-__device__ __forceinline__ bool wide(const StartJob& j) {
-    return ((reinterpret_cast<uintptr_t>(j.m) | reinterpret_cast<uintptr_t>(j.g)) & 15) == 0;
+__device__ __forceinline__ bool wide(const Matrix& j) {
+    return ((reinterpret_cast<uintptr_t>(j.mom) | reinterpret_cast<uintptr_t>(j.g)) & 15) == 0;
 }
 
 template <bool BF16>
 __global__ __launch_bounds__(256) void muon_momentum_kernel(const Start a) {
     __shared__ double sums[4];
-    const StartJob& j = a.table.find(0, blockIdx.x);
-    const uint32_t block = blockIdx.x - j.first_tile;
-    const int64_t count = (int64_t)j.rows * j.cols;
+    const int at = find(a.table.first, a.table.n, blockIdx.x);
+    const Matrix& j = a.table.matrix[at];
+    const uint32_t block = blockIdx.x - a.table.first[at];
+    const int64_t count = (int64_t)j.m * j.n;
     double sum = 0.0;
     const int64_t vecs = wide(j) ? count / 4 : 0, stride = (int64_t)j.parts * 256;
     constexpr int U = 4;  // pieces in flight a thread
@@ -168,7 +214,7 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const Start a) {
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             const int64_t at = i + k * stride < vecs ? i + k * stride : i;
-            m[k] = reinterpret_cast<const f32x4*>(j.m)[at];
+            m[k] = reinterpret_cast<const f32x4*>(j.mom)[at];
             g[k] = grad4<BF16>(j.g, at);
         }
 #pragma unroll
@@ -180,12 +226,12 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const Start a) {
                 const double u = a.nesterov ? g[k][e] + a.momentum * m[k][e] : m[k][e];
                 sum += u * u;
             }
-            reinterpret_cast<f32x4*>(j.m)[i + k * stride] = m[k];
+            reinterpret_cast<f32x4*>(j.mom)[i + k * stride] = m[k];
         }
     }
     for (int64_t i = vecs * 4 + (int64_t)block * 256 + threadIdx.x; i < count; i += stride) {
-        const float g = grad_at<BF16>(j.g, i), m = a.momentum * j.m[i] + g;
-        j.m[i] = m;
+        const float g = grad_at<BF16>(j.g, i), m = a.momentum * j.mom[i] + g;
+        j.mom[i] = m;
         const double u = a.nesterov ? g + a.momentum * m : m;
         sum += u * u;
     }
@@ -202,8 +248,13 @@ template <bool BF16>
 __global__ __launch_bounds__(256) void muon_start_kernel(const Start a) {
     __shared__ float tile[64][65];
     __shared__ double sums[4];
-    const StartJob& j = a.table.find(1, blockIdx.x);
-    const uint32_t block = blockIdx.x - j.first;
+    const int at = find(a.table.divided, a.table.n, blockIdx.x);
+    const Matrix& j = a.table.matrix[at];
+    const uint32_t block = blockIdx.x - a.table.divided[at];
+    // w is rows x cols: `direct` has its rows, `turned` its columns
+    const int32_t rows = j.tall ? j.n : j.m, cols = j.tall ? j.m : j.n;
+    uint8_t *const direct = j.tall ? j.xt[0] : j.x[0], *const turned = j.tall ? j.x[0] : j.xt[0];
+    const uint32_t pitch_d = j.tall ? j.mp : j.np, pitch_t = j.tall ? j.np : j.mp;
     const int tid = threadIdx.x;
     double sum = tid < (int)j.parts ? j.norm[tid] : 0.0;
 #pragma unroll
@@ -211,28 +262,28 @@ __global__ __launch_bounds__(256) void muon_start_kernel(const Start a) {
     if ((tid & 63) == 0) sums[tid >> 6] = sum;
     __syncthreads();
     const float inv = (float)((double)kXScale / (sqrt((sums[0] + sums[1]) + (sums[2] + sums[3])) + (double)a.eps));
-    const uint32_t tiles = (uint32_t)(j.cols + 63) / 64;
+    const uint32_t tiles = (uint32_t)(cols + 63) / 64;
     const int32_t r0 = (int32_t)(block / tiles) * 64, c0 = (int32_t)(block % tiles) * 64;
-    const bool fours = j.cols % 4 == 0 && wide(j);
+    const bool fours = cols % 4 == 0 && wide(j);
     // thread (r, 8 values): two passes of 32 rows
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
         const int r = 32 * p + tid / 8, c = tid % 8 * 8;
-        const int64_t i = (int64_t)(r0 + r) * j.cols + c0 + c;
+        const int64_t i = (int64_t)(r0 + r) * cols + c0 + c;
         float v[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             f32x4 m = {0.0f, 0.0f, 0.0f, 0.0f}, g = m;
             if (fours) {
-                if (r0 + r < j.rows && c0 + c + 4 * h < j.cols) {
-                    m = *reinterpret_cast<const f32x4*>(j.m + i + 4 * h);
+                if (r0 + r < rows && c0 + c + 4 * h < cols) {
+                    m = *reinterpret_cast<const f32x4*>(j.mom + i + 4 * h);
                     if (a.nesterov) g = grad4<BF16>(j.g, i / 4 + h);
                 }
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (r0 + r < j.rows && c0 + c + 4 * h + e < j.cols) {
-                        m[e] = j.m[i + 4 * h + e];
+                    if (r0 + r < rows && c0 + c + 4 * h + e < cols) {
+                        m[e] = j.mom[i + 4 * h + e];
                         if (a.nesterov) g[e] = grad_at<BF16>(j.g, i + 4 * h + e);
                     }
             }
@@ -242,7 +293,7 @@ __global__ __launch_bounds__(256) void muon_start_kernel(const Start a) {
                 tile[r][c + 4 * h + e] = v[4 * h + e];
             }
         }
-        if (r0 + r < j.rows && c0 + c < (j.cols + 31) / 32 * 32) put8(j.direct + (r0 + r) * (int64_t)j.pitch_d + place(c0 + c), v);
+        if (r0 + r < rows && c0 + c < (cols + 31) / 32 * 32) put8(direct + (r0 + r) * (int64_t)pitch_d + place(c0 + c), v);
     }
     __syncthreads();
     // eight lanes write the 128 bytes of 32 values: leading halves of 8 each, then trailing ones
@@ -252,8 +303,8 @@ __global__ __launch_bounds__(256) void muon_start_kernel(const Start a) {
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = tile[r + e][c];
-        if (c0 + c < j.cols && r0 + r < (j.rows + 31) / 32 * 32)
-            put_half8(j.turned + (c0 + c) * (int64_t)j.pitch_t + place(r0 + r), v, tid & 4);
+        if (c0 + c < cols && r0 + r < (rows + 31) / 32 * 32)
+            put_half8(turned + (c0 + c) * (int64_t)pitch_t + place(r0 + r), v, tid & 4);
     }
 }
 
@@ -293,16 +344,19 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ?
         end = (uint32_t)((uint64_t)(block + 1) * a.stages / a.blocks);
     }
     while (u < end) {
-        const Job& j = FINISH || whole ? a.table.find(0, block) : a.table.find(1, u);
+        const int at = FINISH || whole ? find(a.table.first, a.table.n, block) : find(a.table.divided, a.table.n, u);
+        const auto* const x = constant(a.table.matrix + at);
+        const Job j = job_of(x, a.step);
+        const uint32_t first_tile = *constant(a.table.first + at), first_stage = *constant(a.table.divided + at);
         const uint32_t stages = j.pitch / 128;
-        const uint32_t skip = a.whole > j.first_tile ? a.whole - j.first_tile : 0;  // of its tiles, those with a block of their own
+        const uint32_t skip = a.whole > first_tile ? a.whole - first_tile : 0;  // of its tiles, those with a block of their own
         uint32_t tile, s0 = 0, s1 = stages;
         if (FINISH || whole) {
-            tile = block - j.first_tile;
+            tile = block - first_tile;
             u = end;
         } else {
-            tile = (u - j.first) / stages;
-            s0 = u - j.first - tile * stages;
+            tile = (u - first_stage) / stages;
+            s0 = u - first_stage - tile * stages;
             s1 = end - u < stages - s0 ? s0 + (end - u) : stages;
             u += s1 - s0;
             tile += skip;
@@ -323,7 +377,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ?
                 for (int v = 0; v < 16; ++v) acc[i][t][v] = 0.0f;
         if constexpr (FINISH) {
             // the blocks of the tile's first and last stage
-            const uint64_t first = (uint64_t)j.first + (uint64_t)(tile - skip) * stages;
+            const uint64_t first = (uint64_t)first_stage + (uint64_t)(tile - skip) * stages;
             const uint32_t b0 = (uint32_t)(((first + 1) * a.blocks + a.stages - 1) / a.stages) - 1;
             const uint32_t b1 = (uint32_t)(((first + stages) * a.blocks + a.stages - 1) / a.stages) - 1;
             if (b0 == b1) return;  // its product wrote it
@@ -346,7 +400,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ?
             typename Loop::RowsB rb;
             ra.init(j.a, m0, j.M, j.pitch, wave, lane, Loop::copy_seg(wave, lane));
             rb.init(j.b, n0, j.N, j.pitch, wave, lane, Loop::copy_seg(wave, lane));
-            Loop::run(ra, rb, smem, (int)s0, (int)s1, j.pitch, wave, lane, acc);
+            Loop::run(ra, rb, smem, (int)s0, (int)s1, (int)(s1 - s0), j.pitch, wave, lane, acc);
             if (s1 - s0 < stages) {
                 f32x4* dst = a.part + ((int64_t)(2 * block + (s0 == 0)) * QUADS * Loop::WAVES + wave) * 64 + lane;
 #pragma unroll
@@ -366,9 +420,9 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ?
         const int wm = wave / WAVES_N, wn = wave % WAVES_N, half = lane >> 5, l32 = lane & 31;
         constexpr int CG = Loop::WN / 8, RPP = 64 / CG;
         const int32_t Np = (j.N + 31) / 32 * 32, Mp = (j.M + 31) / 32 * 32;
-        const float lr = j.w ? (a.lr_dev ? *a.lr_dev : a.lr) : 0.0f;
-        const float keep = 1.0f - lr * j.weight_decay, move = -lr * j.scale * (1.0f / kXScale);
-        const bool even = j.N % 4 == 0 && (reinterpret_cast<uintptr_t>(j.w) & 15) == 0;
+        const float lr = j.to_w ? (a.lr_dev ? *a.lr_dev : a.lr) : 0.0f;
+        const float keep = 1.0f - lr * x->weight_decay, move = -lr * x->scale * (1.0f / kXScale);
+        const bool even = j.N % 4 == 0 && (reinterpret_cast<uintptr_t>(x->w) & 15) == 0;
         const bool turn = j.turned && !(j.symmetric && tm == tn);
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
@@ -389,10 +443,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ?
                 float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
                 const bool in = row < j.M && col < Np;
                 if (j.aux) {
-                    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                    if (in) get8(j.aux + (int64_t)row * j.pitch_o + place(col), x);
+                    float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                    if (in) get8(j.aux + (int64_t)row * j.pitch_o + place(col), y);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = j.p * v[e] + j.q * x[e] + (row == col + e && row < j.M ? j.diag : 0.0f);
+                    for (int e = 0; e < 8; ++e) v[e] = j.p * v[e] + j.q * y[e] + (row == col + e && row < j.M ? j.diag : 0.0f);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] *= j.p;
@@ -402,21 +456,27 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ?
                     s[0] = f32x4{v[0], v[1], v[2], v[3]};
                     s[1] = f32x4{v[4], v[5], v[6], v[7]};
                 }
-                if (j.w && row < j.M) {
-                    float* w = j.w + (int64_t)row * j.N + col;
-                    if (even) {
+                if (j.to_w && even && row < j.M) {
+                    float* w = x->w + (int64_t)row * j.N + col;
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            if (col + 4 * h < j.N) {
-                                f32x4 x = *reinterpret_cast<f32x4*>(w + 4 * h);
+                    for (int h = 0; h < 2; ++h)
+                        if (col + 4 * h < j.N) {
+                            f32x4 y = *reinterpret_cast<f32x4*>(w + 4 * h);
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) x[e] = keep * x[e] + move * v[4 * h + e];
-                                *reinterpret_cast<f32x4*>(w + 4 * h) = x;
-                            }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (col + e < j.N) w[e] = keep * w[e] + move * v[e];
+                            for (int e = 0; e < 4; ++e) y[e] = keep * y[e] + move * v[4 * h + e];
+                            *reinterpret_cast<f32x4*>(w + 4 * h) = y;
+                        }
+                }
+            }
+            if (j.to_w && !even) {  // rows begin anywhere: a value a lane, side by side (p of it is still to come: no aux here)
+                constexpr int ROWS = Loop::WN < 64 ? 64 / Loop::WN : 1, COLS = Loop::WN < 64 ? Loop::WN : 64;
+#pragma unroll 4
+                for (int k = 0; k < 32 / ROWS * (Loop::WN / COLS); ++k) {
+                    const int r = k / (Loop::WN / COLS) * ROWS + lane / COLS, c = k % (Loop::WN / COLS) * COLS + lane % COLS;
+                    const int32_t n = n0 + wn * Loop::WN + c;
+                    if (row0 + r < j.M && n < j.N) {
+                        float* const w = x->w + (int64_t)(row0 + r) * j.N + n;
+                        *w = keep * *w + move * (j.p * stage[r * PITCH + c]);
                     }
                 }
             }
@@ -439,8 +499,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ?
     }
 }
 
-// What a product costs with a tile, in units of 10 ns: a stage of a block that is one of `side` on its CU, and of one alone; bytes
-// of the sums of a block.  Measured on 4096 x 8192 x 4096 (2.46, 1.32 and 0.7 us a stage side by side) and on 512 x 3200 x 2048 (0.78
+// What a product costs with a tile, in units of 10 ns: a stage of a block that is one of `side` on its CU, and of one alone; adding a
+// part of a divided tile.  Measured on 4096 x 8192 x 4096 (2.46, 1.32 and 0.7 us a stage side by side) and on 512 x 3200 x 2048 (0.78
 // and 0.44 us alone, 128 and 64).
 struct TileCost {
     int tile, side, busy, alone, part;
@@ -453,24 +513,26 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 int64_t part_bytes(const TileCost& c, int64_t blocks) { return blocks * 2 * c.tile * c.tile * 4; }
 
 
-// The jobs of a launch, and how they are run.
+uint64_t job_tiles(const Matrix& x, const Step& step, int tile) {
+    const uint64_t m = tiles_of(x.m, tile);
+    return step.kind == APPLY ? m * tiles_of(x.n, tile) : m * (m + 1) / 2;
+}
+
+// How a launch is run: a block a tile for `whole` of its tiles, `blocks` for the stages of the rest.
 struct Plan {
+    Step step;
     int tile;
-    uint32_t tiles, whole, stages, blocks;  // a block a tile for `whole` of them, `blocks` for the stages of the rest
-};
-struct Launch : Plan {
-    Job job[kMuonMatrices];
-    int n;
+    uint32_t tiles, whole, stages, blocks;
 };
 
 // The tile, and how many tiles have a block of their own: whatever ends first by the costs above.
-void plan(Launch& a) {
+Plan plan_of(const Matrix* x, int count, const Step& step) {
+    Plan a = {step, 0, 0, 0, 0, 0};
     double least = 1e300;
     for (const TileCost& c : kTiles) {
         uint64_t tiles = 0, stages = 0, longest = 0;
-        for (int i = 0; i < a.n; ++i) {
-            const uint64_t m = tiles_of(a.job[i].M, c.tile), n = tiles_of(a.job[i].N, c.tile), s = a.job[i].pitch / 128;
-            const uint64_t t = a.job[i].symmetric ? m * (m + 1) / 2 : m * n;
+        for (int i = 0; i < count; ++i) {
+            const uint64_t s = (step.kind == GRAM ? x[i].np : x[i].mp) / 128, t = job_tiles(x[i], step, c.tile);
             tiles += t;
             stages += t * s;
             longest = longest > s ? longest : s;
@@ -503,29 +565,26 @@ void plan(Launch& a) {
             }
         }
     }
-    uint32_t stage = 0, tile = 0;
-    for (int i = 0; i < a.n; ++i) {
-        Job& j = a.job[i];
-        const uint32_t m = (uint32_t)tiles_of(j.M, a.tile), n = (uint32_t)tiles_of(j.N, a.tile);
-        const uint32_t t = j.symmetric ? m * (m + 1) / 2 : m * n;
-        j.first = stage;
-        j.first_tile = tile;
-        const uint32_t skip = a.whole <= tile ? 0 : std::min(a.whole - tile, t);
-        tile += t;
-        stage += (t - skip) * (j.pitch / 128);
+    uint64_t before = 0;
+    for (int i = 0; i < count; ++i) {
+        const uint64_t t = job_tiles(x[i], step, a.tile), skip = a.whole <= before ? 0 : std::min(a.whole - before, t);
+        before += t;
+        a.stages += (uint32_t)((t - skip) * ((step.kind == GRAM ? x[i].np : x[i].mp) / 128));
     }
-    a.stages = stage;
+    return a;
 }
 
-template <bool FINISH>
-hipError_t launch_tiles(const Products& a, int tile, uint32_t blocks, hipStream_t s) {
-    if (tile == 256)
-        hipLaunchKernelGGL((muon_product_kernel<256, 2, 4, 2, FINISH>), dim3(blocks), dim3(512), 0, s, a);
-    else if (tile == 128)
-        hipLaunchKernelGGL((muon_product_kernel<128, 2, 2, 2, FINISH>), dim3(blocks), dim3(256), 0, s, a);
-    else
-        hipLaunchKernelGGL((muon_product_kernel<64, 2, 2, 3, FINISH>), dim3(blocks), dim3(256), 0, s, a);
+template <int BT, int WAVES_M, int WAVES_N, int STAGES>
+hipError_t launch_tile(const Products& a, const Plan& p, hipStream_t s) {
+    const dim3 threads(64 * WAVES_M * WAVES_N);
+    hipLaunchKernelGGL((muon_product_kernel<BT, WAVES_M, WAVES_N, STAGES, false>), dim3(p.whole + p.blocks), threads, 0, s, a);
+    if (p.blocks) hipLaunchKernelGGL((muon_product_kernel<BT, WAVES_M, WAVES_N, STAGES, true>), dim3(p.tiles - p.whole), threads, 0, s, a);
     return hipGetLastError();
+}
+
+hipError_t launch_products(const Products& a, const Plan& p, hipStream_t s) {
+    if (p.tile == 256) return launch_tile<256, 2, 4, 2>(a, p, s);
+    return p.tile == 128 ? launch_tile<128, 2, 2, 2>(a, p, s) : launch_tile<64, 2, 2, 3>(a, p, s);
 }
 
 // Words on their way into the workspace, some 4000 bytes a launch.
@@ -552,164 +611,69 @@ struct Writer {
     }
 };
 
-// Words of the table of n jobs.
-template <typename T>
-int64_t table_words(int n) {
-    static_assert(sizeof(T) % 8 == 0, "pointers lie at multiples of 8");
-    return 2 * round_up(n, 8) + n * (int64_t)sizeof(T) / 4;
+// The launches of so many steps, in order.
+template <typename F>
+void each_step(int steps, F f) {
+    for (int now = 0; steps > 0; now ^= 1) {
+        const int two = steps > 1;
+        steps -= two ? 2 : 1;
+        f(Step{GRAM, 0, 0, now, 0});
+        f(Step{POLY, 0, 0, now, 0});
+        if (two) {
+            f(Step{TIMES, 0, 0, now, 0});
+            f(Step{BOTH, 0, 0, now, 0});
+            f(Step{POLY, 1, 0, now, 0});
+            f(Step{PAIR, 1, 0, now, 0});
+        }
+        f(Step{APPLY, 0, two, now, steps == 0});
+    }
 }
+constexpr int kMostLaunches = kMuonSteps / 2 * 7;
 
-template <typename T>
-Table<T> table_at(const void* p, int n) {
-    const uint32_t* w = static_cast<const uint32_t*>(p);
-    const int64_t each = round_up(n, 8);
-    return {{w, w + each}, reinterpret_cast<const T*>(w + 2 * each), n};
-}
-
-template <typename T>
-void write_table(Writer& to, const T* job, int n) {
-    const uint32_t most = 0xFFFFFFFFu;
-    for (int64_t i = 0; i < round_up(n, 8); ++i) to.put(i < n ? &job[i].first_tile : &most, 1);
-    for (int64_t i = 0; i < round_up(n, 8); ++i) to.put(i < n ? &job[i].first : &most, 1);
-    to.put(job, n * (int)sizeof(T) / 4);
-}
-
-// A matrix in the workspace: its sides, m <= n, and where its arrays begin (bytes).
-struct Place {
-    int64_t m, n, mp, np;  // mp, np: bytes of a row of m (n) values
-    int64_t x[2], xt[2], a, t, p[3], norm, end;
-    bool tall;
+// The workspace of a group: the matrices' arrays, the most sums of divided tiles (three steps have every kind of launch), the table.
+struct Layout {
+    Matrix x[kMuonMatrices];
+    int64_t part, table, end;
 };
 
-Place place_of(const tbn_muon_tensor& t, int64_t at) {
-    Place p;
-    p.tall = t.rows > t.cols;
-    p.m = p.tall ? t.cols : t.rows;
-    p.n = p.tall ? t.rows : t.cols;
-    p.mp = round_up(p.m, 32) * 4;
-    p.np = round_up(p.n, 32) * 4;
+void lay_out(const tbn_muon_tensor* t, int n, uint8_t* ws, Layout* l) {
+    int64_t at = 0;
     auto take = [&](int64_t bytes) {
-        const int64_t was = at;
+        uint8_t* const was = ws + at;
         at += round_up(bytes, 256);
         return was;
     };
-    for (int i = 0; i < 2; ++i) p.x[i] = take(p.m * p.np), p.xt[i] = take(p.n * p.mp);
-    p.a = take(p.m * p.mp);
-    p.t = take(p.m * p.mp);
-    for (int64_t& b : p.p) b = take(p.m * p.mp);
-    p.norm = take(256 * 8);
-    p.end = at;
-    return p;
-}
-
-// C = A B^T of rows of k values in `bytes`, for symmetric C (m x m) or any (m x n).
-Job product(const uint8_t* a, const uint8_t* b, int64_t bytes, int64_t m, int64_t n, bool symmetric, float p) {
-    Job j = {};
-    j.a = a;
-    j.b = b;
-    j.pitch = (uint32_t)bytes;
-    j.M = (int32_t)m;
-    j.N = (int32_t)n;
-    j.symmetric = symmetric;
-    j.p = p;
-    return j;
-}
-
-// ... a symmetric one of symmetric factors of this matrix, into `to`.
-Job square(const Place& at, uint8_t* ws, int64_t a, int64_t b, int64_t to, float p) {
-    Job j = product(ws + a, ws + b, at.mp, at.m, at.m, true, p);
-    j.direct = j.turned = ws + to;
-    j.pitch_o = j.pitch_t = (uint32_t)at.mp;
-    return j;
-}
-
-// The launches of a group's steps, in order, each given to `run`.
-template <typename F>
-hipError_t muon_launches(const tbn_muon_tensor* t, int n, const Place* at, uint8_t* ws, int steps, F run) {
-    Launch l;
-    hipError_t e;
-    auto begin = [&] { l.n = 0; };
-    auto end = [&] {
-        plan(l);
-        return run(l);
-    };
-    for (int now = 0; steps > 0; now ^= 1) {
-        const bool two = steps > 1;
-        steps -= two ? 2 : 1;
-        begin();
-        for (int i = 0; i < n; ++i) {
-            const Place& p = at[i];
-            Job& j = l.job[l.n++] = product(ws + p.x[now], ws + p.x[now], p.np, p.m, p.m, true, 0x1p-10f);  // 2^24 to 2^14
-            j.direct = j.turned = ws + p.a;
-            j.pitch_o = j.pitch_t = (uint32_t)p.mp;
-        }
-        if ((e = end()) != hipSuccess) return e;
-        for (int k = 0; k < (two ? 2 : 1); ++k) {
-            begin();
-            for (int i = 0; i < n; ++i) {
-                const Place& p = at[i];
-                Job& j = l.job[l.n++] = square(p, ws, p.a, p.a, p.p[k], kC * 0x1p-15f);  // 2^28 and 2^14 to 2^13
-                j.aux = ws + p.a;
-                j.q = kB * 0.5f;
-                j.diag = kA * 0x1p13f;
-            }
-            if ((e = end()) != hipSuccess) return e;
-            if (!two) break;
-            begin();
-            for (int i = 0; i < n; ++i) {
-                const Place& p = at[i];
-                // P A; after the second step the product of both P
-                l.job[l.n++] = k == 0 ? square(p, ws, p.p[0], p.a, p.t, 0x1p-14f) : square(p, ws, p.p[1], p.p[0], p.p[2], 0x1p-14f);
-            }
-            if ((e = end()) != hipSuccess) return e;
-            if (k) break;
-            begin();
-            for (int i = 0; i < n; ++i) l.job[l.n++] = square(at[i], ws, at[i].p[0], at[i].t, at[i].a, 0x1p-12f);  // P A P
-            if ((e = end()) != hipSuccess) return e;
-        }
-        begin();
-        for (int i = 0; i < n; ++i) {
-            const Place& p = at[i];
-            const uint8_t *by = ws + p.p[two ? 2 : 0], *xt = ws + p.xt[now];
-            const float down = two ? 0x1p-12f : 0x1p-13f;
-            const bool last = steps == 0, turn = last && p.tall;  // the last one along the rows of w
-            Job& j = l.job[l.n++] = turn ? product(xt, by, p.mp, p.n, p.m, false, down) : product(by, xt, p.mp, p.m, p.n, false, down);
-            if (last) {
-                j.w = t[i].w;
-                j.weight_decay = t[i].weight_decay;
-                j.scale = t[i].scale;
-            } else {
-                j.direct = ws + p.x[now ^ 1];
-                j.turned = ws + p.xt[now ^ 1];
-                j.pitch_o = (uint32_t)p.np;
-                j.pitch_t = (uint32_t)p.mp;
-            }
-        }
-        if ((e = end()) != hipSuccess) return e;
-    }
-    return hipSuccess;
-}
-
-// The most bytes of sums of divided tiles: three steps have every kind of launch.
-int64_t part_bytes(const tbn_muon_tensor* t, int n, const Place* at) {
-    int64_t most = 0;
-    (void)muon_launches(t, n, at, nullptr, 3, [&](const Launch& l) {
-        most = std::max(most, (int64_t)l.blocks * 2 * l.tile * l.tile * 4);
-        return hipSuccess;
-    });
-    return round_up(most, 256);
-}
-
-constexpr int kMostLaunches = kMuonSteps / 2 * 7;
-
-int64_t place_all(const tbn_muon_tensor* t, int n, Place* at) {
-    int64_t end = 0;
     for (int i = 0; i < n; ++i) {
-        at[i] = place_of(t[i], end);
-        end = at[i].end;
+        Matrix& x = l->x[i];
+        x.w = t[i].w;
+        x.mom = t[i].m;
+        x.g = t[i].g;
+        x.tall = t[i].rows > t[i].cols;
+        x.m = x.tall ? t[i].cols : t[i].rows;
+        x.n = x.tall ? t[i].rows : t[i].cols;
+        x.mp = (uint32_t)round_up(x.m, 32) * 4;
+        x.np = (uint32_t)round_up(x.n, 32) * 4;
+        x.weight_decay = t[i].weight_decay;
+        x.scale = t[i].scale;
+        const int64_t parts = ((int64_t)x.m * x.n + 4095) / 4096;
+        x.parts = (uint32_t)(parts < 256 ? parts : 256);
+        for (int k = 0; k < 2; ++k) x.x[k] = take((int64_t)x.m * x.np), x.xt[k] = take((int64_t)x.n * x.mp);
+        x.a = take((int64_t)x.m * x.mp);
+        x.t = take((int64_t)x.m * x.mp);
+        for (uint8_t*& p : x.p) p = take((int64_t)x.m * x.mp);
+        x.norm = reinterpret_cast<double*>(take(256 * 8));
     }
-    return end;
+    l->part = at;
+    int64_t most = 0;
+    each_step(3, [&](const Step& step) {
+        const Plan p = plan_of(l->x, n, step);
+        most = std::max(most, (int64_t)p.blocks * 2 * p.tile * p.tile * 4);
+    });
+    l->table = l->part + round_up(most, 256);
+    l->end = l->table + n * (int64_t)sizeof(Matrix) + (kMostLaunches + 1) * 2 * round_up(n, 8) * 4;
 }
+
+static_assert(sizeof(Matrix) % 8 == 0, "one behind the other");
 
 }  // namespace
 
@@ -724,58 +688,48 @@ int muon_group(const tbn_muon_tensor* t, int n) {
 }
 
 int64_t muon_group_bytes(const tbn_muon_tensor* t, int n) {
-    Place at[kMuonMatrices];
-    const int64_t end = place_all(t, n, at);
-    return end + part_bytes(t, n, at) + (table_words<StartJob>(n) + kMostLaunches * table_words<Job>(n)) * 4;
+    Layout l;
+    lay_out(t, n, nullptr, &l);
+    return l.end;
 }
 
 hipError_t launch_muon_group(const tbn_muon_tensor* t, int n, const MuonHyper& h, uint8_t* ws, hipStream_t s) {
-    Place at[kMuonMatrices];
-    const int64_t end = place_all(t, n, at);
-    f32x4* const part = reinterpret_cast<f32x4*>(ws + end);
-    uint32_t* table = reinterpret_cast<uint32_t*>(ws + end + part_bytes(t, n, at));
+    Layout l;
+    lay_out(t, n, ws, &l);
     hipError_t e;
 
     // the tables of all launches, then the launches
-    StartJob start[kMuonMatrices] = {};
-    uint32_t blocks = 0, tiles = 0;
-    for (int i = 0; i < n; ++i) {
-        StartJob& j = start[i];
-        const Place& p = at[i];
-        j.m = t[i].m;
-        j.g = t[i].g;
-        j.rows = t[i].rows;
-        j.cols = t[i].cols;
-        j.direct = ws + (p.tall ? p.xt[0] : p.x[0]);
-        j.turned = ws + (p.tall ? p.x[0] : p.xt[0]);
-        j.pitch_d = (uint32_t)(p.tall ? p.mp : p.np);
-        j.pitch_t = (uint32_t)(p.tall ? p.np : p.mp);
-        j.norm = reinterpret_cast<double*>(ws + p.norm);
-        const int64_t parts = ((int64_t)j.rows * j.cols + 4095) / 4096;
-        j.parts = (uint32_t)(parts < 256 ? parts : 256);
-        j.first_tile = blocks;  // of the first kernel
-        j.first = tiles;        // of the second
-        blocks += j.parts;
-        tiles += (uint32_t)(tiles_of(j.rows, 64) * tiles_of(j.cols, 64));
-    }
-    Writer to(table, s);
-    write_table(to, start, n);
+    const int64_t each = round_up(n, 8);
+    Writer to(ws + l.table, s);
+    to.put(l.x, n * (int)sizeof(Matrix) / 4);
+    auto put_firsts = [&](auto of) {  // running sums over the matrices
+        uint32_t sum = 0;
+        for (int i = 0; i < each; ++i) {
+            to.put(&sum, 1);
+            if (i < n) sum += of(i);
+        }
+        return sum;
+    };
+    const uint32_t blocks = put_firsts([&](int i) { return l.x[i].parts; });
+    const uint32_t tiles = put_firsts([&](int i) { return (uint32_t)(tiles_of(l.x[i].m, 64) * tiles_of(l.x[i].n, 64)); });
     Plan plans[kMostLaunches];
     int launches = 0;
-    e = muon_launches(t, n, at, ws, h.steps, [&](const Launch& l) {
-        write_table(to, l.job, l.n);
-        plans[launches++] = l;
-        return to.e;
+    each_step(h.steps, [&](const Step& step) {
+        const Plan p = plans[launches++] = plan_of(l.x, n, step);
+        put_firsts([&](int i) { return (uint32_t)job_tiles(l.x[i], step, p.tile); });
+        uint64_t before = 0;
+        put_firsts([&](int i) {
+            const uint64_t t = job_tiles(l.x[i], step, p.tile), skip = p.whole <= before ? 0 : std::min(p.whole - before, t);
+            before += t;
+            return (uint32_t)((t - skip) * ((step.kind == GRAM ? l.x[i].np : l.x[i].mp) / 128));
+        });
     });
     to.flush();
-    if (e != hipSuccess || (e = to.e) != hipSuccess) return e;
+    if ((e = to.e) != hipSuccess) return e;
 
-    Start st = {};
-    st.table = table_at<StartJob>(table, n);
-    st.momentum = h.momentum;
-    st.eps = h.eps;
-    st.nesterov = h.nesterov;
-    table += table_words<StartJob>(n);
+    const uint32_t* first = reinterpret_cast<const uint32_t*>(ws + l.table + n * (int64_t)sizeof(Matrix));
+    Table table = {first, first + each, reinterpret_cast<const Matrix*>(ws + l.table), n};
+    const Start st = {table, h.nesterov, h.momentum, h.eps};
     if (h.g_f32)
         hipLaunchKernelGGL((muon_momentum_kernel<false>), dim3(blocks), dim3(256), 0, s, st);
     else
@@ -789,17 +743,18 @@ hipError_t launch_muon_group(const tbn_muon_tensor* t, int n, const MuonHyper& h
 
     for (int i = 0; i < launches; ++i) {
         const Plan& p = plans[i];
+        table.first += 2 * each;
+        table.divided += 2 * each;
         Products a = {};
-        a.table = table_at<Job>(table, n);
-        a.part = part;
+        a.table = table;
+        a.step = p.step;
+        a.part = reinterpret_cast<f32x4*>(ws + l.part);
         a.lr = h.lr;
         a.lr_dev = h.lr_dev;
         a.whole = p.whole;
         a.stages = p.stages;
         a.blocks = p.blocks;
-        table += table_words<Job>(n);
-        if ((e = launch_tiles<false>(a, p.tile, p.whole + p.blocks, s)) != hipSuccess) return e;
-        if (p.blocks && (e = launch_tiles<true>(a, p.tile, p.tiles - p.whole, s)) != hipSuccess) return e;
+        if ((e = launch_products(a, p, s)) != hipSuccess) return e;
     }
     return hipSuccess;
 }

@@ -91,10 +91,10 @@ struct NtLoop {
     // Logical 16-byte segment that a lane copies of its row.
     static __device__ __forceinline__ int copy_seg(int wave, int lane) { return (lane & 7) ^ ((4 * (wave & 1)) | ((lane >> 4) & 3)); }
 
-    // Adds the products of stages s0 .. s1 - 1 to acc.  `row_bytes`: of A's rows.  Every wave of the block calls it; it ends
-    // behind a barrier, after which the LDS is free.
-    static __device__ __forceinline__ void run(const RowsA& ra, const RowsB& rb, uint8_t* smem, int s0, int s1, uint32_t row_bytes, int wave,
-                                               int lane, Acc (&acc)[TM][TN]) {
+    // Adds the products of stages s0 .. s1 - 1 to acc.  `row_bytes`: of A's rows.  Every wave of the block calls it, with the same
+    // `rounds` (of barriers), at least s1 - s0; it ends behind a barrier, after which the LDS is free.
+    static __device__ __forceinline__ void run(const RowsA& ra, const RowsB& rb, uint8_t* smem, int s0, int s1, int rounds, uint32_t row_bytes,
+                                               int wave, int lane, Acc (&acc)[TM][TN]) {
         const int wm = wave / WAVES_N, wn = wave % WAVES_N;
         const int half = lane >> 5, l32 = lane & 31;
         const int sw = (l32 >> 1) & 7;
@@ -122,12 +122,13 @@ struct NtLoop {
             if (s < n) issue(s, 0, COPIES);
         int cslot = 0;
         const int arow = (wm * WM + l32) * 128, brow = (wn * WN + l32) * 128 + BM * 128;
-        for (int s = 0; s < n; ++s) {
+        for (int s = 0; s < rounds; ++s) {
             if (s + STAGES - 2 < n)
                 wait_vmcnt((STAGES - 2) * COPIES);
             else
                 wait_vmcnt(0);
             __syncthreads();
+            if (s >= n) continue;
             const uint8_t* st = smem + cslot * STAGE;
             cslot = cslot + 1 == STAGES ? 0 : cslot + 1;
             u32x4 a[2][Op::PARTS][TM], b[2][Op::PARTS][TN];
@@ -164,6 +165,46 @@ struct NtLoop {
         __syncthreads();
     }
 };
+
+// A block of GROUPS groups of waves, each with a part of the stages and an LDS ring of its own, for tiles that are too few to fill the
+// GPU: the first group's sums plus the others', in order.  Each group brings at most BYTES of LDS; ends behind a barrier.
+template <int GROUPS, class Loop>
+__device__ __forceinline__ void nt_join(uint8_t* smem, int group, int wave, int lane, typename Loop::Acc (&acc)[Loop::TM][Loop::TN]) {
+    if constexpr (GROUPS > 1) {
+        constexpr int QUADS = Loop::TM * Loop::TN * 4;
+        static_assert((GROUPS - 1) * QUADS * 16 * 64 * Loop::WAVES <= GROUPS * Loop::BYTES, "sums fit in the rings");
+        typedef typename Loop::Acc Acc;
+        typedef decltype(Acc{}[0] + Acc{}[0]) T;
+        typedef T Quad __attribute__((ext_vector_type(4)));
+        Quad* const at = reinterpret_cast<Quad*>(smem) + wave * 64 + lane;
+        if (group) {
+#pragma unroll
+            for (int i = 0; i < Loop::TM; ++i)
+#pragma unroll
+                for (int t = 0; t < Loop::TN; ++t)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        at[(((group - 1) * Loop::TM + i) * Loop::TN * 4 + t * 4 + g) * Loop::WAVES * 64] =
+                            Quad{acc[i][t][4 * g], acc[i][t][4 * g + 1], acc[i][t][4 * g + 2], acc[i][t][4 * g + 3]};
+        }
+        __syncthreads();
+        if (!group) {
+#pragma unroll
+            for (int k = 0; k < GROUPS - 1; ++k)
+#pragma unroll
+                for (int i = 0; i < Loop::TM; ++i)
+#pragma unroll
+                    for (int t = 0; t < Loop::TN; ++t)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const Quad v = at[((k * Loop::TM + i) * Loop::TN * 4 + t * 4 + g) * Loop::WAVES * 64];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[i][t][4 * g + e] += v[e];
+                        }
+        }
+        __syncthreads();
+    }
+}
 
 // Tile (m, n) of the work index w: bands of 8 tile rows, so that the blocks that an XCD runs side by side share rows of
 // both operands in its L2.

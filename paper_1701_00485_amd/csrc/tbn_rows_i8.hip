@@ -104,59 +104,59 @@ __global__ __launch_bounds__(256) void rows_i8_kernel(const void* __restrict__ x
 }
 
 // ---- what follows the sums ---------------------------------------------------------------
-// y of 8 consecutive channels n0 .. n0 + 7 of row m from their sums, the row's and the channels' scales and biases; `whole`: they all
-// exist and lie 16-byte aligned.
+// y of channel n of row m from its sum, the row's and the channel's scale and its bias.
+__device__ __forceinline__ void finish1(const RowsI8Args& a, int64_t m, int32_t n, float s, float sx, float sw, float bias) {
+    const int64_t o = m * a.n + n;
+    float v = s * (sx * sw) + bias;
+    if (a.residual) v += a.y_f32 ? reinterpret_cast<const float*>(a.residual)[o] : bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(a.residual)[o]);
+    if (a.relu) v = v > 0.0f || v != v ? v : 0.0f;
+    if (a.y_f32)
+        reinterpret_cast<float*>(a.y)[o] = v;
+    else
+        reinterpret_cast<uint16_t*>(a.y)[o] = (uint16_t)f32_to_bf16_bits(v);
+}
+
+// ... of 8 consecutive channels, 16-byte aligned (n % 8 == 0).
 __device__ __forceinline__ void finish8(const RowsI8Args& a, int64_t m, int32_t n0, const float (&s)[8], float sx, const float (&sw)[8],
-                                        const float (&bias)[8], bool whole) {
+                                        const float (&bias)[8]) {
     const int64_t o = m * a.n + n0;
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = s[e] * (sx * sw[e]) + bias[e];
-    if (a.residual) {
-        if (whole && !a.y_f32) {
-            const u32x4 r = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.residual) + o);
+    if (a.residual && a.y_f32) {
+        const f32x4* r = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.residual) + o);
+        const f32x4 lo = r[0], hi = r[1];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[2 * e] += bf16_bits_to_f32(r[e] & 0xFFFFu), v[2 * e + 1] += __uint_as_float(r[e] & 0xFFFF0000u);
-        } else {
+        for (int e = 0; e < 4; ++e) v[e] += lo[e], v[4 + e] += hi[e];
+    } else if (a.residual) {
+        const u32x4 r = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.residual) + o);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (n0 + e < a.n)
-                    v[e] += a.y_f32 ? reinterpret_cast<const float*>(a.residual)[o + e]
-                                    : bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(a.residual)[o + e]);
-        }
+        for (int e = 0; e < 4; ++e) v[2 * e] += bf16_bits_to_f32(r[e] & 0xFFFFu), v[2 * e + 1] += __uint_as_float(r[e] & 0xFFFF0000u);
     }
     if (a.relu) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = v[e] > 0.0f || v[e] != v[e] ? v[e] : 0.0f;
     }
-    if (whole && a.y_f32) {
+    if (a.y_f32) {
         f32x4* p = reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.y) + o);
         p[0] = f32x4{v[0], v[1], v[2], v[3]};
         p[1] = f32x4{v[4], v[5], v[6], v[7]};
-    } else if (whole) {
+    } else {
         *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(a.y) + o) =
             u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (n0 + e >= a.n) break;
-            if (a.y_f32)
-                reinterpret_cast<float*>(a.y)[o + e] = v[e];
-            else
-                reinterpret_cast<uint16_t*>(a.y)[o + e] = (uint16_t)f32_to_bf16_bits(v[e]);
-        }
     }
 }
 
 // ---- many rows ---------------------------------------------------------------------------
-template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES>
-__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BM * BN >= 65536 ? 1 : BM * BN >= 16384 ? 2 : 3) void matmul_i8_kernel(const RowsI8Args a) {
+template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int GROUPS>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N * GROUPS, BM * BN >= 65536 || GROUPS > 1 ? 1 : BM * BN >= 8192 ? 2 : 3) void matmul_i8_kernel(const RowsI8Args a) {
     typedef NtLoop<BM, BN, WAVES_M, WAVES_N, STAGES, NtI8, true> Loop;
     constexpr int PITCH = Loop::WN + 4;  // of a staged row, in floats
     static_assert(Loop::BYTES >= Loop::WAVES * 32 * PITCH * 4 + (BM + 2 * BN) * 4, "staging fits in the ring");
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[Loop::BYTES];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[GROUPS * Loop::BYTES];
     const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * Loop::WAVES));
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) - group * Loop::WAVES;
     const uint32_t tiles_n = (uint32_t)((a.n + BN - 1) / BN), tiles_m = (uint32_t)((a.rows + BM - 1) / BM);
     uint32_t tm, tn;
     nt_tile((uint32_t)xcd_remap(blockIdx.x, gridDim.x), tiles_m, tiles_n, &tm, &tn);
@@ -174,13 +174,15 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BM * BN >= 65536 ? 1 : BM *
         for (int t = 0; t < Loop::TN; ++t)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][t][v] = 0;
-    Loop::run(ra, rb, smem, 0, (a.c + 127) / 128, (uint32_t)a.c, wave, lane, acc);
+    const int stages = (a.c + 127) / 128, each = (stages + GROUPS - 1) / GROUPS;
+    Loop::run(ra, rb, smem + group * Loop::BYTES, min(group * each, stages), min((group + 1) * each, stages), each, (uint32_t)a.c, wave, lane, acc);
+    nt_join<GROUPS, Loop>(smem, group, wave, lane, acc);
 
     // the tile's scales and biases, behind the waves' staging
     float* const row_scale = reinterpret_cast<float*>(smem) + Loop::WAVES * 32 * PITCH;
     float* const col_scale = row_scale + BM;
     float* const col_bias = col_scale + BN;
-    for (int i = threadIdx.x; i < BM + BN; i += 64 * Loop::WAVES) {
+    for (int i = threadIdx.x; i < BM + BN; i += 64 * Loop::WAVES * GROUPS) {
         if (i < BM) {
             row_scale[i] = m0 + i < a.rows ? a.x_scale[m0 + i] : 0.0f;
         } else {
@@ -191,6 +193,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BM * BN >= 65536 ? 1 : BM *
         }
     }
     __syncthreads();
+    if (group) return;
     // a wave turns each 32 rows of its tile in LDS and writes them with 16-byte stores
     float* stage = reinterpret_cast<float*>(smem) + wave * 32 * PITCH;
     const int wm = wave / WAVES_N, wn = wave % WAVES_N, half = lane >> 5, l32 = lane & 31;
@@ -209,6 +212,19 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BM * BN >= 65536 ? 1 : BM *
                     f32x4{(float)acc[i][t][4 * g], (float)acc[i][t][4 * g + 1], (float)acc[i][t][4 * g + 2], (float)acc[i][t][4 * g + 3]};
         __builtin_amdgcn_wave_barrier();
         const int col = n0 + wn * Loop::WN + 8 * (lane % CG);
+        if (!even) {  // rows begin anywhere: a value a lane, side by side
+            constexpr int ROWS = Loop::WN < 64 ? 64 / Loop::WN : 1, COLS = Loop::WN < 64 ? Loop::WN : 64;
+#pragma unroll 4
+            for (int k = 0; k < 32 / ROWS * (Loop::WN / COLS); ++k) {
+                const int r = k / (Loop::WN / COLS) * ROWS + lane / COLS, c = k % (Loop::WN / COLS) * COLS + lane % COLS;
+                const int64_t m = m0 + wm * Loop::WM + 32 * i + r;
+                if (m < a.rows && n0 + wn * Loop::WN + c < a.n)
+                    finish1(a, m, n0 + wn * Loop::WN + c, stage[r * PITCH + c], row_scale[wm * Loop::WM + 32 * i + r], col_scale[wn * Loop::WN + c],
+                            col_bias[wn * Loop::WN + c]);
+            }
+            __builtin_amdgcn_wave_barrier();
+            continue;
+        }
 #pragma unroll
         for (int p = 0; p < 32 / RPP; ++p) {
             const int r = p * RPP + lane / CG;
@@ -216,7 +232,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BM * BN >= 65536 ? 1 : BM *
             const f32x4* s = reinterpret_cast<const f32x4*>(stage + r * PITCH + 8 * (lane % CG));
             const f32x4 lo = s[0], hi = s[1];
             const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            if (m < a.rows && col < a.n) finish8(a, m, col, v, row_scale[wm * Loop::WM + 32 * i + r], sw, bias, even);
+            if (m < a.rows && col < a.n) finish8(a, m, col, v, row_scale[wm * Loop::WM + 32 * i + r], sw, bias);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -227,7 +243,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BM * BN >= 65536 ? 1 : BM *
 // 128 bytes of every channel a step: lane (f = l % 16, q = l / 16) reads bytes 32 q .. 32 q + 31 of channel f's as two
 // 16-byte pieces, a matrix instruction each, and of row f of x the same bytes (the order of the values in a sum of
 // integers is free).  The waves' sums meet in LDS.
-template <int NG, int WAVES>
+template <int NG, int WAVES, int DEPTH>
 __global__ __launch_bounds__(64 * WAVES) void matvec_i8_kernel(const RowsI8Args a) {
     __shared__ i32x4 sums[WAVES][NG][64];
     const int lane = threadIdx.x & 63;
@@ -244,7 +260,6 @@ __global__ __launch_bounds__(64 * WAVES) void matvec_i8_kernel(const RowsI8Args 
     i32x4 acc[NG];
 #pragma unroll
     for (int g = 0; g < NG; ++g) acc[g] = i32x4{0, 0, 0, 0};
-    constexpr int DEPTH = 2;
     i32x4 wv[DEPTH][NG][2], xv[DEPTH][2];
     auto load = [&](int d, int s) {
 #pragma unroll
@@ -285,24 +300,15 @@ __global__ __launch_bounds__(64 * WAVES) void matvec_i8_kernel(const RowsI8Args 
         for (int e = 0; e < 4; ++e) {
             const int32_t n = n0 + 16 * g + 4 * q + e;
             if (n >= a.n) break;
-            const int64_t o = (int64_t)f * a.n + n;
-            const float sw = a.scale ? a.w_scale[n] * a.scale[n] : a.w_scale[n];
-            float v = (float)t[e] * (a.x_scale[f] * sw) + (a.bias ? a.bias[n] : 0.0f);
-            if (a.residual)
-                v += a.y_f32 ? reinterpret_cast<const float*>(a.residual)[o] : bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(a.residual)[o]);
-            if (a.relu) v = v > 0.0f || v != v ? v : 0.0f;
-            if (a.y_f32)
-                reinterpret_cast<float*>(a.y)[o] = v;
-            else
-                reinterpret_cast<uint16_t*>(a.y)[o] = (uint16_t)f32_to_bf16_bits(v);
+            finish1(a, f, n, (float)t[e], a.x_scale[f], a.scale ? a.w_scale[n] * a.scale[n] : a.w_scale[n], a.bias ? a.bias[n] : 0.0f);
         }
     }
 }
 
-template <int BM, int BN, int WM, int WN, int STAGES>
+template <int BM, int BN, int WM, int WN, int STAGES, int GROUPS>
 hipError_t launch_tiles(const RowsI8Args& a, hipStream_t s) {
     const int64_t blocks = (a.rows + BM - 1) / BM * ((a.n + BN - 1) / BN);
-    hipLaunchKernelGGL((matmul_i8_kernel<BM, BN, WM, WN, STAGES>), dim3((unsigned)blocks), dim3(64 * WM * WN), 0, s, a);
+    hipLaunchKernelGGL((matmul_i8_kernel<BM, BN, WM, WN, STAGES, GROUPS>), dim3((unsigned)blocks), dim3(64 * WM * WN * GROUPS), 0, s, a);
     return hipGetLastError();
 }
 
@@ -336,21 +342,19 @@ hipError_t launch_rows_i8(const void* x, int x_f32, int64_t rows, int32_t c, int
 hipError_t launch_matmul_i8(const RowsI8Args& a, hipStream_t s) {
     if (a.rows <= 16) {
         const int64_t groups = (a.n + 15) / 16;
-#define TBN_VEC(ng) hipLaunchKernelGGL((matvec_i8_kernel<ng, 8>), dim3((unsigned)((groups + ng - 1) / ng)), dim3(512), 0, s, a)
-        if (groups >= 4 * 256)
-            TBN_VEC(4);
-        else if (groups >= 2 * 256)
+#define TBN_VEC(ng) hipLaunchKernelGGL((matvec_i8_kernel<ng, 4, 4>), dim3((unsigned)((groups + ng - 1) / ng)), dim3(256), 0, s, a)
+        if (groups >= 1024)
             TBN_VEC(2);
         else
             TBN_VEC(1);
 #undef TBN_VEC
         return hipGetLastError();
     }
-    const int64_t big = (a.rows + 255) / 256 * ((a.n + 255) / 256);
-    if (big >= 192) return launch_tiles<256, 256, 2, 4, 2>(a, s);
-    const int64_t mid = (a.rows + 127) / 128 * ((a.n + 127) / 128);
-    if (mid >= 192) return launch_tiles<128, 128, 2, 2, 2>(a, s);
-    return launch_tiles<64, 64, 2, 2, 3>(a, s);
+    auto tiles = [&](int64_t m, int64_t n) { return (a.rows + m - 1) / m * ((a.n + n - 1) / n); };
+    if (tiles(256, 256) >= 192) return launch_tiles<256, 256, 2, 4, 2, 1>(a, s);
+    if (tiles(128, 64) >= 256) return launch_tiles<128, 64, 2, 2, 3, 1>(a, s);
+    if (tiles(64, 64) > 256 || a.c <= 512) return launch_tiles<64, 64, 2, 2, 3, 1>(a, s);
+    return launch_tiles<64, 64, 2, 2, 2, 4>(a, s);
 }
 
 }  // namespace tbn
