@@ -508,28 +508,29 @@ hipError_t launch(const GluArgs& a, const uint16_t* gu, hipStream_t s) {
     if (a.rows <= 16) {
         const int64_t groups = (a.f + 15) / 16;
         const int lds = ((int)a.rows + 1) * ((a.c + 255) / 256) * 512;  // of x and a row of zeros
-#define TBN_FEW(ng, waves, staged)                                                                                              \
-    hipLaunchKernelGGL((glu_few_kernel<ng, waves, 2, staged, ACT>), dim3((unsigned)((groups + ng - 1) / ng)), dim3(64 * waves), \
+#define TBN_FEW(ng, waves, depth, staged)                                                                                           \
+    hipLaunchKernelGGL((glu_few_kernel<ng, waves, depth, staged, ACT>), dim3((unsigned)((groups + ng - 1) / ng)), dim3(64 * waves), \
                        staged ? lds : 0, s, a)
         if (a.rows <= 4 && lds <= 48 * 1024) {
             if (groups >= 1024)
-                TBN_FEW(2, 8, true);
+                TBN_FEW(2, 8, 2, true);
             else
-                TBN_FEW(1, 4, true);
+                TBN_FEW(1, 4, 2, true);
         } else if (groups >= 1024) {
-            TBN_FEW(4, 4, false);
+            TBN_FEW(4, 8, 1, false);
         } else if (groups >= 512) {
-            TBN_FEW(2, 4, false);
+            TBN_FEW(2, 4, 2, false);
         } else {
-            TBN_FEW(1, 4, false);
+            TBN_FEW(1, 4, 2, false);
         }
 #undef TBN_FEW
         return hipGetLastError();
     }
     auto tiles = [&](int64_t m, int64_t n) { return (a.rows + m - 1) / m * ((a.f + n - 1) / n); };
     if (tiles(256, 128) >= 192) return launch_tiles<256, 128, 2, 4, 4, 1, ACT>(a, s);
+    if (tiles(128, 128) >= 192) return launch_tiles<128, 128, 2, 4, 4, 1, ACT>(a, s);
     if (tiles(128, 64) >= 192) return launch_tiles<128, 64, 2, 2, 4, 1, ACT>(a, s);
-    if (tiles(64, 64) > 256 || a.c <= 256) return launch_tiles<64, 64, 2, 2, 4, 1, ACT>(a, s);
+    if (tiles(64, 64) > 256 || a.c <= 1024) return launch_tiles<64, 64, 2, 2, 4, 1, ACT>(a, s);
     if (tiles(64, 64) > 128) return launch_tiles<64, 64, 2, 2, 4, 4, ACT>(a, s);
     return launch_tiles<64, 32, 2, 1, 4, 4, ACT>(a, s);
 }

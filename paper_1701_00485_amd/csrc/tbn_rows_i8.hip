@@ -352,8 +352,9 @@ hipError_t launch_matmul_i8(const RowsI8Args& a, hipStream_t s) {
     }
     auto tiles = [&](int64_t m, int64_t n) { return (a.rows + m - 1) / m * ((a.n + n - 1) / n); };
     if (tiles(256, 256) >= 192) return launch_tiles<256, 256, 2, 4, 2, 1>(a, s);
+    if (tiles(128, 128) >= 192) return launch_tiles<128, 128, 2, 4, 4, 1>(a, s);
     if (tiles(128, 64) >= 256) return launch_tiles<128, 64, 2, 2, 3, 1>(a, s);
-    if (tiles(64, 64) > 256 || a.c <= 512) return launch_tiles<64, 64, 2, 2, 3, 1>(a, s);
+    if (tiles(64, 64) > 256 || a.c <= 1024) return launch_tiles<64, 64, 2, 2, 3, 1>(a, s);
     return launch_tiles<64, 64, 2, 2, 2, 4>(a, s);
 }
 
