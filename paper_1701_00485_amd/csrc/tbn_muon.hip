@@ -330,12 +330,13 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ?
     __shared__ __attribute__((aligned(1024))) uint8_t smem[Loop::BYTES];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    constexpr int QUADS = TM * TN * 4, UNROLL = BT >= 256 ? 1 : BT >= 128 ? 2 : 4;
+    constexpr int QUADS = TM * TN * 4, UNROLL = 4;
     // blocks below a.whole: a tile each; those behind them: an even part of the stages of the other tiles
     const bool whole = !FINISH && blockIdx.x < a.whole;
     uint32_t block, u = 0, end = 1;
+    const int strip = FINISH ? (int)(blockIdx.x % TM) : 0;  // of 32 rows of every wave
     if (FINISH) {
-        block = a.whole + blockIdx.x;
+        block = a.whole + blockIdx.x / TM;
     } else if (whole) {
         block = (uint32_t)xcd_remap(blockIdx.x, a.whole);
     } else {
@@ -368,9 +369,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ?
             nt_tile(tile, (uint32_t)(j.M + BT - 1) / BT, (uint32_t)(j.N + BT - 1) / BT, &tm, &tn);
         const int32_t m0 = (int32_t)(tm * BT), n0 = (int32_t)(tn * BT);
 
-        f32x16 acc[TM][TN];
+        constexpr int STRIPS = FINISH ? 1 : TM;
+        f32x16 acc[STRIPS][TN];
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < STRIPS; ++i)
 #pragma unroll
             for (int t = 0; t < TN; ++t)
 #pragma unroll
@@ -383,17 +385,15 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ?
             if (b0 == b1) return;  // its product wrote it
 #pragma unroll UNROLL
             for (uint32_t b = b0; b <= b1; ++b) {
-                const f32x4* src = a.part + ((int64_t)(2 * b + (b == b0)) * QUADS * Loop::WAVES + wave) * 64 + lane;
+                const f32x4* src = a.part + (((int64_t)(2 * b + (b == b0)) * QUADS + strip * TN * 4) * Loop::WAVES + wave) * 64 + lane;
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
+                for (int t = 0; t < TN; ++t)
 #pragma unroll
-                    for (int t = 0; t < TN; ++t)
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x4 v = src[(t * 4 + g) * Loop::WAVES * 64];
 #pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const f32x4 v = src[((i * TN + t) * 4 + g) * Loop::WAVES * 64];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[i][t][4 * g + e] += v[e];
-                        }
+                        for (int e = 0; e < 4; ++e) acc[0][t][4 * g + e] += v[e];
+                    }
             }
         } else {
             typename Loop::RowsA ra;
@@ -425,7 +425,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ?
         const bool even = j.N % 4 == 0 && (reinterpret_cast<uintptr_t>(x->w) & 15) == 0;
         const bool turn = j.turned && !(j.symmetric && tm == tn);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
+        for (int i = 0; i < STRIPS; ++i) {
 #pragma unroll
             for (int t = 0; t < TN; ++t)
 #pragma unroll
@@ -433,7 +433,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ?
                     *reinterpret_cast<f32x4*>(stage + l32 * PITCH + 32 * t + 8 * g + 4 * half) =
                         f32x4{acc[i][t][4 * g], acc[i][t][4 * g + 1], acc[i][t][4 * g + 2], acc[i][t][4 * g + 3]};
             __builtin_amdgcn_wave_barrier();
-            const int32_t row0 = m0 + wm * Loop::WM + 32 * i, col = n0 + wn * Loop::WN + 8 * (lane % CG);
+            const int32_t row0 = m0 + wm * Loop::WM + 32 * (FINISH ? strip : i), col = n0 + wn * Loop::WN + 8 * (lane % CG);
 #pragma unroll
             for (int p = 0; p < 32 / RPP; ++p) {
                 const int r = p * RPP + lane / CG;
@@ -578,7 +578,7 @@ template <int BT, int WAVES_M, int WAVES_N, int STAGES>
 hipError_t launch_tile(const Products& a, const Plan& p, hipStream_t s) {
     const dim3 threads(64 * WAVES_M * WAVES_N);
     hipLaunchKernelGGL((muon_product_kernel<BT, WAVES_M, WAVES_N, STAGES, false>), dim3(p.whole + p.blocks), threads, 0, s, a);
-    if (p.blocks) hipLaunchKernelGGL((muon_product_kernel<BT, WAVES_M, WAVES_N, STAGES, true>), dim3(p.tiles - p.whole), threads, 0, s, a);
+    if (p.blocks) hipLaunchKernelGGL((muon_product_kernel<BT, WAVES_M, WAVES_N, STAGES, true>), dim3((p.tiles - p.whole) * (BT / WAVES_M / 32)), threads, 0, s, a);
     return hipGetLastError();
 }
 
