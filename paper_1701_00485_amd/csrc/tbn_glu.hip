@@ -4,6 +4,8 @@
 // the g and u that the forward pass kept or, with the same products again, from x.
 //
 // The codes of the 2 f filters are packed as those of one layer, gates first (TBN2, see tbn.h).
+#include <algorithm>
+
 #include "tbn_kernels.h"
 #include "tbn_nt.h"
 
@@ -128,11 +130,13 @@ __device__ __forceinline__ void finish1(const GluArgs& a, int64_t m, int32_t k, 
 // ---- many rows ---------------------------------------------------------------------------
 // A block owns BM rows and NH gates with the NH others of the same columns, so that a lane holds the g and the u of an
 // output.  Rows of x go through LDS as in tbn_nt.h (64 features a stage, a ring of STAGES); of the 2 NH filters the
-// stage's codes, 16 bytes each, decoded in registers into bf16 pairs, two operations a pair.
+// stage's codes, 16 bytes each, decoded in registers into bf16 pairs, two operations a pair, between the matrix instructions that
+// bound it: 8192 x 4096 -> 2 x 8192 in 800 us, 1.37 PFLOP/s (copies issued at a stage's begin and operands made in a row: 857).
+// Two blocks of 128 x 128 a compute unit, each with a barrier a stage, do as well as one of 256 x 128.
 // GROUPS groups of such waves, each with a part of the stages and a ring of its own, serve tiles that are too few to fill the GPU; the
 // first adds the others' sums.
 template <int BM, int NH, int WAVES_M, int WAVES_N, int STAGES, int GROUPS, int ACT>
-__global__ __launch_bounds__(64 * WAVES_M * WAVES_N * GROUPS, BM * NH >= 32768 || GROUPS > 1 ? 1 : 2) void glu_kernel(const GluArgs a) {
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N * GROUPS, GROUPS > 1 ? 1 : 2) void glu_kernel(const GluArgs a) {
     constexpr int WAVES = WAVES_M * WAVES_N;
     constexpr int WM = BM / WAVES_M, WN = NH / WAVES_N, TM = WM / 32, TH = WN / 32, TN = 2 * TH;
     constexpr int STAGE = BM * 128 + 2 * NH * 16, CODES = 2 * NH / 64;  // 1 KiB copies of codes a stage
@@ -168,19 +172,19 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * GROUPS, BM * NH >= 32768 |
     uint8_t* const ring = smem + group * RING;
     const uint32_t base = lds_addr(ring);
     int islot = 0;
-    auto issue = [&](int s, int j0, int j1) {
-        const uint32_t lds = base + (uint32_t)(islot * STAGE);
-        const uint32_t kb = (uint32_t)(first + s) * 128u;
-        const uint32_t at = kb + 16u * seg < row_bytes ? kb : kb | 0x80000000u;
-#pragma unroll
-        for (int j = 0; j < COPIES; ++j) {
-            if (j < j0 || j >= j1) continue;
-            if (j < Rows::COPIES)
-                rows.issue(j, lds, at, wave);
-            else
-                dma_b128(rsrc_c, lds + BM * 128 + piece * 1024, code_off + (uint32_t)(first + s) * 1024u);
-        }
-        if (j1 == COPIES) islot = islot + 1 == STAGES ? 0 : islot + 1;
+    uint32_t copy_lds = 0, copy_x = 0, copy_codes = 0;  // of the stage whose copies are issued (past the last one: zeros, as in tbn_nt.h)
+    auto aim = [&](int s) {
+        const uint32_t past = s < n ? 0u : 0x80000000u, at = (uint32_t)(first + s) * 128u;
+        copy_lds = base + (uint32_t)(islot * STAGE);
+        copy_x = at + 16u * seg < row_bytes ? at | past : at | 0x80000000u;
+        copy_codes = code_off + (uint32_t)(first + s) * 1024u | past;
+        islot = islot + 1 == STAGES ? 0 : islot + 1;
+    };
+    auto copy = [&](int j) {
+        if (j < Rows::COPIES)
+            rows.issue(j, copy_lds, copy_x, wave);
+        else
+            dma_b128(rsrc_c, copy_lds + BM * 128 + piece * 1024, copy_codes);
     };
 
     const int sw = (l32 >> 1) & 7;
@@ -199,64 +203,108 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * GROUPS, BM * NH >= 32768 |
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][t][v] = 0.0f;
 
-#pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s)
-        if (s < n) issue(s, 0, COPIES);
-    int cslot = 0;
-    for (int s = 0; s < each; ++s) {
-        if (s + STAGES - 2 < n)
-            wait_vmcnt((STAGES - 2) * COPIES);
-        else
-            wait_vmcnt(0);
-        __syncthreads();
-        if (s + STAGES - 1 < n) issue(s + STAGES - 1, 0, COPIES);
-        if (GROUPS > 1 && s >= n) continue;
-        const uint8_t* st = ring + cslot * STAGE;
-        cslot = cslot + 1 == STAGES ? 0 : cslot + 1;
-        u32x4 raw[TN];
-#pragma unroll
-        for (int t = 0; t < TN; ++t)
-            raw[t] = *reinterpret_cast<const u32x4*>(st + bcol + ((t < TH ? 0 : NH) + 32 * (t % TH)) * 16);
-        u32x4 x[2][TM];
-        bf16x8 w[2][TN];
-        auto read = [&](int u, int k) {
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-                x[k][i] = *reinterpret_cast<const u32x4*>(st + arow + 32 * 128 * i + 16 * ((2 * u + half) ^ sw));
-        };
-        auto decode = [&](int u, int k) {
-#pragma unroll
-            for (int t = 0; t < TN; ++t) {
-                u32x4 d;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) d[j] = ((raw[t][u] & mask[j]) << shl[j]) + 0x3F803F80u;
-                w[k][t] = as_bf16x8(d);
-            }
-        };
-        read(0, 0);
-        decode(0, 0);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (u + 1 < 4) {
-                read(u + 1, (u + 1) & 1);
-                decode(u + 1, (u + 1) & 1);
-            }
+    auto pin = [&]() {  // as in tbn_nt.h
+        if constexpr (TM * TN >= 16) {
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int t = 0; t < TN; ++t) acc[i][t] = mfma32(w[u & 1][t], as_bf16x8(x[u & 1][i]), acc[i][t]);
-            if (u + 1 < 4) {
-#pragma unroll
-                for (int k = 0; k < TM * TN; ++k) {
-                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                    if (k < TM) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x002, TM >= 4 ? 2 : 8 / TM, 0);
-                }
-            }
-            __builtin_amdgcn_sched_barrier(0);
+                for (int t = 0; t < TN; ++t) asm volatile("" : "+a"(acc[i][t]));
         }
+    };
+    u32x4 raw[TN], x[2][TM], w[2][TN];
+    auto codes = [&](const uint8_t* st, int t) { raw[t] = *reinterpret_cast<const u32x4*>(st + bcol + ((t < TH ? 0 : NH) + 32 * (t % TH)) * 16); };
+    auto read = [&](const uint8_t* st, int u, int i) {
+        x[u & 1][i] = *reinterpret_cast<const u32x4*>(st + arow + 32 * 128 * i + 16 * ((2 * u + half) ^ sw));
+    };
+    auto decode = [&](int u, int d) {  // word d of the filters' operands of step u
+        const int t = d / 4, j = d % 4;
+        w[u & 1][t][j] = ((raw[t][u] & mask[j]) << shl[j]) + 0x3F803F80u;
+    };
+    // Step u of a stage, while the operands of step v of the stage at `st` are made: the next step of the same stage, or, in a
+    // stage's last step, the first one of the next, whose codes are read first; then copies are issued too.
+    constexpr int MUL = TM * TN, WORDS = 4 * TN, LAST = 3;
+    auto step = [&](int u, const uint8_t* st, int v, bool last) {
+        constexpr bool MANY = MUL >= 8;
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!MANY) {
+            if (last) {
+#pragma unroll
+                for (int t = 0; t < TN; ++t) codes(st, t);
+            }
+#pragma unroll
+            for (int i = 0; i < TM; ++i) read(st, v, i);
+            if (!last) {
+#pragma unroll
+                for (int d = 0; d < WORDS; ++d) decode(v, d);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < MUL; ++k) {
+            const int i = k / TN, t = k % TN;
+            acc[i][t] = mfma32(as_bf16x8(w[u & 1][t]), as_bf16x8(x[u & 1][i]), acc[i][t]);
+            if constexpr (MANY) {
+                if (last) {
+#pragma unroll
+                    for (int c = 2 * k * TN / MUL; c < 2 * (k + 1) * TN / MUL && c < TN; ++c) codes(st, c);
+                }
+#pragma unroll
+                for (int r = k * TM / MUL; r < (k + 1) * TM / MUL; ++r) read(st, v, r);
+                if (last) {
+#pragma unroll
+                    for (int d = (2 * k - MUL) * WORDS / MUL; d < (2 * k + 2 - MUL) * WORDS / MUL; ++d)
+                        if (d >= 0) decode(v, d);
+#pragma unroll
+                    for (int j = k * COPIES / MUL; j < (k + 1) * COPIES / MUL; ++j) copy(j);
+                } else {
+#pragma unroll
+                    for (int d = k * WORDS / MUL; d < (k + 1) * WORDS / MUL; ++d) decode(v, d);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if constexpr (!MANY) {
+            if (last) {
+#pragma unroll
+                for (int j = 0; j < COPIES; ++j) copy(j);
+#pragma unroll
+                for (int d = 0; d < WORDS; ++d) decode(v, d);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s) {
+        aim(s);
+#pragma unroll
+        for (int j = 0; j < COPIES; ++j) copy(j);
     }
+    wait_vmcnt((STAGES - 1) * COPIES);
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < TN; ++t) codes(ring, t);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) read(ring, 0, i);
+#pragma unroll
+    for (int d = 0; d < WORDS; ++d) decode(0, d);
+    pin();
+    int slot = 0;
+    for (int s = 0; s < each; ++s) {
+        const uint8_t* st = ring + slot * STAGE;
+        slot = slot + 1 == STAGES ? 0 : slot + 1;
+        if (GROUPS == 1 || s < n) {
+#pragma unroll
+            for (int u = 0; u < LAST; ++u) step(u, st, u + 1, false);
+        }
+        // this wave's copies of the next stage have landed, its reads of this one are done, and so are the other waves'
+        wait_vmcnt((STAGES - 2) * COPIES);
+        __syncthreads();
+        if (GROUPS > 1 && s >= n) continue;
+        aim(s + STAGES);  // into this stage's place
+        step(LAST, ring + slot * STAGE, 0, true);
+    }
+    pin();
+    wait_vmcnt(0);
 
     // ---- lane l of tile (i, t) holds row 32 i + l % 32 and, for each v / 4, columns 32 t + 8 (v / 4) + 4 (l / 32) + 0..3;
     //      32 rows of g and u at a time are turned in LDS, so that a lane has 8 columns of a row ----
@@ -348,10 +396,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * GROUPS, BM * NH >= 32768 |
 }
 
 // ---- up to 16 rows -----------------------------------------------------------------------
-// The codes are read once and bound it.  A block owns 16 NG gates and the others of the same columns; its waves divide the
-// features.  Lane (f = l % 16, q = l / 16) reads, of filter f of each group, the 16 bytes of element block ib + q and, of row f
-// of x, the same 64 features; matrix instruction s of a step takes elements 8 s .. 8 s + 7 of each block (the order of the
-// elements is the same in both operands, which is all that a sum asks).  The waves' sums meet in LDS.
+// The codes are read once and bound it: 59 MB of 4096 -> 2 x 28672 in 18.4 us for 1 row (3.2 TB/s), in 21.4 us for 16.  Lane
+// (f = l % 16, q = l / 16) reads, of filter f of 16, the 16 bytes of element block ib + q and, of row f of x, the same 64
+// features; matrix instruction s of a step takes elements 8 s .. 8 s + 7 of each block (the order of the elements is the
+// same in both operands, which is all that a sum asks).
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 // Elements 8 h .. 8 h + 7 of a packed word as bf16 pairs, two operations a pair.
@@ -363,9 +411,116 @@ __device__ __forceinline__ bf16x8 decode_half(uint32_t w) {
     return as_bf16x8(d);
 }
 
-template <int NG, int WAVES, int DEPTH, bool STAGED, int ACT>
+// Of up to 4096 SL features: a block, one a compute unit, owns a range of the groups of 16 gates and the others of the same columns.
+// Wave (i, j) of its KS x GS keeps x's steps i, i + KS, .. of 256 features in registers and streams the codes of groups j, j + GS, ..,
+// four (SL 2: two) ahead; the KS sums of an output meet in LDS, four groups a wave at a time.  Without x in registers, a block for
+// each 64 gates (glu_few_kernel): 26.5 us for 16 rows of 4096 -> 2 x 28672, and 7.6 for 1 x 512 -> 2 x 1024, 3.6 here.
+template <int SL, int ACT>
+__global__ __launch_bounds__(1024) void glu_stream_kernel(const GluArgs a, int KS, int GS) {
+    constexpr int BATCH = 4, AHEAD = SL == 1 ? 4 : 2;
+    __shared__ __attribute__((aligned(16))) float part[BATCH * 16 * 512];  // [BATCH GS groups][KS][gates, others][16 rows][16 columns]
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int j = wave / KS, i = wave - j * KS;
+    const int f = lane & 15, q = lane >> 4;
+    const int nb = (a.c + 63) / 64;  // element blocks, four a step, one a lane group
+    const int groups = (a.f + 15) / 16;
+    const int g0 = (int)((int64_t)groups * blockIdx.x / gridDim.x), g1 = (int)((int64_t)groups * (blockIdx.x + 1) / gridDim.x);
+    const int rounds = (g1 - g0 + GS - 1) / GS;
+    const u32x4* const codes = reinterpret_cast<const u32x4*>(a.codes);
+    int ib[SL];
+#pragma unroll
+    for (int s = 0; s < SL; ++s) ib[s] = 4 * (i + KS * s) + q;
+    u32x4 w[AHEAD][SL][2], x[SL][8];
+    auto load = [&](int d, int r) {
+        const int k = min((g0 + j + GS * r) * 16 + f, a.f - 1);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int filter = k + (h ? a.f : 0);
+            const u32x4* const p = codes + (int64_t)(filter / 64) * nb * 64 + filter % 64;
+#pragma unroll
+            for (int s = 0; s < SL; ++s) w[d][s][h] = __builtin_nontemporal_load(p + (int64_t)min(ib[s], nb - 1) * 64);
+        }
+    };
+    // A step's 512 bytes of each row, two rows a load, are turned in this wave's 8 KiB of LDS.  Read as the matrix instruction wants
+    // them, 16 bytes of a line by each lane, 16 rows fetch each line eight times (16 x 4096 -> 2 x 8192: 14.1 us, 10.1 turned);
+    // up to 4 rows stay in the cache, and turning them costs 0.5 to 2 us.
+    uint8_t* const turn = reinterpret_cast<uint8_t*>(part) + wave * 8192;
+    auto ahead = [&]() {
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d)
+            if (d < rounds) load(d, d);
+    };
+    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.x), 0, (int)(a.rows * a.c * 2), 0x00020000);
+    auto get = [&](int row, int c) {  // zeros past the row's end and past the last row
+        return __builtin_amdgcn_raw_buffer_load_b128(rx, c < a.c ? (row * a.c + c) * 2 : (int)0x80000000, 0, 0);
+    };
+    if (a.rows <= 4) {
+#pragma unroll
+        for (int s = 0; s < SL; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[s][e] = get(f, ib[s] * 64 + 8 * e);
+        ahead();
+    } else {
+#pragma unroll
+        for (int s = 0; s < SL; ++s) {
+            u32x4 v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = get(2 * e + (lane >> 5), (i + KS * s) * 256 + 8 * (lane & 31));
+            if (s == SL - 1) ahead();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int row = 2 * e + (lane >> 5);
+                *reinterpret_cast<u32x4*>(turn + row * 512 + 16 * ((lane & 31) ^ row)) = v[e];
+            }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[s][e] = *reinterpret_cast<const u32x4*>(turn + f * 512 + 16 * ((8 * q + e) ^ f));
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+    }
+    for (int r0 = 0; r0 < rounds; r0 += BATCH) {
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+            if (r0 + b >= rounds) break;
+            f32x4 acc[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) acc[h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int s = 0; s < SL; ++s)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        acc[h] = mfma16(decode_half<0>(w[b % AHEAD][s][h][e]), as_bf16x8(x[s][2 * e]), acc[h]);
+                        acc[h] = mfma16(decode_half<1>(w[b % AHEAD][s][h][e]), as_bf16x8(x[s][2 * e + 1]), acc[h]);
+                    }
+            if (r0 + b + AHEAD < rounds) load(b % AHEAD, r0 + b + AHEAD);
+            // lane (f, q) holds row f, columns 4 q .. 4 q + 3
+#pragma unroll
+            for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4*>(part + (((b * GS + j) * KS + i) * 2 + h) * 256 + f * 16 + 4 * q) = acc[h];
+        }
+        __syncthreads();
+        const int outputs = min(BATCH, rounds - r0) * GS * 256;
+        for (int o = threadIdx.x; o < outputs; o += 64 * KS * GS) {
+            const int row = o / 16 % 16, k = (g0 + GS * r0 + o / 256) * 16 + o % 16;
+            if (row >= a.rows || k >= min(g1 * 16, a.f)) continue;
+            const float ag = a.alpha[k], au = a.alpha[a.f + k];
+            const float* const v = part + o / 256 * KS * 512 + o % 256;
+            float g = v[0], u = v[256];
+#pragma unroll 4
+            for (int n = 1; n < KS; ++n) g += v[512 * n], u += v[512 * n + 256];
+            finish1<ACT>(a, row, k, g * ag, u * au);
+        }
+        if (r0 + BATCH < rounds) __syncthreads();
+    }
+}
+
+// Of more features: a block owns 16 NG gates and the others of the same columns, its waves a range of the features each, and x is read
+// with the codes.
+template <int NG, int WAVES, int DEPTH, int ACT>
 __global__ __launch_bounds__(64 * WAVES) void glu_few_kernel(const GluArgs a) {
-    extern __shared__ __attribute__((aligned(16))) uint16_t xl[];  // STAGED: [rows + 1][steps 256], the last row zero
     __shared__ f32x4 sums[WAVES][2 * NG][64];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -385,72 +540,32 @@ __global__ __launch_bounds__(64 * WAVES) void glu_few_kernel(const GluArgs a) {
     f32x4 acc[2 * NG];
 #pragma unroll
     for (int g = 0; g < 2 * NG; ++g) acc[g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    u32x4 w[DEPTH][2 * NG], x[STAGED ? 1 : DEPTH][8];
-    const uint16_t* const xs = xl + (have ? f : (int)a.rows) * steps * 256;
+    u32x4 w[DEPTH][2 * NG], x[DEPTH][8];
     auto load = [&](int d, int s) {
         const int ib = 4 * s + q;
-        if constexpr (!STAGED) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int c = ib * 64 + 8 * e;
-                x[d][e] = u32x4{0u, 0u, 0u, 0u};
-                if (have && c < a.c) x[d][e] = *reinterpret_cast<const u32x4*>(xp + c);
-            }
+        for (int e = 0; e < 8; ++e) {
+            const int c = ib * 64 + 8 * e;
+            x[d][e] = u32x4{0u, 0u, 0u, 0u};
+            if (have && c < a.c) x[d][e] = *reinterpret_cast<const u32x4*>(xp + c);
         }
 #pragma unroll
         for (int g = 0; g < 2 * NG; ++g) w[d][g] = __builtin_nontemporal_load(wp[g] + (int64_t)(ib < nb ? ib : nb - 1) * 64);
     };
-    auto multiply = [&](int d, int s) {
-        if constexpr (STAGED) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[0][e] = *reinterpret_cast<const u32x4*>(xs + (4 * s + q) * 64 + 8 * e);
-        }
-        const int dx = STAGED ? 0 : d;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int g = 0; g < 2 * NG; ++g) {
-                acc[g] = mfma16(decode_half<0>(w[d][g][e]), as_bf16x8(x[dx][2 * e]), acc[g]);
-                acc[g] = mfma16(decode_half<1>(w[d][g][e]), as_bf16x8(x[dx][2 * e + 1]), acc[g]);
-            }
-    };
-    if constexpr (STAGED) {
-        // the first loads of x before those of the codes: writing them to LDS waits for them alone
-        const int per = steps * 32, pieces = ((int)a.rows + 1) * per;  // 16-byte pieces of a row, and all
-        u32x4 v[4];
-        auto get = [&](int i0) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int i = i0 + 64 * WAVES * u, r = i / per, c = (i - r * per) * 8;
-                v[u] = u32x4{0u, 0u, 0u, 0u};
-                if (i < pieces && r < a.rows && c < a.c) v[u] = *reinterpret_cast<const u32x4*>(a.x + (int64_t)r * a.c + c);
-            }
-        };
-        auto put = [&](int i0) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (i0 + 64 * WAVES * u < pieces) reinterpret_cast<u32x4*>(xl)[i0 + 64 * WAVES * u] = v[u];
-        };
-        get(threadIdx.x);
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d)
-            if (s0 + d < s1) load(d, s0 + d);
-        put(threadIdx.x);
-        for (int i0 = threadIdx.x + 64 * WAVES * 4; i0 < pieces; i0 += 64 * WAVES * 4) {
-            get(i0);
-            put(i0);
-        }
-        __syncthreads();
-    } else {
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d)
-            if (s0 + d < s1) load(d, s0 + d);
-    }
+    for (int d = 0; d < DEPTH; ++d)
+        if (s0 + d < s1) load(d, s0 + d);
     for (int s = s0; s < s1; s += DEPTH) {
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
             if (s + d >= s1) break;
-            multiply(d, s + d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int g = 0; g < 2 * NG; ++g) {
+                    acc[g] = mfma16(decode_half<0>(w[d][g][e]), as_bf16x8(x[d][2 * e]), acc[g]);
+                    acc[g] = mfma16(decode_half<1>(w[d][g][e]), as_bf16x8(x[d][2 * e + 1]), acc[g]);
+                }
             if (s + d + DEPTH < s1) load(d, s + d + DEPTH);
         }
     }
@@ -498,6 +613,14 @@ hipError_t launch_tiles(const GluArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
+template <int SL, int ACT>
+hipError_t launch_stream(const GluArgs& a, hipStream_t s) {
+    const int steps = (a.c + 255) / 256, groups = (a.f + 15) / 16;
+    const int KS = (steps + SL - 1) / SL, GS = std::max(1, std::min((groups + 255) / 256, 16 / KS));
+    hipLaunchKernelGGL((glu_stream_kernel<SL, ACT>), dim3((unsigned)std::min(groups, 256)), dim3(64 * KS * GS), 0, s, a, KS, GS);
+    return hipGetLastError();
+}
+
 template <int ACT>
 hipError_t launch(const GluArgs& a, const uint16_t* gu, hipStream_t s) {
     if (gu) {
@@ -506,33 +629,39 @@ hipError_t launch(const GluArgs& a, const uint16_t* gu, hipStream_t s) {
         return hipGetLastError();
     }
     if (a.rows <= 16) {
+        if (a.c <= 256 * 16) return launch_stream<1, ACT>(a, s);
+        if (a.c <= 256 * 32) return launch_stream<2, ACT>(a, s);
+        // 16 x 8192 -> 2 f, NG 1, 2, 4: f 28672 98.8, 66.6, 46.4 us; 14336 55.2, 35.5, 25.2; 8192 29.8, 18.7, 23.6; 4096 16.7, 17.7, 22.8
         const int64_t groups = (a.f + 15) / 16;
-        const int lds = ((int)a.rows + 1) * ((a.c + 255) / 256) * 512;  // of x and a row of zeros
-#define TBN_FEW(ng, waves, depth, staged)                                                                                           \
-    hipLaunchKernelGGL((glu_few_kernel<ng, waves, depth, staged, ACT>), dim3((unsigned)((groups + ng - 1) / ng)), dim3(64 * waves), \
-                       staged ? lds : 0, s, a)
-        if (a.rows <= 4 && lds <= 48 * 1024) {
-            if (groups >= 1024)
-                TBN_FEW(2, 8, 2, true);
-            else
-                TBN_FEW(1, 4, 2, true);
-        } else if (groups >= 1024) {
-            TBN_FEW(4, 8, 1, false);
-        } else if (groups >= 512) {
-            TBN_FEW(2, 4, 2, false);
-        } else {
-            TBN_FEW(1, 4, 2, false);
-        }
+#define TBN_FEW(ng, waves, depth) \
+    hipLaunchKernelGGL((glu_few_kernel<ng, waves, depth, ACT>), dim3((unsigned)((groups + ng - 1) / ng)), dim3(64 * waves), 0, s, a)
+        if (groups >= 768)
+            TBN_FEW(4, 8, 1);
+        else if (groups >= 512)
+            TBN_FEW(2, 4, 2);
+        else
+            TBN_FEW(1, 4, 2);
 #undef TBN_FEW
         return hipGetLastError();
     }
+    // The largest tile that leaves no more than a third of the 256 compute units idle; below one tile a unit, tiles whose stages
+    // groups of waves divide.  Times in us:
+    //   rows x c -> 2 x f          128x128  128x64  64x64  64x64 x 4  64x32 x 4
+    //   8192 x 4096 -> 2 x 8192      800      936    1051                         (256 x 128 by four or eight waves: 798, 814)
+    //    768 x 4096 -> 2 x 4096       51.0     54.2    54.2    63.9      88.8     192 tiles of 128 x 128
+    //    640 x 4096 -> 2 x 4096       49.5     52.4    51.3    60.9      74.3     160
+    //    512 x 4096 -> 2 x 4096       48.2     34.7    39.9    46.2      61.6     256 tiles of 128 x 64
+    //    777 x 1000 -> 2 x 1333       30.8     19.3    16.7    24.6      30.8     147
+    //    256 x 4096 -> 2 x 4096       49.0     31.9    25.4    23.4      32.2     256 tiles of 64 x 64
+    //    200 x 1536 -> 2 x 4096       23.5     15.4    11.9    12.2      17.7     256
+    //     64 x 4096 -> 2 x 8192       47.6     31.3    23.8    20.2      16.5     128
+    //     17 x  512 -> 2 x 1024       11.1      8.1     7.1     8.7       6.9      16
     auto tiles = [&](int64_t m, int64_t n) { return (a.rows + m - 1) / m * ((a.f + n - 1) / n); };
-    if (tiles(256, 128) >= 192) return launch_tiles<256, 128, 2, 4, 4, 1, ACT>(a, s);
-    if (tiles(128, 128) >= 192) return launch_tiles<128, 128, 2, 4, 4, 1, ACT>(a, s);
+    if (tiles(128, 128) >= 160) return launch_tiles<128, 128, 2, 2, 4, 1, ACT>(a, s);
     if (tiles(128, 64) >= 192) return launch_tiles<128, 64, 2, 2, 4, 1, ACT>(a, s);
-    if (tiles(64, 64) > 256 || a.c <= 1024) return launch_tiles<64, 64, 2, 2, 4, 1, ACT>(a, s);
-    if (tiles(64, 64) > 128) return launch_tiles<64, 64, 2, 2, 4, 4, ACT>(a, s);
-    return launch_tiles<64, 32, 2, 1, 4, 4, ACT>(a, s);
+    if (tiles(64, 64) <= 128 && a.c >= 512) return launch_tiles<64, 32, 2, 1, 4, 4, ACT>(a, s);
+    if (tiles(64, 64) <= 256 && a.c >= 2048) return launch_tiles<64, 64, 2, 2, 4, 4, ACT>(a, s);
+    return launch_tiles<64, 64, 2, 2, 4, 1, ACT>(a, s);
 }
 
 }  // namespace

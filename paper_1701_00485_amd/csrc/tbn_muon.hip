@@ -583,7 +583,7 @@ hipError_t launch_tile(const Products& a, const Plan& p, hipStream_t s) {
 }
 
 hipError_t launch_products(const Products& a, const Plan& p, hipStream_t s) {
-    if (p.tile == 256) return launch_tile<256, 2, 4, 2>(a, p, s);
+    if (p.tile == 256) return launch_tile<256, 2, 2, 2>(a, p, s);
     return p.tile == 128 ? launch_tile<128, 2, 2, 2>(a, p, s) : launch_tile<64, 2, 2, 3>(a, p, s);
 }
 

@@ -9,8 +9,8 @@
 //   * Of a block's waves each owns (BM / WAVES_M) x (BN / WAVES_N) outputs.  The second operand goes first into the matrix
 //     instruction, so that lane l of 32x32 tile (i, t) holds row 32 i + l % 32 and, for each v / 4, the four consecutive
 //     columns 32 t + 8 (v / 4) + 4 (l / 32) + 0..3.
-//   * Operands of step u + 1 are read from LDS while the matrix instructions of step u run; the copies of the next stage
-//     are spread over the steps.
+//   * Operands of a step are read from LDS while the matrix instructions of the step before run, those of a stage's first step too: the
+//     barrier between two stages lies before the last step of the earlier one, whose operands are in registers by then.
 #pragma once
 
 #include "tbn_device.h"
@@ -25,36 +25,25 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // 8-bit integers: four steps of 32 a stage, exact 32-bit sums.
 struct NtI8 {
     typedef i32x16 Acc;
-    static constexpr int STEPS = 4, PARTS = 1;
+    static constexpr int STEPS = 4, PARTS = 1, PRODUCTS = 1;
     static __device__ __forceinline__ int seg(int u, int, int half) { return 2 * u + half; }
-    template <int TM, int TN>
-    static __device__ __forceinline__ void step(const u32x4 (&a)[PARTS][TM], const u32x4 (&b)[PARTS][TN], Acc (&acc)[TM][TN]) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int t = 0; t < TN; ++t)
-                acc[i][t] = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, b[0][t]),
-                                                                  __builtin_bit_cast(i32x4, a[0][i]), acc[i][t], 0, 0, 0);
+    static constexpr __device__ int part_a(int) { return 0; }
+    static constexpr __device__ int part_b(int) { return 0; }
+    static __device__ __forceinline__ i32x16 mul(u32x4 b, u32x4 a, i32x16 c) {
+        return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, b), __builtin_bit_cast(i32x4, a), c, 0, 0, 0);
     }
 };
 
-// 32-bit values x = hi + lo in two fp16 halves (22 bits of x): two steps of 16 a stage, three products each; lo lo, 2^-22
-// of the product, is left out.
+// 32-bit values x = hi + lo in two fp16 halves (22 bits of x): two steps of 16 a stage, three products each (hi lo, lo hi, hi hi); lo lo,
+// 2^-22 of the product, is left out.
 struct NtF16x2 {
     typedef f32x16 Acc;
-    static constexpr int STEPS = 2, PARTS = 2;
+    static constexpr int STEPS = 2, PARTS = 2, PRODUCTS = 3;
     static __device__ __forceinline__ int seg(int u, int part, int half) { return 4 * part + 2 * u + half; }
+    static constexpr __device__ int part_a(int p) { return p == 1; }
+    static constexpr __device__ int part_b(int p) { return p == 0; }
     static __device__ __forceinline__ f32x16 mul(u32x4 b, u32x4 a, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
-    }
-    template <int TM, int TN>
-    static __device__ __forceinline__ void step(const u32x4 (&a)[PARTS][TM], const u32x4 (&b)[PARTS][TN], Acc (&acc)[TM][TN]) {
-#pragma unroll
-        for (int p = 0; p < 3; ++p)  // lo hi, hi lo, hi hi
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int t = 0; t < TN; ++t) acc[i][t] = mul(b[p == 0][t], a[p == 1][i], acc[i][t]);
     }
 };
 
@@ -78,7 +67,7 @@ struct NtRows {
     }
 };
 
-template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, class Op, bool EARLY = false>
+template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, class Op>
 struct NtLoop {
     static constexpr int WAVES = WAVES_M * WAVES_N;
     static constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, TM = WM / 32, TN = WN / 32;
@@ -102,67 +91,108 @@ struct NtLoop {
         const uint32_t my = 16u * copy_seg(wave, lane);
         const int n = s1 - s0;
         int islot = 0;
-        // copies j0 .. j1 - 1 of stage s
-        auto issue = [&](int s, int j0, int j1) {
-            const uint32_t lds = base + (uint32_t)(islot * STAGE);
-            const uint32_t kb = (uint32_t)(s0 + s) * 128u;
-            const uint32_t at_a = kb + my < row_bytes ? kb : kb | 0x80000000u;
-#pragma unroll
-            for (int j = 0; j < COPIES; ++j) {
-                if (j < j0 || j >= j1) continue;
-                if (j < RowsA::COPIES)
-                    ra.issue(j, lds, at_a, wave);
-                else
-                    rb.issue(j - RowsA::COPIES, lds + BM * 128, kb, wave);
-            }
-            if (j1 == COPIES) islot = islot + 1 == STAGES ? 0 : islot + 1;
+        uint32_t copy_lds = 0, copy_at = 0, copy_at_a = 0;  // of the stage whose copies are issued
+        auto aim = [&](int s) {
+            copy_lds = base + (uint32_t)(islot * STAGE);
+            // past the last stage nothing is read and zeros are written, so that every stage issues and waits for the same copies
+            copy_at = (uint32_t)(s0 + s) * 128u | (s < n ? 0u : 0x80000000u);
+            copy_at_a = copy_at + my < row_bytes ? copy_at : copy_at | 0x80000000u;
+            islot = islot + 1 == STAGES ? 0 : islot + 1;
         };
-#pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s)
-            if (s < n) issue(s, 0, COPIES);
-        int cslot = 0;
-        const int arow = (wm * WM + l32) * 128, brow = (wn * WN + l32) * 128 + BM * 128;
-        for (int s = 0; s < rounds; ++s) {
-            if (s + STAGES - 2 < n)
-                wait_vmcnt((STAGES - 2) * COPIES);
+        auto copy = [&](int j) {
+            if (j < RowsA::COPIES)
+                ra.issue(j, copy_lds, copy_at_a, wave);
             else
-                wait_vmcnt(0);
+                rb.issue(j - RowsA::COPIES, copy_lds + BM * 128, copy_at, wave);
+        };
+        const int arow = (wm * WM + l32) * 128, brow = (wn * WN + l32) * 128 + BM * 128;
+        u32x4 a[2][Op::PARTS][TM], b[2][Op::PARTS][TN];
+        constexpr int READS = Op::PARTS * (TM + TN), MUL = TM * TN * Op::PRODUCTS;
+        auto read = [&](const uint8_t* st, int u, int r) {  // operand r of step u
+            const int p = r / (TM + TN), i = r % (TM + TN), so = 16 * (Op::seg(u, p, half) ^ sw);
+            if (i < TN)
+                b[u & 1][p][i] = *reinterpret_cast<const u32x4*>(st + brow + 32 * 128 * i + so);
+            else
+                a[u & 1][p][i - TN] = *reinterpret_cast<const u32x4*>(st + arow + 32 * 128 * (i - TN) + so);
+        };
+        auto multiply = [&](int u, int k) {  // instruction k of step u
+            const int p = k / (TM * TN), i = k / TN % TM, t = k % TN;
+            acc[i][t] = Op::mul(b[u & 1][Op::part_b(p)][t], a[u & 1][Op::part_a(p)][i], acc[i][t]);
+        };
+        // Step u, while the operands of step v of the stage at `st` are read and, in a stage's last step, copies issued: each between two
+        // instructions where a step has many (256 x 256 tiles of four waves 4096 x 8192 x 4096: 620 us, in a row 690), in a row where
+        // it has few (64 x 64 tiles 512 x 512 x 512: 7.6 us, between them 8.3).
+        auto step = [&](int u, const uint8_t* st, int v, bool copies) {
+            constexpr bool MANY = MUL >= 12;
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (!MANY) {
+#pragma unroll
+                for (int r = 0; r < READS; ++r) read(st, v, r);
+            }
+#pragma unroll
+            for (int k = 0; k < MUL; ++k) {
+                multiply(u, k);
+                if constexpr (MANY) {
+#pragma unroll
+                    for (int r = k * READS / MUL; r < (k + 1) * READS / MUL; ++r) read(st, v, r);
+#pragma unroll
+                    for (int j = k * COPIES / MUL; j < (k + 1) * COPIES / MUL; ++j)
+                        if (copies) copy(j);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if constexpr (!MANY) {
+#pragma unroll
+                for (int j = 0; j < COPIES; ++j)
+                    if (copies) copy(j);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        constexpr int LAST = Op::STEPS - 1;
+        static_assert(LAST & 1, "a stage begins with the first operand registers");
+
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s) {
+            aim(s);
+#pragma unroll
+            for (int j = 0; j < COPIES; ++j) copy(j);
+        }
+        wait_vmcnt((STAGES - 1) * COPIES);
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < READS; ++r) read(smem, 0, r);
+        pin(acc);
+        int slot = 0;
+        for (int s = 0; s < rounds; ++s) {
+            const uint8_t* st = smem + slot * STAGE;
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+            if (s < n) {
+#pragma unroll
+                for (int u = 0; u < LAST; ++u) {
+                    step(u, st, u + 1, false);
+                }
+            }
+            // this wave's copies of the next stage have landed, its reads of this one are done, and so are the other waves'
+            wait_vmcnt((STAGES - 2) * COPIES);
             __syncthreads();
             if (s >= n) continue;
-            const uint8_t* st = smem + cslot * STAGE;
-            cslot = cslot + 1 == STAGES ? 0 : cslot + 1;
-            u32x4 a[2][Op::PARTS][TM], b[2][Op::PARTS][TN];
-            auto read = [&](int u, int k) {
-#pragma unroll
-                for (int p = 0; p < Op::PARTS; ++p) {
-                    const int so = 16 * (Op::seg(u, p, half) ^ sw);
-#pragma unroll
-                    for (int t = 0; t < TN; ++t) b[k][p][t] = *reinterpret_cast<const u32x4*>(st + brow + 32 * 128 * t + so);
-#pragma unroll
-                    for (int i = 0; i < TM; ++i) a[k][p][i] = *reinterpret_cast<const u32x4*>(st + arow + 32 * 128 * i + so);
-                }
-            };
-            read(0, 0);
-#pragma unroll
-            for (int u = 0; u < Op::STEPS; ++u) {
-                if (EARLY && u == 0 && s + STAGES - 1 < n) issue(s + STAGES - 1, 0, COPIES);
-                if (!EARLY && s + STAGES - 1 < n) issue(s + STAGES - 1, u * COPIES / Op::STEPS, (u + 1) * COPIES / Op::STEPS);
-                if (u + 1 < Op::STEPS) read(u + 1, (u + 1) & 1);
-                Op::step(a[u & 1], b[u & 1], acc);
-                if (u + 1 < Op::STEPS) {
-                    constexpr int READS = Op::PARTS * (TM + TN), MUL = TM * TN * (Op::PARTS == 1 ? 1 : 3);
-#pragma unroll
-                    for (int k = 0; k < (READS < MUL ? READS : MUL); ++k) {
-                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                        __builtin_amdgcn_sched_group_barrier(0x100, (READS + MUL - 1) / MUL, 0);
-                    }
-#pragma unroll
-                    for (int k = READS; k < MUL; ++k) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            const uint8_t* next = smem + slot * STAGE;
+            aim(s + STAGES);  // into this stage's place
+            step(LAST, next, 0, true);
         }
+        pin(acc);
+        wait_vmcnt(0);
         __syncthreads();
+    }
+
+    // 256 sums a lane stay in accumulation registers throughout (else the compiler moves a third of them at every step).
+    static __device__ __forceinline__ void pin(Acc (&acc)[TM][TN]) {
+        if constexpr (TM * TN >= 16) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int t = 0; t < TN; ++t) asm volatile("" : "+a"(acc[i][t]));
+        }
     }
 };
 

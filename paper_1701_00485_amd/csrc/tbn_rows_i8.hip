@@ -150,7 +150,7 @@ __device__ __forceinline__ void finish8(const RowsI8Args& a, int64_t m, int32_t 
 // ---- many rows ---------------------------------------------------------------------------
 template <int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int GROUPS>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * GROUPS, BM * BN >= 65536 || GROUPS > 1 ? 1 : BM * BN >= 8192 ? 2 : 3) void matmul_i8_kernel(const RowsI8Args a) {
-    typedef NtLoop<BM, BN, WAVES_M, WAVES_N, STAGES, NtI8, true> Loop;
+    typedef NtLoop<BM, BN, WAVES_M, WAVES_N, STAGES, NtI8> Loop;
     constexpr int PITCH = Loop::WN + 4;  // of a staged row, in floats
     static_assert(Loop::BYTES >= Loop::WAVES * 32 * PITCH * 4 + (BM + 2 * BN) * 4, "staging fits in the ring");
     __shared__ __attribute__((aligned(1024))) uint8_t smem[GROUPS * Loop::BYTES];
@@ -350,12 +350,26 @@ hipError_t launch_matmul_i8(const RowsI8Args& a, hipStream_t s) {
 #undef TBN_VEC
         return hipGetLastError();
     }
+    // The largest tile that leaves no more than a quarter of the 256 compute units idle; below one tile a unit, tiles whose
+    // stages four groups of waves divide.  128 x 128 by four waves, two blocks a unit, or by eight, one.  Times in us, c 4096:
+    //   rows x n        256x256  128x128/4  128x128/8  128x64  64x64  64x64 x 4
+    //   8192 x 8192      241       256        334        343    401     657
+    //   3200 x 4096       57.2      61.7       79.0       75.5   87.8   140.5    208 tiles of 256 x 256
+    //   2560 x 4096       56.1      56.6       59.5       57.1   69.7   108.8    160
+    //   2048 x 4096       54.5      36.1       42.3       47.5   57.9    88.4    512 tiles of 128 x 128
+    //   1024 x 4096       51.0      27.4       22.1       24.3   31.5    45.5    256
+    //    768 x 4096       50.7      26.0       20.5       20.9   23.9    35.8    192
+    //    640 x 4096       51.9      25.5       19.9       20.0   21.6    34.7    160
+    //    512 x 4096       49.0      23.3       19.4       15.7   16.7    24.3    256 tiles of 128 x 64
+    //    256 x 4352                                       14.9   15.3    20.5    272 tiles of 64 x 64
+    //    256 x 4096                                       14.9   12.8    11.3    256; c 2048: 8.3, 8.1; c 1024: 6.0, 6.5
     auto tiles = [&](int64_t m, int64_t n) { return (a.rows + m - 1) / m * ((a.n + n - 1) / n); };
-    if (tiles(256, 256) >= 192) return launch_tiles<256, 256, 2, 4, 2, 1>(a, s);
-    if (tiles(128, 128) >= 192) return launch_tiles<128, 128, 2, 4, 4, 1>(a, s);
+    if (tiles(256, 256) >= 192) return launch_tiles<256, 256, 2, 2, 2, 1>(a, s);
+    if (tiles(128, 128) > 256) return launch_tiles<128, 128, 2, 2, 2, 1>(a, s);
+    if (tiles(128, 128) >= 160) return launch_tiles<128, 128, 2, 4, 4, 1>(a, s);
     if (tiles(128, 64) >= 256) return launch_tiles<128, 64, 2, 2, 3, 1>(a, s);
-    if (tiles(64, 64) > 256 || a.c <= 1024) return launch_tiles<64, 64, 2, 2, 3, 1>(a, s);
-    return launch_tiles<64, 64, 2, 2, 2, 4>(a, s);
+    if (tiles(64, 64) <= 256 && a.c >= 2048) return launch_tiles<64, 64, 2, 2, 2, 4>(a, s);
+    return launch_tiles<64, 64, 2, 2, 3, 1>(a, s);
 }
 
 }  // namespace tbn

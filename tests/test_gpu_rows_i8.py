@@ -87,11 +87,12 @@ def check(y, acc, s, bias=0.0, res=0.0, relu=False):
 
 
 SHAPES = [(1, 1, 16), (1, 5, 32), (2, 33, 16), (16, 100, 48), (7, 1000, 1008), (16, 16400, 80), (1, 16385, 144), (3, 64, 131056),  # few rows
-          (17, 1, 16), (17, 40, 128), (64, 64, 512), (33, 257, 144),                              # 64 x 64, few stages
-          (17, 300, 1008), (100, 500, 1008), (200, 130, 4112), (64, 1000, 640), (40, 64, 131056),   # ... in groups of waves
-          (320, 3500, 560),                                                                       # ... without
-          (1000, 2100, 176), (777, 2049, 144),                                                    # 128 x 64
-          (3100, 4100, 304), (4000, 3333, 128)]                                                   # 256 x 256
+          (17, 1, 16), (17, 40, 128), (64, 64, 512), (33, 257, 144), (17, 300, 1008), (777, 2049, 144), (320, 3500, 560),  # 64 x 64
+          (17, 300, 2064), (100, 500, 4112), (200, 130, 4112), (64, 1000, 2048), (40, 64, 131056),    # ... in groups of waves
+          (1000, 2100, 176), (1100, 1900, 304),                                                       # 128 x 64
+          (1700, 1700, 176), (1290, 2048, 1008),                                                      # 128 x 128 by eight waves
+          (2100, 2200, 176), (1500, 2900, 1008),                                                      # ... by four
+          (3100, 4100, 304), (4000, 3333, 128)]                                                       # 256 x 256
 
 
 @pytest.mark.parametrize("rows,n,c", SHAPES)
