@@ -462,16 +462,18 @@ __global__ __launch_bounds__(1024) void glu_stream_kernel(const GluArgs a, int K
             for (int e = 0; e < 8; ++e) x[s][e] = get(f, ib[s] * 64 + 8 * e);
         ahead();
     } else {
+        u32x4 v[SL][8];
+#pragma unroll
+        for (int s = 0; s < SL; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[s][e] = get(2 * e + (lane >> 5), (i + KS * s) * 256 + 8 * (lane & 31));
+        ahead();
 #pragma unroll
         for (int s = 0; s < SL; ++s) {
-            u32x4 v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = get(2 * e + (lane >> 5), (i + KS * s) * 256 + 8 * (lane & 31));
-            if (s == SL - 1) ahead();
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int row = 2 * e + (lane >> 5);
-                *reinterpret_cast<u32x4*>(turn + row * 512 + 16 * ((lane & 31) ^ row)) = v[e];
+                *reinterpret_cast<u32x4*>(turn + row * 512 + 16 * ((lane & 31) ^ row)) = v[s][e];
             }
             __builtin_amdgcn_wave_barrier();
 #pragma unroll

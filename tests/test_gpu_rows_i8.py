@@ -86,7 +86,9 @@ def check(y, acc, s, bias=0.0, res=0.0, relu=False):
     assert off.max().item() <= 0, off.max().item()
 
 
-SHAPES = [(1, 1, 16), (1, 5, 32), (2, 33, 16), (16, 100, 48), (7, 1000, 1008), (16, 16400, 80), (1, 16385, 144), (3, 64, 131056),  # few rows
+SHAPES = [(1, 1, 16), (1, 5, 32), (2, 33, 16), (16, 100, 48), (7, 1000, 1008), (16, 16400, 80), (1, 16385, 144), (4, 70000, 272),  # few rows
+          (16, 300, 4096), (5, 18000, 2064), (16, 50, 4112), (9, 9001, 8192),                         # ... all of a block's waves
+          (3, 64, 131056), (16, 33, 8208), (1, 1000, 8208),                                           # ... x with the weights
           (17, 1, 16), (17, 40, 128), (64, 64, 512), (33, 257, 144), (17, 300, 1008), (777, 2049, 144), (320, 3500, 560),  # 64 x 64
           (17, 300, 2064), (100, 500, 4112), (200, 130, 4112), (64, 1000, 2048), (40, 64, 131056),    # ... in groups of waves
           (1000, 2100, 176), (1100, 1900, 304),                                                       # 128 x 64
