@@ -194,10 +194,11 @@ tbn_status tbn_muon_step(const tbn_muon_tensor* tensors, int32_t n, tbn_dtype gt
         if (!std::isfinite(tensors[i].weight_decay) || !std::isfinite(tensors[i].scale))
             return fail(TBN_ERR_SHAPE, "weight_decay and scale have to be finite");
     }
-    if (!(hyper->momentum >= 0 && hyper->momentum < 1)) return fail(TBN_ERR_SHAPE, "momentum has to be in [0, 1)");
+    // (as the kernels take them, in fp32)
+    if (!((float)hyper->momentum >= 0 && (float)hyper->momentum < 1)) return fail(TBN_ERR_SHAPE, "momentum has to be in [0, 1)");
     if (!(hyper->eps >= 1e-30 && hyper->eps <= 1)) return fail(TBN_ERR_SHAPE, "eps has to be in [1e-30, 1]");
     if (hyper->steps < 1 || hyper->steps > tbn::kMuonSteps) return fail(TBN_ERR_SHAPE, "1 to 32 steps");
-    if (!hyper->lr_dev && !std::isfinite(hyper->lr)) return fail(TBN_ERR_SHAPE, "lr has to be finite");
+    if (!hyper->lr_dev && !std::isfinite((float)hyper->lr)) return fail(TBN_ERR_SHAPE, "lr has to be finite");
     if (!aligned(hyper->lr_dev, 4)) return fail(TBN_ERR_ALIGN, "misaligned lr_dev");
     const int64_t need = muon_ws(tensors, n);
     if ((st = check_ws(ws, ws_bytes, need)) != TBN_OK) return st;

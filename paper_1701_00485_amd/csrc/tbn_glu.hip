@@ -594,6 +594,7 @@ __global__ __launch_bounds__(64 * WAVES) void glu_few_kernel(const GluArgs a) {
 }
 
 // ---- from kept projections ---------------------------------------------------------------
+// A thread takes 8 columns of a row: dh, g and u in, dg and du out, 10 bytes an element, which bound it (8192 x 8192: 134 us, 5.0 TB/s).
 template <int ACT>
 __global__ __launch_bounds__(256) void glu_bwd_kernel(const GluArgs a, const uint16_t* __restrict__ gu, uint32_t groups) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;

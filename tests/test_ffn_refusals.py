@@ -95,7 +95,7 @@ def test_muon():
     assert _muon(w=None) == _muon(m=None) == _muon(g=None) == _muon(hyper=False) == NULL
     assert _muon(gt=2) == UNSUPPORTED
     assert _muon(w=P[0] + 2) == _muon(m=P[1] + 1) == _muon(g=P[2] + 2) == _muon(gt=0, g=P[2] + 1) == _muon(lr_dev=BAD) == ALIGN
-    for k, bad in (("momentum", (1.0, -0.1, NAN)), ("eps", (0.0, 1e-31, 2.0, NAN)), ("steps", (0, -1, 33)), ("lr", (NAN, INF))):
+    for k, bad in (("momentum", (1.0, 1.0 - 1e-9, -0.1, NAN)), ("eps", (0.0, 1e-31, 2.0, NAN)), ("steps", (0, -1, 33)), ("lr", (NAN, INF, 1e39))):
         assert all(_muon(**{k: v}) == SHAPE for v in bad), k
     assert _muon(decay=NAN) == _muon(scale=INF) == SHAPE
     assert _muon(ws=None) == _muon(size=1000) == WORKSPACE and _muon(ws=P[3] + 8) == ALIGN
