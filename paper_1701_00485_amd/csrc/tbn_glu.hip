@@ -5,6 +5,7 @@
 //
 // The codes of the 2 f filters are packed as those of one layer, gates first (TBN2, see tbn.h).
 #include <algorithm>
+#include <type_traits>
 
 #include "tbn_kernels.h"
 #include "tbn_nt.h"
@@ -41,44 +42,51 @@ __device__ __forceinline__ void unpack8(u32x4 r, float (&v)[8]) {
     for (int e = 0; e < 4; ++e) v[2 * e] = bf16_bits_to_f32(r[e] & 0xFFFFu), v[2 * e + 1] = __uint_as_float(r[e] & 0xFFFF0000u);
 }
 
-// Eight values of a row whose first has index `at`, `n` of them real; `whole`: all, and 16-byte aligned.
-__device__ __forceinline__ void get8(const uint16_t* p, int64_t at, int n, bool whole, float (&v)[8]) {
-    if (whole) {
-        unpack8(*reinterpret_cast<const u32x4*>(p + at), v);
-        return;
-    }
+// Eight values of a row whose first has index `at`: 16-byte aligned, anywhere, or `n` of them.
+enum Eight { EVEN, WHOLE, PART };
+template <Eight E>
+__device__ __forceinline__ void get8(const uint16_t* p, int64_t at, int n, float (&v)[8]) {
+    if constexpr (E == PART) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n ? bf16_bits_to_f32(p[at + e]) : 0.0f;
+        for (int e = 0; e < 8; ++e) v[e] = e < n ? bf16_bits_to_f32(p[at + e]) : 0.0f;
+    } else {
+        typedef typename std::conditional<E == EVEN, u32x4, u32x4_at2>::type V;
+        unpack8(*reinterpret_cast<const V*>(p + at), v);
+    }
 }
-__device__ __forceinline__ void put8(uint16_t* p, int64_t at, int n, bool whole, const float (&v)[8]) {
-    if (whole) {
-        *reinterpret_cast<u32x4*>(p + at) =
+template <Eight E>
+__device__ __forceinline__ void put8(uint16_t* p, int64_t at, int n, const float (&v)[8]) {
+    if constexpr (E == PART) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n) p[at + e] = (uint16_t)f32_to_bf16_bits(v[e]);
+    } else {
+        typedef typename std::conditional<E == EVEN, u32x4, u32x4_at2>::type V;
+        *reinterpret_cast<V*>(p + at) =
             u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-        return;
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < n) p[at + e] = (uint16_t)f32_to_bf16_bits(v[e]);
 }
-__device__ __forceinline__ void put8(float* p, int64_t at, int n, bool whole, const float (&v)[8]) {
-    if (whole) {
-        reinterpret_cast<f32x4*>(p + at)[0] = f32x4{v[0], v[1], v[2], v[3]};
-        reinterpret_cast<f32x4*>(p + at)[1] = f32x4{v[4], v[5], v[6], v[7]};
-        return;
-    }
+template <Eight E>
+__device__ __forceinline__ void put8(float* p, int64_t at, int n, const float (&v)[8]) {
+    if constexpr (E == PART) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < n) p[at + e] = v[e];
+        for (int e = 0; e < 8; ++e)
+            if (e < n) p[at + e] = v[e];
+    } else {
+        typedef typename std::conditional<E == EVEN, f32x4, f32x4_at4>::type V;
+        reinterpret_cast<V*>(p + at)[0] = f32x4{v[0], v[1], v[2], v[3]};
+        reinterpret_cast<V*>(p + at)[1] = f32x4{v[4], v[5], v[6], v[7]};
+    }
 }
 
 // What follows g and u of columns k .. k + 7 of row m (n of them real): h, the kept projections or the gradients.
-template <int ACT>
-__device__ __forceinline__ void finish8(const GluArgs& a, int64_t m, int32_t k, int n, bool whole, const float (&g)[8], const float (&u)[8]) {
+template <int ACT, Eight E>
+__device__ __forceinline__ void finish8(const GluArgs& a, int64_t m, int32_t k, int n, const float (&g)[8], const float (&u)[8]) {
     const int64_t o = m * a.f + k, og = m * 2 * a.f + k;
     float h[8];
     if (a.dh) {
         float dh[8], dg[8], du[8];
-        get8(a.dh, o, n, whole, dh);
+        get8<E>(a.dh, o, n, dh);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             float slope;
@@ -87,21 +95,32 @@ __device__ __forceinline__ void finish8(const GluArgs& a, int64_t m, int32_t k, 
             du[e] = dh[e] * y;
             h[e] = y * u[e];
         }
-        put8(a.gu, og, n, whole, dg);
-        put8(a.gu, og + a.f, n, whole, du);
+        put8<E>(a.gu, og, n, dg);
+        put8<E>(a.gu, og + a.f, n, du);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[e] = activate<false>(ACT, g[e], nullptr) * u[e];
         if (a.gu) {
-            put8(a.gu, og, n, whole, g);
-            put8(a.gu, og + a.f, n, whole, u);
+            put8<E>(a.gu, og, n, g);
+            put8<E>(a.gu, og + a.f, n, u);
         }
     }
     if (!a.h) return;
     if (a.h_f32)
-        put8(reinterpret_cast<float*>(a.h), o, n, whole, h);
+        put8<E>(reinterpret_cast<float*>(a.h), o, n, h);
     else
-        put8(reinterpret_cast<uint16_t*>(a.h), o, n, whole, h);
+        put8<E>(reinterpret_cast<uint16_t*>(a.h), o, n, h);
+}
+
+// ... whichever way the rows lie.
+template <int ACT>
+__device__ __forceinline__ void finish8(const GluArgs& a, int64_t m, int32_t k, int n, const float (&g)[8], const float (&u)[8]) {
+    if (a.f % 8 == 0)
+        finish8<ACT, EVEN>(a, m, k, n, g, u);
+    else if (n == 8)
+        finish8<ACT, WHOLE>(a, m, k, n, g, u);
+    else
+        finish8<ACT, PART>(a, m, k, n, g, u);
 }
 
 // ... of one column.
@@ -352,7 +371,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * GROUPS, GROUPS > 1 ? 1 : 2
     constexpr int CG = WN / 8, RPP = 64 / CG;
     const int cl = 8 * (lane % CG);
     const int32_t k = k0 + wn * WN + cl;
-    const bool whole = a.f % 8 == 0;
+    const int n8 = a.f - k < 8 ? a.f - k : 8;
     float ag[8], au[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) ag[e] = alpha[wn * WN + cl + e], au[e] = alpha[NH + wn * WN + cl + e];
@@ -368,18 +387,6 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * GROUPS, GROUPS > 1 ? 1 : 2
                     f32x4{acc[i][t + TH][4 * g], acc[i][t + TH][4 * g + 1], acc[i][t + TH][4 * g + 2], acc[i][t + TH][4 * g + 3]};
             }
         __builtin_amdgcn_wave_barrier();
-        if (!whole) {  // rows begin anywhere: a value a lane, side by side
-            constexpr int ROWS = 64 / WN;
-            const int c = lane % WN;
-            const float a1 = alpha[wn * WN + c], a2 = alpha[NH + wn * WN + c];
-#pragma unroll 1
-            for (int r = lane / WN; r < 32; r += ROWS) {
-                const int64_t m = m0 + wm * WM + 32 * i + r;
-                if (m < a.rows && k0 + wn * WN + c < a.f) finish1<ACT>(a, m, k0 + wn * WN + c, sg[r * PITCH + c] * a1, su[r * PITCH + c] * a2);
-            }
-            __builtin_amdgcn_wave_barrier();
-            continue;
-        }
 #pragma unroll 1
         for (int p = 0; p < 32 / RPP; ++p) {
             const int r = p * RPP + lane / CG;
@@ -391,7 +398,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * GROUPS, GROUPS > 1 ? 1 : 2
 #pragma unroll
                 for (int e = 0; e < 4; ++e) g[4 * h + e] = vg[e] * ag[4 * h + e], u[4 * h + e] = vu[e] * au[4 * h + e];
             }
-            if (m < a.rows && k < a.f) finish8<ACT>(a, m, k, 8, true, g, u);
+            if (m < a.rows && n8 > 0) finish8<ACT>(a, m, k, n8, g, u);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -591,7 +598,7 @@ __global__ __launch_bounds__(64 * WAVES) void glu_few_kernel(const GluArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (e < n) g8[e] = g[e] * a.alpha[k + e], u8[e] = u[e] * a.alpha[a.f + k + e];
-        finish8<ACT>(a, f, k, n, false, g8, u8);
+        finish8<ACT, PART>(a, f, k, n, g8, u8);
     }
 }
 
@@ -604,11 +611,18 @@ __global__ __launch_bounds__(256) void glu_bwd_kernel(const GluArgs a, const uin
     if (m >= a.rows) return;
     const int32_t k = (int32_t)(i - m * groups) * 8;
     const int n = a.f - k < 8 ? a.f - k : 8;
-    const bool whole = a.f % 8 == 0;
     float g[8], u[8];
-    get8(gu, m * 2 * a.f + k, n, whole, g);
-    get8(gu, m * 2 * a.f + a.f + k, n, whole, u);
-    finish8<ACT>(a, m, k, n, whole, g, u);
+    if (a.f % 8 == 0) {
+        get8<EVEN>(gu, m * 2 * a.f + k, n, g);
+        get8<EVEN>(gu, m * 2 * a.f + a.f + k, n, u);
+    } else if (n == 8) {
+        get8<WHOLE>(gu, m * 2 * a.f + k, n, g);
+        get8<WHOLE>(gu, m * 2 * a.f + a.f + k, n, u);
+    } else {
+        get8<PART>(gu, m * 2 * a.f + k, n, g);
+        get8<PART>(gu, m * 2 * a.f + a.f + k, n, u);
+    }
+    finish8<ACT>(a, m, k, n, g, u);
 }
 
 template <int BM, int NH, int WM, int WN, int STAGES, int GROUPS, int ACT>
@@ -656,7 +670,7 @@ hipError_t launch(const GluArgs& a, const uint16_t* gu, hipStream_t s) {
     //    768 x 4096 -> 2 x 4096       51.0     54.2    54.2    63.9      88.8     192 tiles of 128 x 128
     //    640 x 4096 -> 2 x 4096       49.5     52.4    51.3    60.9      74.3     160
     //    512 x 4096 -> 2 x 4096       48.2     34.7    39.9    46.2      61.6     256 tiles of 128 x 64
-    //    777 x 1000 -> 2 x 1333       30.8     19.3    16.7    24.6      30.8     147
+    //    777 x 1000 -> 2 x 1333       21.6     14.9    14.2    19.7      22.7     147
     //    256 x 4096 -> 2 x 4096       49.0     31.9    25.4    23.4      32.2     256 tiles of 64 x 64
     //    200 x 1536 -> 2 x 4096       23.5     15.4    11.9    12.2      17.7     256
     //     64 x 4096 -> 2 x 8192       47.6     31.3    23.8    20.2      16.5     128

@@ -1,6 +1,7 @@
 // tbn_rows_i8.hip -- products in 8-bit integers with a scale for each row of both operands (each token, each channel):
 // the rows made 8-bit, and y[m][n] = act(scale_m scale_n sum over k of q[m][k] w[n][k] + bias_n + residual), the sum exact.
 #include <algorithm>
+#include <type_traits>
 
 #include "tbn_kernels.h"
 #include "tbn_nt.h"
@@ -125,20 +126,23 @@ __device__ __forceinline__ void finish1(const RowsI8Args& a, int64_t m, int32_t 
         reinterpret_cast<uint16_t*>(a.y)[o] = (uint16_t)f32_to_bf16_bits(v);
 }
 
-// ... of 8 consecutive channels, 16-byte aligned (n % 8 == 0).
+// ... of 8 consecutive channels, `EVEN`: 16-byte aligned (n % 8 == 0).
+template <bool EVEN>
 __device__ __forceinline__ void finish8(const RowsI8Args& a, int64_t m, int32_t n0, const float (&s)[8], float sx, const float (&sw)[8],
                                         const float (&bias)[8]) {
+    typedef typename std::conditional<EVEN, f32x4, f32x4_at4>::type V32;
+    typedef typename std::conditional<EVEN, u32x4, u32x4_at2>::type V16;
     const int64_t o = m * a.n + n0;
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = s[e] * (sx * sw[e]) + bias[e];
     if (a.residual && a.y_f32) {
-        const f32x4* r = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.residual) + o);
+        const V32* r = reinterpret_cast<const V32*>(reinterpret_cast<const float*>(a.residual) + o);
         const f32x4 lo = r[0], hi = r[1];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] += lo[e], v[4 + e] += hi[e];
     } else if (a.residual) {
-        const u32x4 r = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.residual) + o);
+        const u32x4 r = *reinterpret_cast<const V16*>(reinterpret_cast<const uint16_t*>(a.residual) + o);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[2 * e] += bf16_bits_to_f32(r[e] & 0xFFFFu), v[2 * e + 1] += __uint_as_float(r[e] & 0xFFFF0000u);
     }
@@ -147,11 +151,11 @@ __device__ __forceinline__ void finish8(const RowsI8Args& a, int64_t m, int32_t 
         for (int e = 0; e < 8; ++e) v[e] = v[e] > 0.0f || v[e] != v[e] ? v[e] : 0.0f;
     }
     if (a.y_f32) {
-        f32x4* p = reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.y) + o);
+        V32* p = reinterpret_cast<V32*>(reinterpret_cast<float*>(a.y) + o);
         p[0] = f32x4{v[0], v[1], v[2], v[3]};
         p[1] = f32x4{v[4], v[5], v[6], v[7]};
     } else {
-        *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(a.y) + o) =
+        *reinterpret_cast<V16*>(reinterpret_cast<uint16_t*>(a.y) + o) =
             u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
     }
 }
@@ -224,27 +228,29 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * GROUPS, BM * BN >= 65536 |
                     f32x4{(float)acc[i][t][4 * g], (float)acc[i][t][4 * g + 1], (float)acc[i][t][4 * g + 2], (float)acc[i][t][4 * g + 3]};
         __builtin_amdgcn_wave_barrier();
         const int col = n0 + wn * Loop::WN + 8 * (lane % CG);
-        if (!even) {  // rows begin anywhere: a value a lane, side by side
-            constexpr int ROWS = Loop::WN < 64 ? 64 / Loop::WN : 1, COLS = Loop::WN < 64 ? Loop::WN : 64;
-#pragma unroll 4
-            for (int k = 0; k < 32 / ROWS * (Loop::WN / COLS); ++k) {
-                const int r = k / (Loop::WN / COLS) * ROWS + lane / COLS, c = k % (Loop::WN / COLS) * COLS + lane % COLS;
-                const int64_t m = m0 + wm * Loop::WM + 32 * i + r;
-                if (m < a.rows && n0 + wn * Loop::WN + c < a.n)
-                    finish1(a, m, n0 + wn * Loop::WN + c, stage[r * PITCH + c], row_scale[wm * Loop::WM + 32 * i + r], col_scale[wn * Loop::WN + c],
-                            col_bias[wn * Loop::WN + c]);
-            }
-            __builtin_amdgcn_wave_barrier();
-            continue;
-        }
-#pragma unroll
-        for (int p = 0; p < 32 / RPP; ++p) {
+        auto row8 = [&](int p, auto then) {
             const int r = p * RPP + lane / CG;
             const int64_t m = m0 + wm * Loop::WM + 32 * i + r;
             const f32x4* s = reinterpret_cast<const f32x4*>(stage + r * PITCH + 8 * (lane % CG));
             const f32x4 lo = s[0], hi = s[1];
             const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            if (m < a.rows && col < a.n) finish8(a, m, col, v, row_scale[wm * Loop::WM + 32 * i + r], sw, bias);
+            if (m < a.rows && col < a.n) then(m, v, row_scale[wm * Loop::WM + 32 * i + r]);
+        };
+        if (even) {
+#pragma unroll
+            for (int p = 0; p < 32 / RPP; ++p) row8(p, [&](int64_t m, const float(&v)[8], float sx) { finish8<true>(a, m, col, v, sx, sw, bias); });
+        } else {
+#pragma unroll 1
+            for (int p = 0; p < 32 / RPP; ++p)
+                row8(p, [&](int64_t m, const float(&v)[8], float sx) {
+                    if (col + 8 <= a.n) {
+                        finish8<false>(a, m, col, v, sx, sw, bias);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 7; ++e)
+                            if (col + e < a.n) finish1(a, m, col + e, v[e], sx, sw[e], bias[e]);
+                    }
+                });
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -424,7 +430,8 @@ hipError_t launch_matmul_i8(const RowsI8Args& a, hipStream_t s) {
     // stages four groups of waves divide.  128 x 128 by four waves, two blocks a unit, or by eight, one.  Times in us, c 4096:
     //   rows x n        256x256  128x128/4  128x128/8  128x64  64x64  64x64 x 4
     //   8192 x 8192      241       256        334        343    401     657
-    //   3200 x 4096       57.2      61.7       79.0       75.5   87.8   140.5    208 tiles of 256 x 256
+    //   4000 x 4097      118        90                                126        272 tiles of 256 x 256
+    //   3200 x 4096       57.2      61.7       79.0       75.5   87.8   140.5    208
     //   2560 x 4096       56.1      56.6       59.5       57.1   69.7   108.8    160
     //   2048 x 4096       54.5      36.1       42.3       47.5   57.9    88.4    512 tiles of 128 x 128
     //   1024 x 4096       51.0      27.4       22.1       24.3   31.5    45.5    256
@@ -434,8 +441,11 @@ hipError_t launch_matmul_i8(const RowsI8Args& a, hipStream_t s) {
     //    256 x 4352                                       14.9   15.3    20.5    272 tiles of 64 x 64
     //    256 x 4096                                       14.9   12.8    11.3    256; c 2048: 8.3, 8.1; c 1024: 6.0, 6.5
     auto tiles = [&](int64_t m, int64_t n) { return (a.rows + m - 1) / m * ((a.n + n - 1) / n); };
-    if (tiles(256, 256) >= 192) return launch_tiles<256, 256, 2, 2, 2, 1>(a, s);
-    if (tiles(128, 128) > 256) return launch_tiles<128, 128, 2, 2, 2, 1>(a, s);
+    // (256 x 256 go in rounds of 256, 56 us here, 128 x 128 in rounds of 512, 36.)
+    if (tiles(128, 128) > 256) {
+        const int64_t large = (tiles(256, 256) + 255) / 256 * 14, small = (tiles(128, 128) + 511) / 512 * 9;
+        return large <= small ? launch_tiles<256, 256, 2, 2, 2, 1>(a, s) : launch_tiles<128, 128, 2, 2, 2, 1>(a, s);
+    }
     if (tiles(128, 128) >= 160) return launch_tiles<128, 128, 2, 4, 4, 1>(a, s);
     if (tiles(128, 64) >= 256) return launch_tiles<128, 64, 2, 2, 3, 1>(a, s);
     if (tiles(64, 64) <= 256 && a.c >= 2048) return launch_tiles<64, 64, 2, 2, 2, 4>(a, s);
