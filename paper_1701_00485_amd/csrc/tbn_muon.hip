@@ -178,7 +178,8 @@ __global__ __launch_bounds__(256) void muon_table_kernel(const Words w) {
 }
 
 // ---- momentum and the update's norm ------------------------------------------------------
-// m = momentum m + g; the sum of the squares of u = g + momentum m (or of m), in 64 bits, a partial sum a block.
+// m = momentum m + g; the sum of the squares of u = g + momentum m (or of m), in 64 bits, a partial sum a block.  Bound by memory:
+// ResNet-18's 11.7 M values with fp32 gradients in 28 us, 5.0 TB/s; 4096 x 8192 with bf16 ones in 93 us, 3.6 TB/s.
 template <bool BF16>
 __device__ __forceinline__ float grad_at(const void* g, int64_t i) {
     return BF16 ? bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(g)[i]) : reinterpret_cast<const float*>(g)[i];
@@ -243,7 +244,8 @@ __global__ __launch_bounds__(256) void muon_momentum_kernel(const Start a) {
 }
 
 // ---- X and its transpose -----------------------------------------------------------------
-// A block takes 64 x 64 values of the update over its norm: rows of `direct` as they lie, rows of `turned` from LDS.
+// A block takes 64 x 64 values of the update over its norm: rows of `direct` as they lie, rows of `turned` from LDS.  Bound by memory:
+// 4096 x 8192 in 100 us, 4.7 TB/s.
 template <bool BF16>
 __global__ __launch_bounds__(256) void muon_start_kernel(const Start a) {
     __shared__ float tile[64][65];
@@ -322,6 +324,10 @@ __device__ __forceinline__ void lower_tile(uint32_t w, uint32_t* i, uint32_t* j)
 // over as many blocks again.  A tile whose stages lie in more than one block is left as sums, two at most for a block, and FINISH,
 // a block a tile, adds them in order and ends it.  (All tiles divided so: of 4096 x 4096 x 8192 578 us against 388, because blocks
 // at different places of the rows share nothing in the L2s.)
+// The matrix instructions bound large ones: P X of 4096 x 8192 in 640 us (256 x 256 tiles by four waves, 1.29 PFLOP/s of the three
+// products; 128 x 128 683 where those took 610 by themselves), a symmetric 4096 x 4096 product in 191 + 10 (1.03).  512 x 512 x 512 take
+// 9.8 us: a launch, the 256 KB that a tile's compute unit has to take in, 64 KB a us, and the tile's end.  Sixteen waves on a tile
+// instead of four take in no more: 9.4 us, and 15 in place of 12 where every compute unit has a tile.
 template <int BT, int WAVES_M, int WAVES_N, int STAGES, bool FINISH>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ? 2 : 3) void muon_product_kernel(const Products a) {
     typedef NtLoop<BT, BT, WAVES_M, WAVES_N, STAGES, NtF16x2> Loop;
@@ -510,8 +516,6 @@ constexpr int kCus = 256;
 
 int64_t tiles_of(int64_t n, int tile) { return (n + tile - 1) / tile; }
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
-int64_t part_bytes(const TileCost& c, int64_t blocks) { return blocks * 2 * c.tile * c.tile * 4; }
-
 
 uint64_t job_tiles(const Matrix& x, const Step& step, int tile) {
     const uint64_t m = tiles_of(x.m, tile);
