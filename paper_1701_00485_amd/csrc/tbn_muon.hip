@@ -326,8 +326,9 @@ __device__ __forceinline__ void lower_tile(uint32_t w, uint32_t* i, uint32_t* j)
 // at different places of the rows share nothing in the L2s.)
 // The matrix instructions bound large ones: P X of 4096 x 8192 in 640 us (256 x 256 tiles by four waves, 1.29 PFLOP/s of the three
 // products; 128 x 128 683 where those took 610 by themselves), a symmetric 4096 x 4096 product in 191 + 10 (1.03).  512 x 512 x 512 take
-// 9.8 us: a launch, the 256 KB that a tile's compute unit has to take in, 64 KB a us, and the tile's end.  Sixteen waves on a tile
-// instead of four take in no more: 9.4 us, and 15 in place of 12 where every compute unit has a tile.
+// 9.8 us: a launch, 16 stages at 0.25 (copies alone 0.13, operands and products alone 0.16: a wave issues both in turn), the tile's end.
+// Sixteen waves on a tile in place of four: 9.4 us, and 15 in place of 12 where every compute unit has a tile; waves that only copy take
+// 0.9 from it, and add 9% where 128 x 128 tiles lie side by side.
 template <int BT, int WAVES_M, int WAVES_N, int STAGES, bool FINISH>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, BT >= 256 ? 1 : BT >= 128 ? 2 : 3) void muon_product_kernel(const Products a) {
     typedef NtLoop<BT, BT, WAVES_M, WAVES_N, STAGES, NtF16x2> Loop;
