@@ -151,6 +151,59 @@ def test_serving_one_token_is_the_batch_within_rounding(tbn):
         assert torch.equal(tbn.matmul_i8(q, s, *net.last, out_dtype=F), y[i:i + 1])  # exact sums: the same bits
 
 
+@pytest.mark.parametrize("rows", [1, 16])
+def test_captured_tokens(tbn, rows):
+    """A serving step of few rows, captured: its replays over new tokens are the eager step's bits."""
+    nets = [Net(tbn, rows, c=1000, f=333), Net(tbn, rows, c=1000, f=333)]
+    for n in nets:
+        n.forward(True)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        nets[0].forward(True)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = nets[0].forward(True)
+    for step in range(5):
+        x = torch.randn(nets[0].x.shape, device="cuda").to(BF)
+        for n in nets:
+            n.x.copy_(x)
+        graph.replay()
+        want = nets[1].forward(True)
+        torch.cuda.synchronize()
+        assert same(out, want), step
+
+
+@pytest.mark.parametrize("rows,c,f", [(1, 64, 7), (3, 500, 33), (16, 4200, 100), (5, 8300, 43), (20, 600, 45), (70, 100, 4100), (70, 2100, 3999), (900, 72, 1333), (1500, 72, 1601)])
+def test_nothing_is_written_behind_an_output(tbn, rows, c, f):
+    """Rows of odd lengths are written 16 bytes at a time: what lies before an output's first value and behind its last stays as it was."""
+    x = torch.randn(rows, c, device="cuda").to(BF)
+    codes, alpha = tbn.quantize(torch.randn(2 * f, c, device="cuda"))[:2]
+    dh = torch.randn(rows, f, device="cuda").to(BF)
+
+    def within(n, dtype, call):
+        buf = torch.full((n + 128,), -7.0, device="cuda", dtype=dtype)
+        out = buf[64:64 + n]
+        call(out)
+        assert (buf[:64] == -7).all() and (buf[64 + n:] == -7).all()
+        return out.clone()
+
+    for dtype in (BF, F):
+        h = within(rows * f, dtype, lambda o: tbn.glu_fwd(x, codes, alpha, h=o.view(rows, f)))
+        assert same([h.view(rows, f)], [tbn.glu_fwd(x, codes, alpha, out_dtype=dtype)[0]])
+    gu = tbn.glu_fwd(x, codes, alpha, want_gu=True)[1]
+    for kw in ({"gu": gu}, {"x": x, "codes": codes, "alpha": alpha}):
+        dgu = within(rows * 2 * f, BF, lambda o: tbn.glu_bwd(dh, dgu=o.view(rows, 2 * f), **kw))
+        assert same([dgu.view(rows, 2 * f)], [tbn.glu_bwd(dh, **kw)[0]])
+    q, s = tbn.quantize_rows_i8(x)
+    wq, ws = tbn.quantize_rows_i8(torch.randn(f, c, device="cuda"))
+    for dtype in (BF, F):
+        res = torch.randn(rows, f, device="cuda").to(dtype)
+        y = within(rows * f, dtype, lambda o: tbn.matmul_i8(q, s, wq, ws, residual=res, y=o.view(rows, f)))
+        assert same([y.view(rows, f)], [tbn.matmul_i8(q, s, wq, ws, residual=res, out_dtype=dtype)])
+
+
 def _calls(tbn):
     net = Net(tbn, 20)
     codes, alpha = tbn.quantize(net.w[0])[:2]
