@@ -405,7 +405,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N * GROUPS, GROUPS > 1 ? 1 : 2
 }
 
 // ---- up to 16 rows -----------------------------------------------------------------------
-// The codes are read once and bound it: 59 MB of 4096 -> 2 x 28672 in 18.4 us for 1 row (3.2 TB/s), in 21.4 us for 16.  Lane
+// The codes are read once, 59 MB of 4096 -> 2 x 28672 in 18.4 us for 1 row (3.2 TB/s), in 21.4 us for 16; their reading and their
+// decoding bound it together, two vector operations a pair (not decoded, 16 rows take 15.6 us; with x of one row read alone 21.1).  Lane
 // (f = l % 16, q = l / 16) reads, of filter f of 16, the 16 bytes of element block ib + q and, of row f of x, the same 64
 // features; matrix instruction s of a step takes elements 8 s .. 8 s + 7 of each block (the order of the elements is the
 // same in both operands, which is all that a sum asks).
