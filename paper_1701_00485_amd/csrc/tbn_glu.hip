@@ -424,7 +424,7 @@ __device__ __forceinline__ bf16x8 decode_half(uint32_t w) {
 // Of up to 4096 SL features: a block, one a compute unit, owns a range of the groups of 16 gates and the others of the same columns.
 // Wave (i, j) of its KS x GS keeps x's steps i, i + KS, .. of 256 features in registers and streams the codes of groups j, j + GS, ..,
 // four (SL 2: two) ahead; the KS sums of an output meet in LDS, four groups a wave at a time.  Without x in registers, a block for
-// each 64 gates (glu_few_kernel): 26.5 us for 16 rows of 4096 -> 2 x 28672, and 7.6 for 1 x 512 -> 2 x 1024, 3.6 here.
+// each 64 gates or 16 (glu_few_kernel): 26.5 us for 16 rows of 4096 -> 2 x 28672, and 3.9 for 1 x 512 -> 2 x 1024, 3.5 here.
 template <int SL, int ACT>
 __global__ __launch_bounds__(1024) void glu_stream_kernel(const GluArgs a, int KS, int GS) {
     constexpr int BATCH = 4, AHEAD = SL == 1 ? 4 : 2;
