@@ -592,7 +592,7 @@ hipError_t launch_products(const Products& a, const Plan& p, hipStream_t s) {
     return p.tile == 128 ? launch_tile<128, 2, 2, 2>(a, p, s) : launch_tile<64, 2, 2, 3>(a, p, s);
 }
 
-// Words on their way into the workspace, some 4000 bytes a launch.
+// Words on their way into the workspace, some 4000 bytes a launch.  A launch that fails is the last one, and what follows is dropped.
 struct Writer {
     Words w;
     uint32_t* next;
@@ -601,7 +601,7 @@ struct Writer {
     Writer(void* to, hipStream_t stream) : next(static_cast<uint32_t*>(to)), s(stream), e(hipSuccess) { w.n = 0; }
     void put(const void* p, int n) {
         const uint32_t* v = static_cast<const uint32_t*>(p);
-        for (int i = 0; i < n; ++i) {
+        for (int i = 0; i < n && e == hipSuccess; ++i) {
             if (w.n == 0) w.to = next;
             w.word[w.n++] = v[i];
             ++next;

@@ -1,6 +1,9 @@
 """What the gated block, Muon's step and the 8-bit products refuse, on the CPU: every call here fails its checks before
 anything is launched (through the C ABI on addresses that are never followed, through Python on host tensors)."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -178,3 +181,29 @@ def test_muon_workspace_grows_with_its_matrices():
     assert 0 < a < b and b >= 4 * 1000 * 2000 * 4
     # many matrices share launches up to 64, and the workspace of one group
     assert tbn.muon_workspace_size(small * 200) == tbn.muon_workspace_size(small * 64)
+
+
+# A step's tables take 34 words a matrix and 36 lists of its matrices, 1000 words a launch: one launch for 1 matrix, two for 20,
+# more for 29 and up.
+_WITHOUT_A_GPU = """
+import ctypes, paper_1701_00485_amd as tbn
+lib = tbn.load()
+for n in (1, 20, 29, 40, 64, 200):
+    t, b = (tbn.MuonTensor * n)(), ctypes.c_size_t()
+    for i in range(n):
+        t[i] = tbn.MuonTensor(0x10000000 + i * 0x1000, 0x20000000 + i * 0x1000, 0x30000000, 8, 16, 0.0, 1.0)
+    h = tbn.MuonHyper(0.02, 0.95, 1e-7, 5, 1, None)
+    assert lib.tbn_muon_workspace_size(t, n, ctypes.byref(b)) == 0
+    print(n, lib.tbn_muon_step(t, n, 1, ctypes.byref(h), 0x40000000, b.value, None), lib.tbn_last_error().decode())
+"""
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="launches have to fail")
+def test_muon_reports_a_launch_that_failed():
+    """Without a GPU the first launch of a step fails: every length of list has that error, and the tables' other words go nowhere."""
+    r = subprocess.run([sys.executable, "-c", _WITHOUT_A_GPU], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                       stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=120)
+    assert r.returncode == 0, r.stdout[-2000:]
+    said = [line.split(" ", 2) for line in r.stdout.splitlines() if line.split(" ", 1)[0].isdigit()]
+    assert [s[0] for s in said] == ["1", "20", "29", "40", "64", "200"]
+    assert all(s[1] == "6" and s[2].startswith("tbn_muon_step: ") and s[2] == said[0][2] for s in said), said
