@@ -19,13 +19,18 @@ namespace {
 //   silu  g s, s = 1 / (1 + e^-g);            s (1 + g (1 - s))
 //   gelu  g phi, phi = (1 + erf(g / sqrt 2)) / 2;   phi + g e^(-g^2 / 2) / sqrt(2 pi)
 //   relu  max(g, 0);                          1 where g > 0, else 0
-// silu's exponential is the hardware's 2^x of a rounded product (off by |g| 2^-24 of itself), its quotient the hardware's reciprocal
-// (2^-23): expf and a division take twice the operations, 803 us for 783 of 8192 x 4096 -> 2 x 8192.
+// silu's exponential is the hardware's 2^t of t = -|g| log2 e rounded, times 1 + (-|g| - t ln 2), what the rounding left (else e^-80 is off
+// by 30 steps of fp32; now every silu of a bf16 gate by at most 1.9e-7 of itself).  Of -|g| it never overflows, and 1 - s is a quotient too, not
+// a difference.  8192 x 4096 -> 2 x 8192: 826 us, with 2^(-g log2 e) alone 816.
 template <bool SLOPE>
 __device__ __forceinline__ float activate(int act, float g, float* slope) {
     if (act == TBN_ACT_SILU) {
-        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g));
-        if (SLOPE) *slope = s * (1.0f + g * (1.0f - s));
+        const float a = fminf(fabsf(g), 128.0f);  // (e^-128 is 0 here; of NaN anything, which g carries on)
+        const float t = -1.44269504f * a, e = __builtin_amdgcn_exp2f(t);
+        const float p = fmaf(e, fmaf(1.90465421e-9f, t, fmaf(-0.69314718f, t, -a)), e);  // e^-|g|; ln 2 in two parts
+        const float y = __builtin_amdgcn_rcpf(1.0f + p), q = p * y;
+        const float s = g < 0.0f ? q : y;
+        if (SLOPE) *slope = s * (1.0f + g * (g < 0.0f ? y : q));
         return g * s;
     }
     if (act == TBN_ACT_GELU) {
