@@ -500,8 +500,8 @@ tbn_status tbn_adapter_bwd(const tbn_adapter_desc* desc, const void* x, tbn_dtyp
 /*
  * A gated block of two-bit filters: f gates and f further filters over the same c features,
  *   g = alpha_k (x W~) of filters 0 .. f - 1,  u = that of filters f .. 2 f - 1,  h = act(g) u,
- * in one pass; act is g / (1 + e^-g) (SILU), g (1 + erf(g / sqrt 2)) / 2 (GELU) or max(g, 0) (RELU), in fp32, silu within
- * 2^-20 of itself (what is below 2^-119 may come as 0).  The 2 f filters are those of one layer (tbn_quantize of a [2 f][c]
+ * in one pass; act is g / (1 + e^-g) (SILU), g (1 + erf(g / sqrt 2)) / 2 (GELU) or max(g, 0) (RELU), in fp32, silu and gelu
+ * within 2^-20 of themselves (what is below 2^-119 may come as 0).  The 2 f filters are those of one layer (tbn_quantize of a [2 f][c]
  * matrix), so that the rest of its backward pass is that of a layer of 2 f filters.
  *   x      [rows][c] bf16.   codes, alpha: TBN2 codes and scales of the 2 f filters.
  *   h      [rows][f], dtype ht.
