@@ -170,7 +170,7 @@ __device__ __forceinline__ void finish1(const GluArgs& a, int64_t m, int32_t k, 
 // A block owns BM rows and NH gates with the NH others of the same columns, so that a lane holds the g and the u of an
 // output.  Rows of x go through LDS as in tbn_nt.h (64 features a stage, a ring of STAGES); of the 2 NH filters the
 // stage's codes, 16 bytes each, decoded in registers into bf16 pairs, two operations a pair, between the matrix instructions that
-// bound it: 8192 x 4096 -> 2 x 8192 in 783 us, 1.40 PFLOP/s (copies issued at a stage's begin and operands made in a row: 857 of then 800).
+// bound it: 8192 x 4096 -> 2 x 8192 in 784 to 828 us, 1.33 to 1.40 PFLOP/s (copies issued at a stage's begin and operands made in a row: 857 of then 800).
 // Two blocks of 128 x 128 a compute unit, each with a barrier a stage, do as well as one of 256 x 128.
 // GROUPS groups of such waves, each with a part of the stages and a ring of its own, serve tiles that are too few to fill the GPU; the
 // first adds the others' sums.
@@ -682,8 +682,9 @@ hipError_t launch(const GluArgs& a, const uint16_t* gu, hipStream_t s) {
 #undef TBN_FEW
         return hipGetLastError();
     }
-    // The largest tile that leaves no more than a third of the 256 compute units idle; below one tile a unit, tiles whose stages
-    // groups of waves divide.  Times in us:
+    // The largest tile of which there are enough for the 256 compute units: 160 of 128 x 128 (up to three units in eight are idle), 192 of
+    // 128 x 64 (one in four); else 64 x 64, up to 256 of them, one a unit, in groups of waves that divide the stages where these are many, and up to
+    // 128 as 64 x 32 so.  Times in us:
     //   rows x c -> 2 x f          128x128  128x64  64x64  64x64 x 4  64x32 x 4
     //   8192 x 4096 -> 2 x 8192      800      936    1051                         (256 x 128 by four or eight waves: 798, 814)
     //    768 x 4096 -> 2 x 4096       51.0     54.2    54.2    63.9      88.8     192 tiles of 128 x 128

@@ -426,8 +426,9 @@ hipError_t launch_matmul_i8(const RowsI8Args& a, hipStream_t s) {
         hipLaunchKernelGGL((matvec_i8_kernel<4, 4>), dim3((unsigned)((a.n + 15) / 16)), dim3(256), 0, s, a);
         return hipGetLastError();
     }
-    // The largest tile that leaves no more than a quarter of the 256 compute units idle; below one tile a unit, tiles whose
-    // stages four groups of waves divide.  128 x 128 by four waves, two blocks a unit, or by eight, one.  Times in us, c 4096:
+    // The largest tile of which there are enough for the 256 compute units: 128 x 128 by four waves, two blocks a unit, from 257 on (or 256 x 256,
+    // whichever takes less time in rounds), by eight, one a unit, from 160 on (up to three units in eight are idle); 128 x 64 from 256 on; else 64 x 64,
+    // up to 256 of them in four groups of waves that divide the stages where these are many.  Times in us, c 4096:
     //   rows x n        256x256  128x128/4  128x128/8  128x64  64x64  64x64 x 4
     //   8192 x 8192      241       256        334        343    401     657
     //   4000 x 4097      118        90                                126        272 tiles of 256 x 256
